@@ -335,6 +335,68 @@ int sa_layernorm_quant(const float *x, long T, int E, const float *gamma, const 
                        float *logits_or_null, void *stream);
 
 /*
+ * Training of the parts around the Linears: LayerNorm, router, gate and balance loss.  The calls below take rows of several
+ * element types; a residual stream (x, dres, dx; dy of the combine) has the type of the rows it meets (y, dy; src, dsrc), or is
+ * SA_F32 under rows of any type.  Sums, statistics and parameter gradients are fp32 or wider, an output is rounded once (to
+ * nearest even), and every sum has a fixed order: a call repeated gives the same bits.
+ */
+#define SA_F32 0
+#define SA_F16 1
+#define SA_BF16 2
+
+/*
+ * LayerNorm of training, biased variance, that leaves what its gradient needs:
+ *   mean[t] = sum_j x[t, j] / E,   rstd[t] = 1 / sqrt(sum_j (x[t, j] - mean[t])^2 / E + eps)
+ *   y[t, j] = (x[t, j] - mean[t]) * rstd[t] * gamma[j] + beta[j]
+ *   logits[t, :] = y[t, :] * wg + bg          the router G of Sec. 4.2, of y before it is rounded to y_type
+ *   x [T, E] of x_type, y_or_null [T, E] of y_type, mean_or_null and rstd_or_null fp32 [T], gamma, beta fp32 [E],
+ *   wg fp32 [E, n_experts], bg fp32 [n_experts], logits_or_null fp32 [T, n_experts], 2 <= n_experts <= 8.
+ * Any E from 1 to 8192 (16-byte alignment is asked of the buffers, not of the rows).  y may be x where the types are the same.
+ */
+int sa_layernorm(const void *x, int x_type, long T, int E, const float *gamma, const float *beta, float eps,
+                 void *y_or_null, int y_type, float *mean_or_null, float *rstd_or_null, const float *wg_or_null,
+                 const float *bg_or_null, int n_experts, float *logits_or_null, void *stream);
+
+/*
+ * Its gradient, with that of the residual around it (Eq. 2: x enters the sum as well) and that of the router behind it:
+ *   h[t, j]  = dy[t, j] + sum_e dlogits[t, e] * wg[j, e]          (without dlogits: dy)
+ *   xh[t, j] = (x[t, j] - mean[t]) * rstd[t],   g = h * gamma
+ *   dx[t, j] = dres[t, j] + rstd[t] * (g[t, j] - sum_i g[t, i] / E - xh[t, j] * sum_i g[t, i] * xh[t, i] / E)
+ *   dgamma[j] = sum_t h[t, j] * xh[t, j],   dbeta[j] = sum_t h[t, j]
+ *   dwg[j, e] = sum_t (xh[t, j] * gamma[j] + beta[j]) * dlogits[t, e],   dbg[e] = sum_t dlogits[t, e]
+ *   dy [T, E] of y_type; x, dres_or_null, dx [T, E] of x_type; mean and rstd fp32 [T] as sa_layernorm left them, or both NULL:
+ *   then they are computed again from x and eps (behind a forward pass that keeps none, as sa_layernorm_quant).
+ * Parameter gradients (fp32 [E], [E], [E, n_experts], [n_experts]): dgamma and dbeta both or neither, dwg and dbg both or
+ * neither and only with dlogits and the other two.  accumulate != 0 adds them to what the buffers hold.  beta is read for dwg only.
+ * T = 0 leaves sums of nothing (zeros, or with accumulate the buffers as they are).  dx may be dres, dy or x (of the same type).
+ * Without parameter gradients no workspace is needed (the query is for calls with them).
+ */
+size_t sa_layernorm_backward_workspace_bytes(long T, int E, int n_experts /* 0: without dlogits */);
+int sa_layernorm_backward(const void *dy, int y_type, const void *x, int x_type, long T, int E, const float *gamma,
+                          const float *beta_or_null, float eps, const float *mean_or_null, const float *rstd_or_null,
+                          const void *dres_or_null, const float *dlogits_or_null, const float *wg_or_null, int n_experts,
+                          void *dx, float *dgamma_or_null, float *dbeta_or_null, float *dwg_or_null, float *dbg_or_null,
+                          int accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The balancing loss of Eq. 4 as a training step has it: both values, the tokens of each expert and the gradient
+ *   dlogits = d(dlosses[0] * losses[0] + dlosses[1] * losses[1]) / dlogits
+ * with IMP, LOAD, p, q and SCV as for sa_moe_balance_loss.  The maximum of the other experts in q_i is that of their logits, ties to
+ * the lowest index; the gradient goes to that one.
+ *   logits [T, E] fp32; alpha [E] fp32; dlosses fp32 [2], the weights of both losses (device memory: a loss scale may be in them);
+ *   valid_or_null uint8 [T]: a token of 0 is padding, counts for nothing, its logits may hold anything and its gradient is 0;
+ *   losses fp32 [2]; sums_or_null fp32 [2, E] = IMP then LOAD; counts_or_null int32 [E], tokens whose largest logit is the expert's
+ *   (ties to the lowest index, as sa_moe_dispatch counts all tokens); dlogits [T, E] fp32.
+ * accumulate != 0 adds the gradient to dlogits (where that of the combine is).  Where no token counts, or the mean of a loss is 0,
+ * that loss and its gradient are 0.  2 <= E <= 8, 0 <= T < 2^31, noise_std > 0.  Sums over tokens are fp64 in a fixed order.
+ */
+size_t sa_moe_balance_loss_grad_workspace_bytes(long T, int E);
+int sa_moe_balance_loss_grad(const float *logits, long T, int E, const uint8_t *valid_or_null, const float *alpha,
+                             float noise_std, const float *dlosses, float *losses, float *sums_or_null,
+                             int32_t *counts_or_null, float *dlogits, int accumulate, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
+/*
  * Between the two shift linears of the Shift expert:
  *   h = lut[clamp(rne(float(y) * s), -127, 127) + 128],  lut int8 [256].
  */
@@ -407,6 +469,20 @@ int sa_gather_rows(const void *src, size_t row_bytes, const sa_rows *rows, void 
                    void *stream);
 int sa_combine_rows(const float *src, const sa_rows *rows, const float *gate_or_null, int E,
                     float *y, void *stream);
+/*
+ * The gradient of combine and of the gate behind it (gate[t] = p_e, the largest of p = softmax(logits[t, :]), ties to the lowest
+ * index, as sa_moe_dispatch leaves it), for each selected row r = rows[i]:
+ *   dsrc[i, :]   = gate[r] * dy[r, :]
+ *   dgate[r]     = sum_j dy[r, j] * src[i, j]
+ *   dlogits[r,k] = dgate[r] * p_e * ((k == e) - p_k)
+ *   dy of y_type (rows as y has them), src and dsrc_or_null [max_rows, E] of src_type, gate_or_null, dgate_or_null fp32 [T] and
+ *   logits_or_null, dlogits_or_null fp32 [T, n_experts].  At least one of the outputs; dlogits needs logits and gate, dgate and
+ *   dlogits need src.  Any E >= 1, 2 <= n_experts <= 8.  With perm as rows and no counts, one call does the rows of all experts, src
+ *   in the order of perm.  Rows that are not selected are left as they are; a row may be selected once only.  dsrc may be src.
+ */
+int sa_combine_rows_backward(const void *dy, int y_type, const void *src_or_null, int src_type, const sa_rows *rows,
+                             const float *gate_or_null, const float *logits_or_null, int n_experts, int E,
+                             void *dsrc_or_null, float *dgate_or_null, float *dlogits_or_null, void *stream);
 
 /*
  * One pass of the block (Eq. 2 restricted to the reparameterised parts):

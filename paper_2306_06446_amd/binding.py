@@ -29,7 +29,11 @@ EXPORTS = [
     "sa_shift_mlp_workspace_bytes", "sa_shift_mlp", "sa_mult_mlp_workspace_bytes",
     "sa_mult_mlp_f16", "sa_mult_mlp_f16_half", "sa_gather_rows", "sa_combine_rows", "sa_block_workspace_bytes",
     "sa_block_forward", "sa_moe_linear_workspace_bytes", "sa_moe_linear", "sa_probe_mfma", "sa_layer_workspace_bytes", "sa_layer_forward",
+    "sa_layernorm", "sa_layernorm_backward_workspace_bytes", "sa_layernorm_backward", "sa_moe_balance_loss_grad_workspace_bytes",
+    "sa_moe_balance_loss_grad", "sa_combine_rows_backward",
 ]
+
+_ROW_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}      # SA_F32, SA_F16, SA_BF16
 
 
 class SAError(RuntimeError):
@@ -83,6 +87,13 @@ def load_library():
                      "sa_shift_mlp_workspace_bytes", "sa_mult_mlp_workspace_bytes",
                      "sa_block_workspace_bytes", "sa_layer_workspace_bytes", "sa_moe_linear_workspace_bytes"):
             getattr(lib, name).restype = ctypes.c_size_t
+        P, I, L, F, Z = ctypes.c_void_p, ctypes.c_int, ctypes.c_long, ctypes.c_float, ctypes.c_size_t
+        for name, args in (("sa_layernorm_backward_workspace_bytes", (L, I, I)), ("sa_moe_balance_loss_grad_workspace_bytes", (L, I))):
+            getattr(lib, name).restype, getattr(lib, name).argtypes = Z, args
+        lib.sa_layernorm.argtypes = (P, I, L, I, P, P, F, P, I, P, P, P, P, I, P, P)
+        lib.sa_layernorm_backward.argtypes = (P, I, P, I, L, I, P, P, F, P, P, P, P, P, I, P, P, P, P, P, I, P, Z, P)
+        lib.sa_moe_balance_loss_grad.argtypes = (P, L, I, P, P, F, P, P, P, P, P, I, P, Z, P)
+        lib.sa_combine_rows_backward.argtypes = (P, I, P, I, P, P, P, I, I, P, P, P, P)
         _lib = lib
     return _lib
 
@@ -118,6 +129,29 @@ def _z(x):
 def _rows(rows=None, counts=None, expert=0, max_rows=0):
     return SaRows(None if rows is None else rows.data_ptr(),
                   None if counts is None else counts.data_ptr(), expert, max_rows)
+
+
+def _address(t, device, name, shape=None, dtype=None):
+    """The address of an argument of the training operators, None for None.  A wrong shape or type would have a kernel read or write past
+    the tensor, another device than the current one is not what the stream works on: refused, like what is not contiguous."""
+    if t is None:
+        return None
+    if t.device != device or not t.is_contiguous():
+        raise ValueError("%s: a contiguous tensor on %s is needed" % (name, device))
+    if shape is not None and t.shape != shape:
+        raise ValueError("%s: shape %s is needed, not %s" % (name, tuple(shape), tuple(t.shape)))
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError("%s: %s is needed, not %s" % (name, dtype, t.dtype))
+    return t.data_ptr()
+
+
+def _current_device(t, name, dtypes, dims=2):
+    """The device that all arguments have to be on, and the stream of it, from a call's first tensor."""
+    if t.dim() != dims or t.dtype not in dtypes:
+        raise ValueError("%s: %d dimensions of %s are needed" % (name, dims, ", ".join(str(d) for d in dtypes)))
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError("%s: is on %s, which is not the current GPU" % (name, t.device))
+    return t.device, torch.cuda.current_stream().cuda_stream
 
 
 def _workspace(nbytes, device):
@@ -497,6 +531,131 @@ def sa_combine_rows(src, y, rows=None, counts=None, expert=0, max_rows=None, gat
     _check(load_library().sa_combine_rows(_ptr(src), ctypes.byref(r), _ptr(gate), src.shape[1], _ptr(y),
                                           _stream()))
     return y
+
+
+def sa_layernorm(x, gamma, beta, eps, y_dtype=None, want_y=True, want_stats=True, wg=None, bg=None, y=None, mean=None, rstd=None,
+                 logits=None):
+    """LayerNorm of training on x [T, E] (fp32, fp16, bf16): returns (y, mean, rstd, logits); entries not asked for are None."""
+    lib = load_library()
+    dev, stream = _current_device(x, "x", _ROW_TYPES)
+    T, E = x.shape
+    if y is None and want_y:
+        y = torch.empty((T, E), dtype=y_dtype or x.dtype, device=dev)
+    if want_stats:
+        mean = torch.empty(T, dtype=torch.float32, device=dev) if mean is None else mean
+        rstd = torch.empty(T, dtype=torch.float32, device=dev) if rstd is None else rstd
+    n = 0 if wg is None else wg.shape[1]
+    if logits is None and wg is not None:
+        logits = torch.empty((T, n), dtype=torch.float32, device=dev)
+    f32 = torch.float32
+    y_type = _ROW_TYPES[x.dtype if y is None else y.dtype]
+    _check(lib.sa_layernorm(
+        _address(x, dev, "x"), _ROW_TYPES[x.dtype], T, E, _address(gamma, dev, "gamma", (E,), f32), _address(beta, dev, "beta", (E,), f32),
+        eps, _address(y, dev, "y", (T, E)), y_type, _address(mean, dev, "mean", (T,), f32), _address(rstd, dev, "rstd", (T,), f32),
+        _address(wg, dev, "wg", (E, n), f32), _address(bg, dev, "bg", (n,), f32), n, _address(logits, dev, "logits", (T, n), f32), stream))
+    return y, mean, rstd, logits
+
+
+def sa_layernorm_backward_workspace_bytes(T, E, n_experts=0):
+    return load_library().sa_layernorm_backward_workspace_bytes(T, E, n_experts)
+
+
+def sa_layernorm_backward(dy, x, gamma, beta, eps, mean=None, rstd=None, dres=None, dlogits=None, wg=None, want_params=True, dx=None,
+                          dgamma=None, dbeta=None, dwg=None, dbg=None, accumulate=False, workspace=None):
+    """Gradient of sa_layernorm, of the residual around it (dres) and of the router behind it (dlogits, wg): returns
+    (dx, dgamma, dbeta, dwg, dbg); entries not asked for are None.  accumulate: onto the parameter gradients given."""
+    lib = load_library()
+    dev, stream = _current_device(x, "x", _ROW_TYPES)
+    T, E = x.shape
+    f32 = torch.float32
+    n = 0 if dlogits is None else dlogits.shape[-1]
+    if dx is None:
+        dx = torch.empty_like(x)
+    if want_params:
+        if accumulate and (dgamma is None or dbeta is None or (n and (dwg is None or dbg is None))):
+            raise ValueError("accumulate: the parameter gradients to add to are needed")
+        dgamma = torch.empty(E, dtype=f32, device=dev) if dgamma is None else dgamma
+        dbeta = torch.empty(E, dtype=f32, device=dev) if dbeta is None else dbeta
+        if n:
+            dwg = torch.empty((E, n), dtype=f32, device=dev) if dwg is None else dwg
+            dbg = torch.empty(n, dtype=f32, device=dev) if dbg is None else dbg
+        if workspace is None:
+            workspace = _workspace(lib.sa_layernorm_backward_workspace_bytes(T, E, n), dev)
+    elif dgamma is not None or dbeta is not None or dwg is not None or dbg is not None:
+        raise ValueError("want_params: buffers of parameter gradients are given, but none are wanted")
+    if dy.dtype not in _ROW_TYPES:
+        raise ValueError("dy: %s is no type of rows" % dy.dtype)
+    _check(lib.sa_layernorm_backward(
+        _address(dy, dev, "dy", (T, E)), _ROW_TYPES[dy.dtype], _address(x, dev, "x"), _ROW_TYPES[x.dtype], T, E,
+        _address(gamma, dev, "gamma", (E,), f32), _address(beta, dev, "beta", (E,), f32), eps, _address(mean, dev, "mean", (T,), f32),
+        _address(rstd, dev, "rstd", (T,), f32), _address(dres, dev, "dres", (T, E), x.dtype), _address(dlogits, dev, "dlogits", (T, n), f32),
+        _address(wg, dev, "wg", (E, n), f32) if n else None, n, _address(dx, dev, "dx", (T, E), x.dtype),
+        _address(dgamma, dev, "dgamma", (E,), f32), _address(dbeta, dev, "dbeta", (E,), f32), _address(dwg, dev, "dwg", (E, n), f32),
+        _address(dbg, dev, "dbg", (n,), f32), int(bool(accumulate)), _address(workspace, dev, "workspace"),
+        0 if workspace is None else workspace.numel() * workspace.element_size(), stream))
+    return dx, dgamma, dbeta, dwg, dbg
+
+
+def sa_moe_balance_loss_grad_workspace_bytes(T, E):
+    return load_library().sa_moe_balance_loss_grad_workspace_bytes(T, E)
+
+
+def sa_moe_balance_loss_grad(logits, alpha, noise_std, dlosses, valid=None, losses=None, sums=None, counts=None, dlogits=None,
+                             accumulate=False, workspace=None):
+    """Eq. 4 with its gradient: returns (losses [2], sums [2, E], counts [E], dlogits [T, E]).  valid: uint8 or bool [T], 0 is padding;
+    accumulate: onto the dlogits given."""
+    lib = load_library()
+    dev, stream = _current_device(logits, "logits", (torch.float32,))
+    T, E = logits.shape
+    f32 = torch.float32
+    if accumulate and dlogits is None:
+        raise ValueError("accumulate: the gradient to add to is needed")
+    losses = torch.empty(2, dtype=f32, device=dev) if losses is None else losses
+    sums = torch.empty((2, E), dtype=f32, device=dev) if sums is None else sums
+    counts = torch.empty(E, dtype=torch.int32, device=dev) if counts is None else counts
+    dlogits = torch.empty_like(logits) if dlogits is None else dlogits
+    if workspace is None:
+        workspace = _workspace(lib.sa_moe_balance_loss_grad_workspace_bytes(T, E), dev)
+    if valid is not None and valid.dtype == torch.bool:
+        valid = valid.view(torch.uint8)
+    _check(lib.sa_moe_balance_loss_grad(
+        _address(logits, dev, "logits"), T, E, _address(valid, dev, "valid", (T,), torch.uint8), _address(alpha, dev, "alpha", (E,), f32),
+        noise_std, _address(dlosses, dev, "dlosses", (2,), f32), _address(losses, dev, "losses", (2,), f32),
+        _address(sums, dev, "sums", (2, E), f32), _address(counts, dev, "counts", (E,), torch.int32),
+        _address(dlogits, dev, "dlogits", (T, E), f32), int(bool(accumulate)), _address(workspace, dev, "workspace"),
+        workspace.numel() * workspace.element_size(), stream))
+    return losses, sums, counts, dlogits
+
+
+def sa_combine_rows_backward(dy, src, rows=None, counts=None, expert=0, max_rows=None, gate=None, logits=None, want_dsrc=True,
+                             dsrc=None, dgate=None, dlogits=None):
+    """Gradient of sa_combine_rows and of the gate: returns (dsrc, dgate, dlogits); dlogits is None without logits.  What is made here
+    holds zeros where no row is selected."""
+    lib = load_library()
+    dev, stream = _current_device(dy, "dy", _ROW_TYPES)
+    T, E = dy.shape
+    f32 = torch.float32
+    if max_rows is None:
+        max_rows = src.shape[0]
+    new = torch.empty if rows is None and counts is None and max_rows == T else torch.zeros
+    if dsrc is None and want_dsrc:
+        dsrc = new((src.shape[0], E), dtype=src.dtype, device=dev)
+    if dgate is None:
+        dgate = new(T, dtype=f32, device=dev)
+    n = 0 if logits is None else logits.shape[1]
+    if dlogits is None and logits is not None:
+        dlogits = new((T, n), dtype=f32, device=dev)
+    if src.dtype not in _ROW_TYPES:
+        raise ValueError("src: %s is no type of rows" % src.dtype)
+    if max_rows > src.shape[0] or (rows is None and max_rows > T) or (rows is not None and counts is None and max_rows > rows.numel()):
+        raise ValueError("max_rows: %d rows are more than there are" % max_rows)
+    r = SaRows(_address(rows, dev, "rows", None, torch.int32), _address(counts, dev, "counts", None, torch.int32), expert, max_rows)
+    _check(lib.sa_combine_rows_backward(
+        _address(dy, dev, "dy"), _ROW_TYPES[dy.dtype], _address(src, dev, "src", (src.shape[0], E)), _ROW_TYPES[src.dtype], ctypes.byref(r),
+        _address(gate, dev, "gate", (T,), f32), _address(logits, dev, "logits", (T, n), f32), n, E,
+        _address(dsrc, dev, "dsrc", src.shape, src.dtype), _address(dgate, dev, "dgate", (T,), f32),
+        _address(dlogits, dev, "dlogits", (T, n), f32), stream))
+    return dsrc, dgate, dlogits
 
 
 class Block:
