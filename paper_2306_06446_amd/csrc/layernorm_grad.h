@@ -1,0 +1,285 @@
+// The gradient of LayerNorm with the residual's and the router's (layernorm_train.hip has the formulas): one pass over the rows.
+#pragma once
+
+#include "layernorm_train.h"
+
+namespace sa {
+
+// What a lane holds of a row that is to come: asked for while the row before it is worked on.
+template <class X, class Y, class S, int ROUTE>
+struct GradRow {
+    Piece<Y, S::VEC> dy[S::CH];
+    Piece<X, S::VEC> x[S::CH], res[S::CH];
+    float mean, rstd, dl[ROUTE ? ROUTE : 1];
+
+    __device__ inline void load(const NormGradArgs &a, const RowPlace<S> &p, long t) {
+        const size_t row = (size_t)t * a.E;
+#pragma unroll
+        for (int c = 0; c < S::CH; ++c) {
+            dy[c].load(static_cast<const Y *>(a.dy) + row + p.at[c]);
+            x[c].load(static_cast<const X *>(a.x) + row + p.at[c]);
+            if (a.dres) res[c].load(static_cast<const X *>(a.dres) + row + p.at[c]);
+        }
+        if (a.mean) mean = a.mean[t], rstd = a.rstd[t];
+        if constexpr (ROUTE > kStreamed) {
+#pragma unroll
+            for (int e = 0; e < ROUTE; ++e) dl[e] = e < a.n ? a.dlogits[(size_t)t * a.n + e] : 0.0f;
+        }
+    }
+};
+
+// A lane's registers, in all: the sums and parameters of its columns, and a row with its normalised values; with another row under way?
+template <class X, class Y, class S, int ROUTE>
+struct GradPlan {
+    static constexpr int HELD = ROUTE > kStreamed ? ROUTE : 0;
+    static constexpr int ELEMS = S::VEC * S::CH;
+    static constexpr int ROW = ELEMS * (2 * sizeof(X) + sizeof(Y)) / 4;
+    static constexpr bool AHEAD = ELEMS * (2 + HELD + 1 + HELD + 2) + 2 * ROW + 48 < 256;
+};
+
+template <class X, class Y, class S, int ROUTE>
+__global__ __launch_bounds__(S::THREADS) void norm_grad_kernel(NormGradArgs a) {
+    using Plan = GradPlan<X, Y, S, ROUTE>;
+    constexpr int VEC = S::VEC, CH = S::CH, HELD = Plan::HELD, Q = 2 + HELD;
+    constexpr bool AHEAD = Plan::AHEAD;
+    constexpr int PC = HELD ? CH : 1, PR = HELD ? HELD : 1;
+    __shared__ float red[S::LANES > 64 ? 2 : 1][2][S::WAVES];
+    __shared__ float side[S::GROUPS > 1 ? S::THREADS * CH * VEC : 1], side_dl[S::GROUPS][PR];
+    const int g = threadIdx.x / S::LANES, l = threadIdx.x % S::LANES;
+    const RowPlace<S> p(l, a.E);
+    const float per = 1.0f / (float)a.E;
+    RowSums<S, 2> sums{red};
+    // gamma is 0 in the elements that are not this lane's: they drop out of the row's sums by it
+    float gm[CH][VEC], w[PR][PC][VEC];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const int j = p.at[c] + i;
+            gm[c][i] = p.mine(c, i) ? a.gamma[j] : 0.0f;
+#pragma unroll
+            for (int e = 0; e < HELD; ++e) w[e][c][i] = e < a.n ? a.wg[(size_t)j * a.n + e] : 0.0f;
+        }
+    float acc[Q][CH][VEC], dl_sum[PR];
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) acc[q][c][i] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < PR; ++e) dl_sum[e] = 0.0f;
+
+    const long stride = (long)gridDim.x * S::GROUPS;
+    auto clamped = [&](long t) { return t < a.T ? t : a.T - 1; };
+    GradRow<X, Y, S, ROUTE> nxt;
+    long t0 = (long)blockIdx.x * S::GROUPS;
+    if constexpr (AHEAD) nxt.load(a, p, clamped(t0 + g));
+    for (; t0 < a.T; t0 += stride) {
+        const long t = t0 + g;
+        if constexpr (!AHEAD) nxt.load(a, p, clamped(t));
+        const GradRow<X, Y, S, ROUTE> r = nxt;
+        if (AHEAD && t0 + stride < a.T) nxt.load(a, p, clamped(t + stride));
+        float mean = r.mean, rstd = r.rstd, s[2];
+        if (!a.mean) {
+            s[0] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) s[0] += p.mine(c, i) ? r.x[c][i] : 0.0f;
+            sums(s, 1);
+            mean = s[0] / (float)a.E;
+            s[0] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const float d = r.x[c][i] - mean;
+                    s[0] = p.mine(c, i) ? __builtin_fmaf(d, d, s[0]) : s[0];
+                }
+            sums(s, 1);
+            rstd = 1.0f / __builtin_sqrtf(s[0] / (float)a.E + a.eps);
+        }
+        float xh[CH][VEC], h[CH][VEC];
+        s[0] = s[1] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                xh[c][i] = (r.x[c][i] - mean) * rstd;
+                h[c][i] = r.dy[c][i];
+#pragma unroll
+                for (int e = 0; e < HELD; ++e) h[c][i] = __builtin_fmaf(r.dl[e], w[e][HELD ? c : 0][i], h[c][i]);
+            }
+        if constexpr (ROUTE == kStreamed) {
+            const float *dl = a.dlogits + (size_t)clamped(t) * a.n;
+#pragma unroll 1
+            for (int e = 0; e < a.n; ++e) {
+                const float *row = a.weights + e * a.by_expert;
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) h[c][i] = __builtin_fmaf(dl[e], row[(size_t)(p.at[c] + i) * a.by_column], h[c][i]);
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float gv = h[c][i] * gm[c][i];
+                s[0] += gv;
+                s[1] = __builtin_fmaf(gv, xh[c][i], s[1]);
+            }
+        sums(s);
+        if (t < a.T) {
+            const float c0 = s[0] * per, c1 = s[1] * per;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                float d[VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    acc[0][c][i] = __builtin_fmaf(h[c][i], xh[c][i], acc[0][c][i]);
+                    acc[1][c][i] += h[c][i];
+#pragma unroll
+                    for (int e = 0; e < HELD; ++e) acc[2 + e][c][i] = __builtin_fmaf(xh[c][i], r.dl[e], acc[2 + e][c][i]);
+                    d[i] = rstd * (h[c][i] * gm[c][i] - c0 - xh[c][i] * c1);
+                    if (a.dres) d[i] += r.res[c][i];
+                }
+                if (p.any(c)) store_piece<X, VEC>(static_cast<X *>(a.dx) + (size_t)t * a.E + p.at[c], d, c < S::FULL ? 0 : p.skip[c]);
+            }
+#pragma unroll
+            for (int e = 0; e < HELD; ++e) dl_sum[e] += r.dl[e];
+        }
+    }
+    if (!a.partial) return;
+    const int columns = padded_columns(a.E), n = ROUTE ? a.n : 0;
+    if constexpr (HELD > 0) {
+        // sum of y dlogits = gamma (sum of xh dlogits) + beta (sum of dlogits)
+        if (a.dwg) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const float gamma = a.gamma[p.at[c] + i], beta = a.beta[p.at[c] + i];
+#pragma unroll
+                    for (int e = 0; e < HELD; ++e) acc[2 + e][c][i] = __builtin_fmaf(gamma, acc[2 + e][c][i], beta * dl_sum[e]);
+                }
+        }
+    }
+    // the workgroup's part: its groups' sums in ascending order
+    float *part = a.partial + (size_t)blockIdx.x * (2 + n) * columns;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        if (q >= 2 + n) continue;
+        if constexpr (S::GROUPS == 1) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+                if (p.any(c)) store_piece<float, VEC>(part + (size_t)q * columns + p.at[c], acc[q][c], c < S::FULL ? 0 : p.skip[c]);
+        } else {
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+                if (p.any(c)) store_piece<float, VEC>(side + g * S::COLUMNS + p.at[c], acc[q][c], c < S::FULL ? 0 : p.skip[c]);
+            __syncthreads();
+            for (int j = threadIdx.x; j < a.E; j += S::THREADS) {
+                float s = side[j];
+#pragma unroll
+                for (int k = 1; k < S::GROUPS; ++k) s += side[k * S::COLUMNS + j];
+                part[(size_t)q * columns + j] = s;
+            }
+        }
+    }
+    if constexpr (HELD > 0) {
+        __syncthreads();
+        if (l == 0) {
+#pragma unroll
+            for (int e = 0; e < HELD; ++e) side_dl[g][e] = dl_sum[e];
+        }
+        __syncthreads();
+        if ((int)threadIdx.x < HELD) {
+            float s = 0.0f;
+            for (int k = 0; k < S::GROUPS; ++k) s += side_dl[k][threadIdx.x];
+            a.partial_dbg[(size_t)blockIdx.x * kMaxExperts + threadIdx.x] = s;
+        }
+    }
+}
+
+// kStreamed: the sums of y dlogits over a part's rows, for a block of columns.
+constexpr int kRouterColumns = 1024;         // of a workgroup
+template <class X>
+__global__ __launch_bounds__(256) void norm_grad_router_kernel(NormGradArgs a, long rows) {
+    const int n = a.n, columns = padded_columns(a.E), part = blockIdx.y;
+    const int j = (int)blockIdx.x * kRouterColumns + (int)threadIdx.x * 4, at = j + 4 <= a.E ? j : a.E - 4;
+    const long t0 = part * rows, t1 = t0 + rows < a.T ? t0 + rows : a.T;
+    float acc[kMaxExperts][4], dl_sum[kMaxExperts];
+#pragma unroll
+    for (int e = 0; e < kMaxExperts; ++e) {
+        dl_sum[e] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[e][i] = 0.0f;
+    }
+#pragma unroll 4
+    for (long t = t0; t < t1; ++t) {
+        Piece<X, 4> x;
+        x.load(static_cast<const X *>(a.x) + (size_t)t * a.E + at);
+        const float mean = a.mean[t], rstd = a.rstd[t];
+        float xh[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) xh[i] = (x[i] - mean) * rstd;
+#pragma unroll
+        for (int e = 0; e < kMaxExperts; ++e) {
+            const float dl = e < n ? a.dlogits[(size_t)t * n + e] : 0.0f;
+            dl_sum[e] += dl;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[e][i] = __builtin_fmaf(xh[i], dl, acc[e][i]);
+        }
+    }
+    float *out = a.partial + ((size_t)part * (2 + n) + 2) * columns + at;
+#pragma unroll
+    for (int e = 0; e < kMaxExperts; ++e) {
+        if (e >= n || j >= a.E) continue;
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __builtin_fmaf(a.gamma[at + i], acc[e][i], a.beta[at + i] * dl_sum[e]);
+        store_piece<float, 4>(out + (size_t)e * columns, v, j - at);
+    }
+    if (blockIdx.x == 0 && threadIdx.x < 1) {
+#pragma unroll
+        for (int e = 0; e < kMaxExperts; ++e) a.partial_dbg[(size_t)part * kMaxExperts + e] = dl_sum[e];
+    }
+}
+
+// Parts of the rows: in as few as keep every CU busy (2 workgroups to each, by their registers), the same number of steps in each.
+template <class S>
+int grad_parts(long T) {
+    const long cap = S::THREADS == 256 ? kMaxGradParts : kMaxGradParts / 2;
+    const long steps = (T + S::GROUPS * cap - 1) / (S::GROUPS * cap);
+    return (int)((T + S::GROUPS * steps - 1) / (S::GROUPS * steps));
+}
+
+template <class X, class Y>
+int launch_norm_grad_rows(const NormGradArgs &a, int *parts, hipStream_t st) {
+    constexpr int VEC = row_vec<X, Y>();
+    auto rows = [&](auto shape, auto route) {
+        using S = decltype(shape);
+        *parts = grad_parts<S>(a.T);
+        if constexpr (decltype(route)::value == kStreamed) {
+            if (a.dwg) {
+                // before dx, which may take the place of x
+                const long per = (a.T + *parts - 1) / *parts;
+                norm_grad_router_kernel<X><<<dim3((unsigned)((a.E + kRouterColumns - 1) / kRouterColumns), (unsigned)*parts), dim3(256), 0, st>>>(a, per);
+                const int rc = check_launch("sa_layernorm_backward(router)");
+                if (rc != SA_OK) return rc;
+            }
+        }
+        norm_grad_kernel<X, Y, S, decltype(route)::value><<<dim3((unsigned)*parts), dim3(S::THREADS), 0, st>>>(a);
+        return check_launch("sa_layernorm_backward(rows)");
+    };
+    auto with = [&](auto route) { return [&rows, route](auto shape) { return rows(shape, route); }; };
+    if (!a.dlogits) return by_shape<VEC>(a.E, with(std::integral_constant<int, 0>()));
+    if (a.n == 2) return by_shape<VEC>(a.E, with(std::integral_constant<int, 2>()));
+    if (a.E > kMaxRoute8Columns) return by_wide_shape<VEC>(a.E, with(std::integral_constant<int, kStreamed>()));
+    return by_shape_route8<VEC>(a.E, with(std::integral_constant<int, kMaxExperts>()));
+}
+
+}  // namespace sa

@@ -182,6 +182,11 @@ struct CombineGradArgs {
     float *dgate, *dlogits;
 };
 
+template <class T>
+__device__ inline float load_elem(const T *p) { return (float)*p; }
+template <class T>
+__device__ inline void store_elem(T *p, float v) { *p = (T)v; }
+
 // A wavefront to a row.
 template <class Y, class S>
 __global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradArgs a) {
