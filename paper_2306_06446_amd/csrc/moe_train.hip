@@ -7,6 +7,8 @@
 //   with c and f the gradients of the sums of p and q:  a = c + J^T (f phi(d) / std),  J p_i = p_i - p_o(i),  dl = p (a - <p, a>)
 #include "common.h"
 #include "layernorm.h"
+#include <type_traits>
+
 #include "row_types.h"
 
 namespace {
@@ -14,51 +16,53 @@ namespace {
 using namespace sa;
 
 constexpr int kMaxE = kMaxExperts;
-constexpr int kTok = 256;                // tokens per workgroup
 
 // A token's routing: p, and for each expert the normal deviate of its distance to the best of the others.
+template <int E>
 struct TokenRouting {
-    float p[kMaxE], z[kMaxE];
+    float p[E], z[E];
     int first, second;                   // largest and second largest logit, ties to the lowest index
 };
 
-__device__ inline TokenRouting route_token(const float *l, int E, float inv_noise_std) {
-    TokenRouting r;
-    float v[kMaxE];
+template <int E>
+__device__ inline TokenRouting<E> route_token(const float *l, float inv_noise_std) {
+    TokenRouting<E> r;
+    float v[E];
 #pragma unroll
-    for (int e = 0; e < kMaxE; ++e) v[e] = e < E ? l[e] : 0.0f;
+    for (int e = 0; e < E; ++e) v[e] = l[e];
     float l0 = v[0], l1 = v[1];
     r.first = 0, r.second = 1;
     if (l1 > l0) { const float t = l0; l0 = l1; l1 = t; r.first = 1, r.second = 0; }
 #pragma unroll
-    for (int e = 2; e < kMaxE; ++e) {
-        if (e >= E) break;
-        if (v[e] > l0) { l1 = l0, r.second = r.first, l0 = v[e], r.first = e; }
-        else if (v[e] > l1) { l1 = v[e], r.second = e; }
+    for (int e = 2; e < E; ++e) {
+        const bool best = v[e] > l0, next = v[e] > l1;
+        r.second = best ? r.first : next ? e : r.second;
+        l1 = best ? l0 : next ? v[e] : l1;
+        r.first = best ? e : r.first;
+        l0 = best ? v[e] : l0;
     }
     float den = 0.0f;
 #pragma unroll
-    for (int e = 0; e < kMaxE; ++e) {
-        r.p[e] = e < E ? expf(v[e] - l0) : 0.0f;
+    for (int e = 0; e < E; ++e) {
+        r.p[e] = expf(v[e] - l0);
         den += r.p[e];
     }
     const float inv = 1.0f / den;
     float p0 = 0.0f, p1 = 0.0f;
 #pragma unroll
-    for (int e = 0; e < kMaxE; ++e) {
+    for (int e = 0; e < E; ++e) {
         r.p[e] *= inv;
-        if (e == r.first) p0 = r.p[e];
-        if (e == r.second) p1 = r.p[e];
+        p0 = e == r.first ? r.p[e] : p0;
+        p1 = e == r.second ? r.p[e] : p1;
     }
 #pragma unroll
-    for (int e = 0; e < kMaxE; ++e) r.z[e] = (r.p[e] - (e == r.first ? p1 : p0)) * inv_noise_std;
+    for (int e = 0; e < E; ++e) r.z[e] = (r.p[e] - (e == r.first ? p1 : p0)) * inv_noise_std;
     return r;
 }
 
 struct BalanceArgs {
     const float *logits;
     long T;
-    int E;
     const uint8_t *valid;
     const float *alpha;
     float noise_std;
@@ -67,110 +71,221 @@ struct BalanceArgs {
     int32_t *counts;
     float *dlogits;
     int accumulate;
-    double *partial;         // [blocks][2 * kMaxE]: sums of p, of q
-    int32_t *partial_counts; // [blocks][kMaxE]
-    float *coeff;            // [2 * kMaxE]: c, f
+    double *partial;         // [2 E][parts]: sums of p, of q
+    int32_t *partial_counts; // [E][parts]
+    int parts;
 };
 
-__device__ inline double wave_sum_d(double v) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
+template <int CTRL>
+__device__ inline double dpp_add_d(double v) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xF, 0xF, true);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xF, 0xF, true);
+    return v + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 
-__global__ __launch_bounds__(kTok) void balance_sums_kernel(BalanceArgs a) {
-    __shared__ double red[kTok / 64][2 * kMaxE];
-    __shared__ int32_t cnt[kTok / 64][kMaxE];
-    const long t = (long)blockIdx.x * kTok + threadIdx.x;
+// Sum over a wavefront in all of its lanes, the most distant lanes first (as group_sum<64>, in fp64).
+__device__ inline double wave_sum_d(double v) {
+    v += __shfl_xor(v, 32, 64);
+    v += __shfl_xor(v, 16, 64);
+    v = dpp_add_d<0x128>(v);
+    v = dpp_add_d<0x124>(v);
+    v = dpp_add_d<0x122>(v);
+    return dpp_add_d<0x121>(v);
+}
+
+// Sums over the tokens first, first + step, ... of every thread of WAVES wavefronts, in thread 0.. of LDS: red[2 E], cnt[E].
+template <int E, int WAVES>
+struct TokenSums {
+    double red[2 * E][WAVES];
+    int32_t cnt[E][WAVES];
+};
+template <int E, int WAVES>
+__device__ inline void sum_tokens(const BalanceArgs &a, long first, long step, TokenSums<E, WAVES> &s) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const bool in = t < a.T && (!a.valid || a.valid[t] != 0);
-    TokenRouting r;
-    r.first = -1;
-    if (in) r = route_token(a.logits + (size_t)t * a.E, a.E, 1.0f / a.noise_std);
+    double sp[E], sq[E];
+    int cnt[E];
 #pragma unroll
-    for (int e = 0; e < kMaxE; ++e) {
-        if (e >= a.E) break;
-        const double sp = wave_sum_d(in ? (double)r.p[e] : 0.0);
-        const double sq = wave_sum_d(in ? 0.5 * (double)erfcf(r.z[e] * -0.70710678118654752f) : 0.0);
-        const int c = __popcll(__ballot(r.first == e));
-        if (lane == 0) red[wave][e] = sp, red[wave][kMaxE + e] = sq, cnt[wave][e] = c;
+    for (int e = 0; e < E; ++e) sp[e] = sq[e] = 0.0, cnt[e] = 0;
+    for (long t = first; t < a.T; t += step) {
+        if (a.valid && a.valid[t] == 0) continue;
+        const TokenRouting<E> r = route_token<E>(a.logits + (size_t)t * E, 1.0f / a.noise_std);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            sp[e] += (double)r.p[e];
+            sq[e] += (double)(0.5f * erfcf(r.z[e] * -0.70710678118654752f));
+            cnt[e] += r.first == e ? 1 : 0;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const double p = wave_sum_d(sp[e]), q = wave_sum_d(sq[e]);
+        int c = cnt[e];
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) c += __shfl_xor(c, off, 64);
+        if (lane == 0) s.red[e][wave] = p, s.red[E + e][wave] = q, s.cnt[e][wave] = c;
     }
     __syncthreads();
-    const int i = threadIdx.x, e = i % kMaxE;
-    if (i < 2 * kMaxE && e < a.E) {
-        double s = 0.0;
-        for (int w = 0; w < kTok / 64; ++w) s += red[w][i];
-        a.partial[(size_t)blockIdx.x * 2 * kMaxE + i] = s;
-        if (i < kMaxE) {
-            int c = 0;
-            for (int w = 0; w < kTok / 64; ++w) c += cnt[w][i];
-            a.partial_counts[(size_t)blockIdx.x * kMaxE + i] = c;
+}
+
+// The losses and, in coeff, the gradients of the sums of p and of q, from the sums u of alpha p and alpha q (LDS).
+template <int E>
+__device__ inline void losses_of(const BalanceArgs &a, const double (&u)[2 * E], float (&coeff)[2 * E], bool write) {
+    const int i = threadIdx.x, kind = i / E, e = i % E;
+    if (i < 2 * E) {
+        double sum = 0.0, squares = 0.0, var = 0.0;
+#pragma unroll
+        for (int k = 0; k < E; ++k) sum += u[kind * E + k], squares += u[kind * E + k] * u[kind * E + k];
+        const double m = sum / E;
+#pragma unroll
+        for (int k = 0; k < E; ++k) var += (u[kind * E + k] - m) * (u[kind * E + k] - m);
+        const bool none = m == 0.0;
+        coeff[i] = none ? 0.0f : (float)(2.0 / (E * m * m) * (u[i] - squares / sum) * (double)a.alpha[e] * (double)a.dlosses[kind]);
+        if (write) {
+            if (e == 0) a.losses[kind] = none ? 0.0f : (float)(var / E / (m * m));
+            if (a.sums) a.sums[i] = (float)u[i];
         }
     }
 }
 
-__global__ __launch_bounds__(64) void balance_losses_kernel(BalanceArgs a, long blocks) {
-    __shared__ double u[2 * kMaxE];
-    const int i = threadIdx.x, e = i % kMaxE, kind = i / kMaxE;
-    if (kind < 2 && e < a.E) {
-        double s = 0.0;
-        for (long b = 0; b < blocks; ++b) s += a.partial[(size_t)b * 2 * kMaxE + i];
-        u[i] = s * (double)a.alpha[e];
-        if (a.sums) a.sums[kind * a.E + e] = (float)u[i];
-    } else if (kind == 2 && e < a.E && a.counts) {
+template <int E>
+__device__ inline void grad_tokens(const BalanceArgs &a, long first, long step, const float (&coeff)[2 * E]) {
+    const float peak = 0.39894228040143268f / a.noise_std;
+    float c[E], f0[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) c[e] = coeff[e], f0[e] = coeff[E + e] * peak;
+    for (long t = first; t < a.T; t += step) {
+        float *dl = a.dlogits + (size_t)t * E;
+        if (a.valid && a.valid[t] == 0) {
+            if (!a.accumulate) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) dl[e] = 0.0f;
+            }
+            continue;
+        }
+        const TokenRouting<E> r = route_token<E>(a.logits + (size_t)t * E, 1.0f / a.noise_std);
+        float up[E], to_first = 0.0f, to_second = 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float f = f0[e] * expf(-0.5f * r.z[e] * r.z[e]);
+            up[e] = c[e] + f;
+            to_second -= e == r.first ? f : 0.0f;
+            to_first -= e == r.first ? 0.0f : f;
+        }
+        float mean = 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            up[e] += e == r.first ? to_first : e == r.second ? to_second : 0.0f;
+            mean = __builtin_fmaf(r.p[e], up[e], mean);
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float d = r.p[e] * (up[e] - mean);
+            dl[e] = a.accumulate ? dl[e] + d : d;
+        }
+    }
+}
+
+constexpr int kSumThreads = 512, kSumWaves = kSumThreads / 64, kMaxSumParts = 256, kMaxGradBlocks = 512;
+constexpr int kOneThreads = 1024;
+constexpr long kOneLogits = 2048;        // up to this many, all of it in one workgroup
+
+template <int E>
+__global__ __launch_bounds__(kSumThreads) void balance_sums_kernel(BalanceArgs a) {
+    __shared__ TokenSums<E, kSumWaves> s;
+    sum_tokens<E, kSumWaves>(a, (long)blockIdx.x * kSumThreads + threadIdx.x, (long)a.parts * kSumThreads, s);
+    const int i = threadIdx.x;
+    if (i < 2 * E) {
+        double v = 0.0;
+        for (int w = 0; w < kSumWaves; ++w) v += s.red[i][w];
+        a.partial[(size_t)i * a.parts + blockIdx.x] = v;
+    } else if (i < 3 * E) {
         int c = 0;
-        for (long b = 0; b < blocks; ++b) c += a.partial_counts[(size_t)b * kMaxE + e];
-        a.counts[e] = c;
+        for (int w = 0; w < kSumWaves; ++w) c += s.cnt[i - 2 * E][w];
+        a.partial_counts[(size_t)(i - 2 * E) * a.parts + blockIdx.x] = c;
+    }
+}
+
+// Every workgroup adds up the parts (a few KB out of the caches) rather than wait for a launch that does.
+template <int E>
+__global__ __launch_bounds__(kSumThreads) void balance_grad_kernel(BalanceArgs a) {
+    __shared__ double u[2 * E];
+    __shared__ float coeff[2 * E];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int v = wave; v < 3 * E; v += kSumWaves) {
+        if (v < 2 * E) {
+            double sum = 0.0;
+            for (int k = lane; k < a.parts; k += 64) sum += a.partial[(size_t)v * a.parts + k];
+            sum = wave_sum_d(sum);
+            if (lane == 0) u[v] = sum * (double)a.alpha[v % E];
+        } else if (blockIdx.x == 0 && a.counts) {
+            int c = 0;
+            for (int k = lane; k < a.parts; k += 64) c += a.partial_counts[(size_t)(v - 2 * E) * a.parts + k];
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) c += __shfl_xor(c, off, 64);
+            if (lane == 0) a.counts[v - 2 * E] = c;
+        }
     }
     __syncthreads();
-    if (kind < 2 && e < a.E) {
-        double sum = 0.0, squares = 0.0, var = 0.0;
-        for (int k = 0; k < a.E; ++k) sum += u[kind * kMaxE + k], squares += u[kind * kMaxE + k] * u[kind * kMaxE + k];
-        const double m = sum / a.E;
-        for (int k = 0; k < a.E; ++k) var += (u[kind * kMaxE + k] - m) * (u[kind * kMaxE + k] - m);
-        const bool none = m == 0.0;
-        if (e == 0) a.losses[kind] = none ? 0.0f : (float)(var / a.E / (m * m));
-        a.coeff[i] = none ? 0.0f : (float)(2.0 / (a.E * m * m) * (u[i] - squares / sum) * (double)a.alpha[e] * (double)a.dlosses[kind]);
-    }
+    losses_of<E>(a, u, coeff, blockIdx.x == 0);
+    __syncthreads();
+    grad_tokens<E>(a, (long)blockIdx.x * kSumThreads + threadIdx.x, (long)gridDim.x * kSumThreads, coeff);
 }
 
-__global__ __launch_bounds__(kTok) void balance_grad_kernel(BalanceArgs a) {
-    const long t = (long)blockIdx.x * kTok + threadIdx.x;
-    if (t >= a.T) return;
-    float *dl = a.dlogits + (size_t)t * a.E;
-    if (a.valid && a.valid[t] == 0) {
-        if (!a.accumulate)
-            for (int e = 0; e < a.E; ++e) dl[e] = 0.0f;
-        return;
+template <int E>
+__global__ __launch_bounds__(kOneThreads) void balance_one_kernel(BalanceArgs a) {
+    __shared__ TokenSums<E, kOneThreads / 64> s;
+    __shared__ double u[2 * E];
+    __shared__ float coeff[2 * E];
+    sum_tokens<E, kOneThreads / 64>(a, threadIdx.x, kOneThreads, s);
+    const int i = threadIdx.x;
+    if (i < 2 * E) {
+        double v = 0.0;
+        for (int w = 0; w < kOneThreads / 64; ++w) v += s.red[i][w];
+        u[i] = v * (double)a.alpha[i % E];
+    } else if (i < 3 * E && a.counts) {
+        int c = 0;
+        for (int w = 0; w < kOneThreads / 64; ++w) c += s.cnt[i - 2 * E][w];
+        a.counts[i - 2 * E] = c;
     }
-    const TokenRouting r = route_token(a.logits + (size_t)t * a.E, a.E, 1.0f / a.noise_std);
-    const float peak = 0.39894228040143268f / a.noise_std;
-    float up[kMaxE], to_first = 0.0f, to_second = 0.0f;
-#pragma unroll
-    for (int e = 0; e < kMaxE; ++e) {
-        up[e] = 0.0f;
-        if (e >= a.E) continue;
-        const float f = a.coeff[kMaxE + e] * peak * expf(-0.5f * r.z[e] * r.z[e]);
-        up[e] = a.coeff[e] + f;
-        if (e == r.first) to_second -= f; else to_first -= f;
-    }
-    float mean = 0.0f;
-#pragma unroll
-    for (int e = 0; e < kMaxE; ++e) {
-        up[e] += (e == r.first ? to_first : 0.0f) + (e == r.second ? to_second : 0.0f);
-        mean = __builtin_fmaf(r.p[e], up[e], mean);
-    }
-#pragma unroll
-    for (int e = 0; e < kMaxE; ++e) {
-        if (e >= a.E) break;
-        const float d = r.p[e] * (up[e] - mean);
-        dl[e] = a.accumulate ? dl[e] + d : d;
-    }
+    __syncthreads();
+    losses_of<E>(a, u, coeff, true);
+    __syncthreads();
+    grad_tokens<E>(a, threadIdx.x, kOneThreads, coeff);
 }
 
-long balance_blocks(long T) { return (T + kTok - 1) / kTok; }
-size_t balance_workspace(long T) {
-    return (size_t)balance_blocks(T) * (2 * kMaxE * 8 + kMaxE * 4) + 256;
+int balance_parts(long T) {
+    const long parts = (T + kSumThreads - 1) / kSumThreads;
+    return (int)(parts < kMaxSumParts ? parts : kMaxSumParts);
+}
+size_t balance_workspace(long T) { return (size_t)balance_parts(T) * kMaxE * (2 * 8 + 4) + 256; }
+
+template <int E>
+int launch_balance(const BalanceArgs &a, hipStream_t st) {
+    if (a.T * E <= kOneLogits) {
+        balance_one_kernel<E><<<dim3(1), dim3(kOneThreads), 0, st>>>(a);
+        return check_launch("sa_moe_balance_loss_grad(one launch)");
+    }
+    balance_sums_kernel<E><<<dim3((unsigned)a.parts), dim3(kSumThreads), 0, st>>>(a);
+    const int rc = check_launch("sa_moe_balance_loss_grad(sums)");
+    if (rc != SA_OK) return rc;
+    const long blocks = (a.T + kSumThreads - 1) / kSumThreads;
+    balance_grad_kernel<E><<<dim3((unsigned)(blocks < kMaxGradBlocks ? blocks : kMaxGradBlocks)), dim3(kSumThreads), 0, st>>>(a);
+    return check_launch("sa_moe_balance_loss_grad(gradient)");
+}
+
+// f(std::integral_constant<int, E>()) for E experts.
+template <class F>
+int by_experts(int E, F &&f) {
+    switch (E) {
+        case 2: return f(std::integral_constant<int, 2>());
+        case 3: return f(std::integral_constant<int, 3>());
+        case 4: return f(std::integral_constant<int, 4>());
+        case 5: return f(std::integral_constant<int, 5>());
+        case 6: return f(std::integral_constant<int, 6>());
+        case 7: return f(std::integral_constant<int, 7>());
+        default: return f(std::integral_constant<int, kMaxE>());
+    }
 }
 
 struct CombineGradArgs {
@@ -211,15 +326,27 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradArgs a) {
     if (lane != 0) return;
     if (a.dgate) a.dgate[r] = s;
     if (a.dlogits) {
-        const TokenRouting t = route_token(a.logits + r * a.n, a.n, 1.0f);
-        float top = 0.0f;
+        float v[kMaxE], best = a.logits[r * a.n], den = 0.0f, top = 0.0f;
+        int first = 0;
 #pragma unroll
-        for (int e = 0; e < kMaxE; ++e)
-            if (e == t.first) top = t.p[e];
+        for (int e = 0; e < kMaxE; ++e) {
+            v[e] = e < a.n ? a.logits[r * a.n + e] : 0.0f;
+            if (e < a.n && v[e] > best) best = v[e], first = e;
+        }
+#pragma unroll
+        for (int e = 0; e < kMaxE; ++e) {
+            v[e] = e < a.n ? expf(v[e] - best) : 0.0f;
+            den += v[e];
+        }
+#pragma unroll
+        for (int e = 0; e < kMaxE; ++e) {
+            v[e] /= den;
+            if (e == first) top = v[e];
+        }
 #pragma unroll
         for (int e = 0; e < kMaxE; ++e) {
             if (e >= a.n) break;
-            a.dlogits[r * a.n + e] = s * top * ((e == t.first ? 1.0f : 0.0f) - t.p[e]);
+            a.dlogits[r * a.n + e] = s * top * ((e == first ? 1.0f : 0.0f) - v[e]);
         }
     }
 }
@@ -257,24 +384,11 @@ extern "C" int sa_moe_balance_loss_grad(const float *logits, long T, int E, cons
     const size_t need = balance_workspace(T);
     SA_REQUIRE(workspace != nullptr && workspace_bytes >= need, SA_ERR_WORKSPACE,
                "sa_moe_balance_loss_grad: workspace of %zu bytes needed, %zu given", need, workspace_bytes);
-    hipStream_t st = sa::as_stream(stream);
-    const long blocks = balance_blocks(T);
-    BalanceArgs a{logits, T, E, valid_or_null, alpha, noise_std, dlosses, losses, sums_or_null, counts_or_null, dlogits, accumulate};
-    uint8_t *ws = static_cast<uint8_t *>(workspace);
-    a.coeff = reinterpret_cast<float *>(ws);
-    a.partial = reinterpret_cast<double *>(ws + 256);
-    a.partial_counts = reinterpret_cast<int32_t *>(ws + 256 + (size_t)blocks * 2 * kMaxE * 8);
-    int rc;
-    if (T > 0) {
-        balance_sums_kernel<<<dim3((unsigned)blocks), dim3(kTok), 0, st>>>(a);
-        rc = sa::check_launch("sa_moe_balance_loss_grad(sums)");
-        if (rc != SA_OK) return rc;
-    }
-    balance_losses_kernel<<<dim3(1), dim3(64), 0, st>>>(a, blocks);
-    rc = sa::check_launch("sa_moe_balance_loss_grad(losses)");
-    if (rc != SA_OK || T == 0) return rc;
-    balance_grad_kernel<<<dim3((unsigned)blocks), dim3(kTok), 0, st>>>(a);
-    return sa::check_launch("sa_moe_balance_loss_grad(gradient)");
+    BalanceArgs a{logits, T, valid_or_null, alpha, noise_std, dlosses, losses, sums_or_null, counts_or_null, dlogits, accumulate};
+    a.parts = balance_parts(T);
+    a.partial = static_cast<double *>(workspace);
+    a.partial_counts = reinterpret_cast<int32_t *>(a.partial + (size_t)a.parts * 2 * kMaxE);
+    return by_experts(E, [&](auto experts) { return launch_balance<decltype(experts)::value>(a, sa::as_stream(stream)); });
 }
 
 extern "C" int sa_combine_rows_backward(const void *dy, int y_type, const void *src_or_null, int src_type, const sa_rows *rows,
