@@ -5,10 +5,9 @@
 //   u_i = alpha_i sum_t p_i, v_i = alpha_i sum_t q_i, losses SCV(u), SCV(v), SCV(u) = mean((u - m)^2) / m^2, m = mean(u)
 //   dSCV / du_i = 2 (u_i - sum u^2 / sum u) / (n m^2)
 //   with c and f the gradients of the sums of p and q:  a = c + J^T (f phi(d) / std),  J p_i = p_i - p_o(i),  dl = p (a - <p, a>)
-#include "common.h"
-#include "layernorm.h"
 #include <type_traits>
 
+#include "common.h"
 #include "row_types.h"
 
 namespace {
@@ -297,65 +296,90 @@ struct CombineGradArgs {
     float *dgate, *dlogits;
 };
 
-template <class T>
-__device__ inline float load_elem(const T *p) { return (float)*p; }
-template <class T>
-__device__ inline void store_elem(T *p, float v) { *p = (T)v; }
+// Maximum over aligned groups of 16 lanes.
+__device__ inline float max16(float v) {
+#define SA_MAX_STEP(CTRL) \
+    v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true)))
+    SA_MAX_STEP(0x128);
+    SA_MAX_STEP(0x124);
+    SA_MAX_STEP(0x122);
+    SA_MAX_STEP(0x121);
+#undef SA_MAX_STEP
+    return v;
+}
 
-// A wavefront to a row.
-template <class Y, class S>
+// 16 to 64 lanes to a row, which they walk over in blocks of S::COLUMNS columns; an expert of its routing to a lane.
+template <class Y, class X, class S>
 __global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradArgs a) {
+    constexpr int VEC = S::VEC, CH = S::CH;
     const int32_t *rows;
     long n_rows;
     resolve_rows(a.sel, rows, n_rows);
-    const long i = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (i >= n_rows) return;
-    const size_t r = rows ? (size_t)rows[i] : (size_t)i;
-    const float gate = a.gate ? a.gate[r] : 1.0f;
-    const Y *dy = static_cast<const Y *>(a.dy) + r * a.E;
+    const int g = threadIdx.x / S::LANES, l = threadIdx.x % S::LANES;
     const bool dot = a.dgate || a.dlogits;
-    float s = 0.0f;
-    for (int j = lane; j < a.E; j += 64) {
-        const float d = load_elem(dy + j);
-        if (dot) s = __builtin_fmaf(d, load_elem(static_cast<const S *>(a.src) + (size_t)i * a.E + j), s);
-        if (a.dsrc) store_elem(static_cast<S *>(a.dsrc) + (size_t)i * a.E + j, gate * d);
-    }
-    if (!dot) return;
-    s = group_sum<64>(s);
-    if (lane != 0) return;
-    if (a.dgate) a.dgate[r] = s;
-    if (a.dlogits) {
-        float v[kMaxE], best = a.logits[r * a.n], den = 0.0f, top = 0.0f;
-        int first = 0;
+    const long stride = (long)gridDim.x * S::GROUPS;
+    for (long i = (long)blockIdx.x * S::GROUPS + g; i < n_rows; i += stride) {
+        const size_t r = rows ? (size_t)rows[i] : (size_t)i;
+        const float gate = a.gate ? a.gate[r] : 1.0f;
+        const Y *dy = static_cast<const Y *>(a.dy) + r * a.E;
+        const X *src = static_cast<const X *>(a.src) + (size_t)i * a.E;
+        X *dsrc = static_cast<X *>(a.dsrc) + (size_t)i * a.E;
+        float s = 0.0f;
+        for (int j0 = 0; j0 < a.E; j0 += S::COLUMNS) {
+            Piece<Y, VEC> d[CH];
+            Piece<X, VEC> v[CH];
+            int at[CH], skip[CH];
 #pragma unroll
-        for (int e = 0; e < kMaxE; ++e) {
-            v[e] = e < a.n ? a.logits[r * a.n + e] : 0.0f;
-            if (e < a.n && v[e] > best) best = v[e], first = e;
+            for (int c = 0; c < CH; ++c) {
+                const int j = j0 + (c * S::LANES + l) * VEC;
+                at[c] = j + VEC <= a.E ? j : a.E - VEC;
+                skip[c] = j - at[c];
+                d[c].load(dy + at[c]);
+                if (dot) v[c].load(src + at[c]);
+            }
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                float out[VEC];
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) {
+                    const float dk = k >= skip[c] ? d[c][k] : 0.0f;
+                    if (dot) s = k >= skip[c] ? __builtin_fmaf(dk, v[c][k], s) : s;
+                    out[k] = gate * dk;
+                }
+                if (a.dsrc && skip[c] < VEC) store_piece<X, VEC>(dsrc + at[c], out, skip[c]);
+            }
         }
-#pragma unroll
-        for (int e = 0; e < kMaxE; ++e) {
-            v[e] = e < a.n ? expf(v[e] - best) : 0.0f;
-            den += v[e];
-        }
-#pragma unroll
-        for (int e = 0; e < kMaxE; ++e) {
-            v[e] /= den;
-            if (e == first) top = v[e];
-        }
-#pragma unroll
-        for (int e = 0; e < kMaxE; ++e) {
-            if (e >= a.n) break;
-            a.dlogits[r * a.n + e] = s * top * ((e == first ? 1.0f : 0.0f) - v[e]);
+        if (!dot) continue;
+        s = group_sum<S::LANES>(s);
+        if (a.dgate && l == 0) a.dgate[r] = s;
+        if (a.dlogits) {
+            // p_first = 1 / den, the largest exponent being 0
+            const float v = l < a.n ? a.logits[r * a.n + l] : -__builtin_inff();
+            const float top = max16(v);
+            const uint64_t best = __ballot(l < a.n && v == top) >> (threadIdx.x & 63 & ~(S::LANES - 1));
+            const float e = l < a.n ? expf(v - top) : 0.0f;
+            const float inv = 1.0f / group_sum<16>(e);
+            if (l < a.n) a.dlogits[r * a.n + l] = s * inv * ((l == __ffsll((unsigned long long)(best & 0xFFFF)) - 1 ? 1.0f : 0.0f) - e * inv);
         }
     }
 }
 
-template <class Y, class S>
+template <class Y, class X>
 struct RunCombineGrad {
     static int run(const CombineGradArgs &a, hipStream_t st) {
-        combine_grad_kernel<Y, S><<<dim3((unsigned)((a.sel.max_rows + 3) / 4)), dim3(256), 0, st>>>(a);
-        return check_launch("sa_combine_rows_backward");
+        constexpr int VEC = row_vec<Y, X>();
+        auto rows = [&](auto shape) {
+            using S = decltype(shape);
+            // 8 workgroups to a CU; the rows there are may be fewer than max_rows
+            const long blocks = (a.sel.max_rows + S::GROUPS - 1) / S::GROUPS;
+            combine_grad_kernel<Y, X, S><<<dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, st>>>(a);
+            return check_launch("sa_combine_rows_backward");
+        };
+        if (a.E < VEC) return rows(RowShape<1, 1, 16, 0>());
+        if (a.E <= 16 * VEC) return rows(RowShape<VEC, 1, 16, 0>());
+        if (a.E <= 32 * VEC) return rows(RowShape<VEC, 1, 32, 0>());
+        if (a.E <= 64 * VEC) return rows(RowShape<VEC, 1, 64, 0>());
+        return rows(RowShape<VEC, 8 / VEC, 64, 0>());
     }
 };
 
