@@ -18,12 +18,19 @@ struct GradRow {
         for (int c = 0; c < S::CH; ++c) {
             dy[c].load(static_cast<const Y *>(a.dy) + row + p.at[c]);
             x[c].load(static_cast<const X *>(a.x) + row + p.at[c]);
-            if (a.dres) res[c].load(static_cast<const X *>(a.dres) + row + p.at[c]);
+        }
+        if (a.dres) {
+#pragma unroll
+            for (int c = 0; c < S::CH; ++c) res[c].load(static_cast<const X *>(a.dres) + row + p.at[c]);
         }
         if (a.mean) mean = a.mean[t], rstd = a.rstd[t];
         if constexpr (ROUTE > kStreamed) {
 #pragma unroll
-            for (int e = 0; e < ROUTE; ++e) dl[e] = e < a.n ? a.dlogits[(size_t)t * a.n + e] : 0.0f;
+            for (int e = 0; e < ROUTE; ++e) {
+                const bool in = ROUTE == 2 || e < a.n;
+                const float v = a.dlogits[(size_t)t * a.n + (in ? e : 0)];
+                dl[e] = in ? v : 0.0f;
+            }
         }
     }
 };
@@ -49,17 +56,12 @@ __global__ __launch_bounds__(S::THREADS) void norm_grad_kernel(NormGradArgs a) {
     const RowPlace<S> p(l, a.E);
     const float per = 1.0f / (float)a.E;
     RowSums<S, 2> sums{red};
-    // gamma is 0 in the elements that are not this lane's: they drop out of the row's sums by it
     float gm[CH][VEC], w[PR][PC][VEC];
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const int j = p.at[c] + i;
-            gm[c][i] = p.mine(c, i) ? a.gamma[j] : 0.0f;
-#pragma unroll
-            for (int e = 0; e < HELD; ++e) w[e][c][i] = e < a.n ? a.wg[(size_t)j * a.n + e] : 0.0f;
-        }
+    for (int c = 0; c < CH; ++c) {
+        load_columns<VEC>(gm[c], a.gamma + p.at[c]);
+        if constexpr (HELD > 0) load_router<VEC, HELD, PC>(w, c, a.wg + (size_t)p.at[c] * a.n, a.n);
+    }
     float acc[Q][CH][VEC], dl_sum[PR];
 #pragma unroll
     for (int q = 0; q < Q; ++q)
@@ -72,33 +74,26 @@ __global__ __launch_bounds__(S::THREADS) void norm_grad_kernel(NormGradArgs a) {
 
     const long stride = (long)gridDim.x * S::GROUPS;
     auto clamped = [&](long t) { return t < a.T ? t : a.T - 1; };
-    GradRow<X, Y, S, ROUTE> nxt;
-    long t0 = (long)blockIdx.x * S::GROUPS;
-    if constexpr (AHEAD) nxt.load(a, p, clamped(t0 + g));
-    for (; t0 < a.T; t0 += stride) {
-        const long t = t0 + g;
-        if constexpr (!AHEAD) nxt.load(a, p, clamped(t));
-        const GradRow<X, Y, S, ROUTE> r = nxt;
-        if (AHEAD && t0 + stride < a.T) nxt.load(a, p, clamped(t + stride));
+    auto work = [&](const GradRow<X, Y, S, ROUTE> &r, long t, bool row_ok) {
         float mean = r.mean, rstd = r.rstd, s[2];
         if (!a.mean) {
             s[0] = 0.0f;
 #pragma unroll
             for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) s[0] += p.mine(c, i) ? r.x[c][i] : 0.0f;
+                for (int i = 0; i < VEC; ++i) s[0] += p.own(c, i, r.x[c][i]);
             sums(s, 1);
-            mean = s[0] / (float)a.E;
+            mean = s[0] * per;
             s[0] = 0.0f;
 #pragma unroll
             for (int c = 0; c < CH; ++c)
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    const float d = r.x[c][i] - mean;
-                    s[0] = p.mine(c, i) ? __builtin_fmaf(d, d, s[0]) : s[0];
+                    const float d = p.own(c, i, r.x[c][i] - mean);
+                    s[0] = __builtin_fmaf(d, d, s[0]);
                 }
             sums(s, 1);
-            rstd = 1.0f / __builtin_sqrtf(s[0] / (float)a.E + a.eps);
+            rstd = 1.0f / __builtin_sqrtf(__builtin_fmaf(s[0], per, a.eps));
         }
         float xh[CH][VEC], h[CH][VEC];
         s[0] = s[1] = 0.0f;
@@ -126,30 +121,44 @@ __global__ __launch_bounds__(S::THREADS) void norm_grad_kernel(NormGradArgs a) {
         for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                const float gv = h[c][i] * gm[c][i];
+                const float gv = p.own(c, i, h[c][i] * gm[c][i]);
                 s[0] += gv;
                 s[1] = __builtin_fmaf(gv, xh[c][i], s[1]);
             }
         sums(s);
-        if (t < a.T) {
-            const float c0 = s[0] * per, c1 = s[1] * per;
+        if (!row_ok) return;
+        const float c0 = s[0] * per, c1 = s[1] * per;
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                float d[VEC];
+        for (int c = 0; c < CH; ++c) {
+            float d[VEC];
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    acc[0][c][i] = __builtin_fmaf(h[c][i], xh[c][i], acc[0][c][i]);
-                    acc[1][c][i] += h[c][i];
+            for (int i = 0; i < VEC; ++i) {
+                acc[0][c][i] = __builtin_fmaf(h[c][i], xh[c][i], acc[0][c][i]);
+                acc[1][c][i] += h[c][i];
 #pragma unroll
-                    for (int e = 0; e < HELD; ++e) acc[2 + e][c][i] = __builtin_fmaf(xh[c][i], r.dl[e], acc[2 + e][c][i]);
-                    d[i] = rstd * (h[c][i] * gm[c][i] - c0 - xh[c][i] * c1);
-                    if (a.dres) d[i] += r.res[c][i];
-                }
-                if (p.any(c)) store_piece<X, VEC>(static_cast<X *>(a.dx) + (size_t)t * a.E + p.at[c], d, c < S::FULL ? 0 : p.skip[c]);
+                for (int e = 0; e < HELD; ++e) acc[2 + e][c][i] = __builtin_fmaf(xh[c][i], r.dl[e], acc[2 + e][c][i]);
+                d[i] = rstd * (h[c][i] * gm[c][i] - c0 - xh[c][i] * c1);
+                if (a.dres) d[i] += r.res[c][i];
             }
-#pragma unroll
-            for (int e = 0; e < HELD; ++e) dl_sum[e] += r.dl[e];
+            store_piece<X, VEC>(static_cast<X *>(a.dx) + (size_t)t * a.E + p.at[c], d);
         }
+#pragma unroll
+        for (int e = 0; e < HELD; ++e) dl_sum[e] += r.dl[e];
+    };
+    // Every step stores the same number of pieces: a wait for the next row then leaves the last row's stores in flight (loads and stores
+    // are counted by one counter, in order).  Rows that are not there come in a last step of their own.
+    GradRow<X, Y, S, ROUTE> nxt;
+    long t0 = (long)blockIdx.x * S::GROUPS;
+    if constexpr (AHEAD) nxt.load(a, p, clamped(t0 + g));
+    for (; t0 + S::GROUPS <= a.T; t0 += stride) {
+        if constexpr (!AHEAD) nxt.load(a, p, t0 + g);
+        const GradRow<X, Y, S, ROUTE> r = nxt;
+        if constexpr (AHEAD) nxt.load(a, p, clamped(t0 + g + stride));
+        work(r, t0 + g, true);
+    }
+    if (S::GROUPS > 1 && t0 < a.T) {
+        if constexpr (!AHEAD) nxt.load(a, p, clamped(t0 + g));
+        work(nxt, t0 + g, t0 + g < a.T);
     }
     if (!a.partial) return;
     const int columns = padded_columns(a.E), n = ROUTE ? a.n : 0;
@@ -160,9 +169,9 @@ __global__ __launch_bounds__(S::THREADS) void norm_grad_kernel(NormGradArgs a) {
             for (int c = 0; c < CH; ++c)
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    const float gamma = a.gamma[p.at[c] + i], beta = a.beta[p.at[c] + i];
+                    const float beta = a.beta[p.at[c] + i];
 #pragma unroll
-                    for (int e = 0; e < HELD; ++e) acc[2 + e][c][i] = __builtin_fmaf(gamma, acc[2 + e][c][i], beta * dl_sum[e]);
+                    for (int e = 0; e < HELD; ++e) acc[2 + e][c][i] = __builtin_fmaf(gm[c][i], acc[2 + e][c][i], beta * dl_sum[e]);
                 }
         }
     }
@@ -174,12 +183,12 @@ __global__ __launch_bounds__(S::THREADS) void norm_grad_kernel(NormGradArgs a) {
         if constexpr (S::GROUPS == 1) {
 #pragma unroll
             for (int c = 0; c < CH; ++c)
-                if (p.any(c)) store_piece<float, VEC>(part + (size_t)q * columns + p.at[c], acc[q][c], c < S::FULL ? 0 : p.skip[c]);
+                store_piece<float, VEC>(part + (size_t)q * columns + p.at[c], acc[q][c]);
         } else {
             __syncthreads();
 #pragma unroll
             for (int c = 0; c < CH; ++c)
-                if (p.any(c)) store_piece<float, VEC>(side + g * S::COLUMNS + p.at[c], acc[q][c], c < S::FULL ? 0 : p.skip[c]);
+                store_piece<float, VEC>(side + g * S::COLUMNS + p.at[c], acc[q][c]);
             __syncthreads();
             for (int j = threadIdx.x; j < a.E; j += S::THREADS) {
                 float s = side[j];
@@ -241,7 +250,7 @@ __global__ __launch_bounds__(256) void norm_grad_router_kernel(NormGradArgs a, l
         float v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = __builtin_fmaf(a.gamma[at + i], acc[e][i], a.beta[at + i] * dl_sum[e]);
-        store_piece<float, 4>(out + (size_t)e * columns, v, j - at);
+        store_piece<float, 4>(out + (size_t)e * columns, v);
     }
     if (blockIdx.x == 0 && threadIdx.x < 1) {
 #pragma unroll

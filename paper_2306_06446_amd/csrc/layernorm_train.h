@@ -82,6 +82,32 @@ int by_shape_route8(int E, F &&f) {
     return f(RowShape<VEC, C, 256, 0>());
 }
 
+// A piece of a parameter row, and of the router's weights [E, n]: N experts, zeros behind the n there are.
+template <int VEC>
+__device__ inline void load_columns(float (&out)[VEC], const float *p) {
+    Piece<float, VEC> v;
+    v.load(p);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) out[i] = v[i];
+}
+template <int VEC, int N, int CH>
+__device__ inline void load_router(float (&out)[N][CH][VEC], int c, const float *p, int n) {
+    if constexpr (N == 2) {
+        Piece<float, 2 * VEC> v;
+        v.load(p);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) out[0][c][i] = v[2 * i], out[1][c][i] = v[2 * i + 1];
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float v = p[i * n + (e < n ? e : 0)];
+                out[e][c][i] = e < n ? v : 0.0f;
+            }
+    }
+}
+
 template <class X, class Y>
 int launch_norm_rows(const NormArgs &a, hipStream_t st);
 // Leaves sums over rows in a.partial, in *parts parts.

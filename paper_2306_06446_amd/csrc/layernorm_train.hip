@@ -7,66 +7,78 @@
 
 namespace sa {
 
-template <class X, class Y, class S, int ROUTE>
+// TRAIN: y, mean and rstd are all wanted (else each is asked about).
+template <class X, class Y, class S, int ROUTE, bool TRAIN>
 __global__ __launch_bounds__(S::THREADS) void train_norm_kernel(NormArgs a) {
     constexpr int VEC = S::VEC, CH = S::CH, HELD = ROUTE > kStreamed ? ROUTE : 0, PR = HELD ? HELD : 1, PC = HELD ? CH : 1;
     __shared__ float red[S::LANES > 64 ? PR : 1][2][S::WAVES];
     const int g = threadIdx.x / S::LANES, l = threadIdx.x % S::LANES;
     const RowPlace<S> p(l, a.E);
+    const float per = 1.0f / (float)a.E;
     RowSums<S, 1> sum{red};
-    float gm[CH][VEC], bt[CH][VEC], w[PR][PC][VEC];
+    float gm[CH][VEC], bt[CH][VEC], w[PR][PC][VEC], bias[PR];
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+    for (int c = 0; c < CH; ++c) {
+        load_columns<VEC>(gm[c], a.gamma + p.at[c]);
+        load_columns<VEC>(bt[c], a.beta + p.at[c]);
+        if constexpr (HELD > 0) {
+            load_router<VEC, HELD, PC>(w, c, a.wg + (size_t)p.at[c] * a.n, a.n);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const int j = p.at[c] + i;
-            gm[c][i] = a.gamma ? a.gamma[j] : 0.0f;
-            bt[c][i] = a.gamma ? a.beta[j] : 0.0f;
+            for (int e = 0; e < HELD; ++e)
 #pragma unroll
-            for (int e = 0; e < HELD; ++e) w[e][c][i] = e < a.n && p.mine(c, i) ? a.wg[(size_t)j * a.n + e] : 0.0f;
+                for (int i = 0; i < VEC; ++i) w[e][c][i] = p.own(c, i, w[e][c][i]);
         }
+    }
+#pragma unroll
+    for (int e = 0; e < HELD; ++e) bias[e] = a.bg[HELD == 2 || e < a.n ? e : 0];
     const long stride = (long)gridDim.x * S::GROUPS;
     auto load = [&](Piece<X, VEC> (&x)[CH], long t) {
         const X *row = static_cast<const X *>(a.x) + (size_t)(t < a.T ? t : a.T - 1) * a.E;
 #pragma unroll
         for (int c = 0; c < CH; ++c) x[c].load(row + p.at[c]);
     };
-    Piece<X, VEC> nxt[CH], x[CH];
-    long t0 = (long)blockIdx.x * S::GROUPS;
-    load(nxt, t0 + g);
-    for (; t0 < a.T; t0 += stride) {
-        const long t = t0 + g;
+    // What there is one of to a row is kept, a step to a lane, and leaves for LANES rows at a time: every step then stores the same
+    // number of pieces, and a wait for the next row leaves the last row's stores in flight (one counter, in order).
+    float kept_mean = 0.0f, kept_rstd = 0.0f, kept[PR];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) x[c] = nxt[c];
-        if (t0 + stride < a.T) load(nxt, t + stride);
+    for (int e = 0; e < PR; ++e) kept[e] = 0.0f;
+    const long t_first = (long)blockIdx.x * S::GROUPS + g;
+    auto flush = [&](long steps) {       // the last 1 to LANES of `steps` steps
+        const long k = (steps - 1) / S::LANES * S::LANES + l, t = t_first + k * stride;
+        if (k >= steps || t >= a.T) return;
+        if (TRAIN || a.mean) a.mean[t] = kept_mean;
+        if (TRAIN || a.rstd) a.rstd[t] = kept_rstd;
+#pragma unroll
+        for (int e = 0; e < HELD; ++e)
+            if (HELD == 2 || e < a.n) a.logits[(size_t)t * a.n + e] = kept[e];
+    };
+    auto work = [&](const Piece<X, VEC> (&x)[CH], long t, bool row_ok, long step) {
         float s[1] = {0.0f};
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) s[0] += p.mine(c, i) ? x[c][i] : 0.0f;
+            for (int i = 0; i < VEC; ++i) s[0] += p.own(c, i, x[c][i]);
         sum(s);
-        const float mean = s[0] / (float)a.E;
+        const float mean = s[0] * per;
         s[0] = 0.0f;
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                const float d = x[c][i] - mean;
-                s[0] = p.mine(c, i) ? __builtin_fmaf(d, d, s[0]) : s[0];
+                const float d = p.own(c, i, x[c][i] - mean);
+                s[0] = __builtin_fmaf(d, d, s[0]);
             }
         sum(s);
-        const float rstd = 1.0f / __builtin_sqrtf(s[0] / (float)a.E + a.eps);
+        const float rstd = 1.0f / __builtin_sqrtf(__builtin_fmaf(s[0], per, a.eps));
+        const bool keep = (int)(step & (S::LANES - 1)) == l;
+        kept_mean = keep ? mean : kept_mean;
+        kept_rstd = keep ? rstd : kept_rstd;
         float y[CH][VEC];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
 #pragma unroll
             for (int i = 0; i < VEC; ++i) y[c][i] = __builtin_fmaf((x[c][i] - mean) * rstd, gm[c][i], bt[c][i]);
-            if (a.y && t < a.T && p.any(c))
-                store_piece<Y, VEC>(static_cast<Y *>(a.y) + (size_t)t * a.E + p.at[c], y[c], c < S::FULL ? 0 : p.skip[c]);
-        }
-        if (l == 0 && t < a.T) {
-            if (a.mean) a.mean[t] = mean;
-            if (a.rstd) a.rstd[t] = rstd;
+            if (row_ok && (TRAIN || a.y)) store_piece<Y, VEC>(static_cast<Y *>(a.y) + (size_t)t * a.E + p.at[c], y[c]);
         }
         if constexpr (HELD > 0) {
             float part[HELD];
@@ -79,13 +91,10 @@ __global__ __launch_bounds__(S::THREADS) void train_norm_kernel(NormArgs a) {
                     for (int i = 0; i < VEC; ++i) part[e] = __builtin_fmaf(y[c][i], w[e][c][i], part[e]);
             }
             RowSums<S, HELD> all{red, sum.turn};
-            all(part, a.n);
+            all(part, HELD == 2 ? 2 : a.n);
             sum.turn = all.turn;
-            if (l == 0 && t < a.T) {
 #pragma unroll
-                for (int e = 0; e < HELD; ++e)
-                    if (e < a.n) a.logits[(size_t)t * a.n + e] = part[e] + a.bg[e];
-            }
+            for (int e = 0; e < HELD; ++e) kept[e] = keep ? part[e] + bias[e] : kept[e];
         }
         if constexpr (ROUTE == kStreamed) {
 #pragma unroll 1
@@ -95,11 +104,27 @@ __global__ __launch_bounds__(S::THREADS) void train_norm_kernel(NormArgs a) {
                 for (int c = 0; c < CH; ++c)
 #pragma unroll
                     for (int i = 0; i < VEC; ++i)
-                        s[0] = p.mine(c, i) ? __builtin_fmaf(y[c][i], a.wg[(size_t)(p.at[c] + i) * a.n + e], s[0]) : s[0];
+                        s[0] = __builtin_fmaf(p.own(c, i, y[c][i]), a.wg[(size_t)(p.at[c] + i) * a.n + e], s[0]);
                 sum(s);
-                if (l == 0 && t < a.T) a.logits[(size_t)t * a.n + e] = s[0] + a.bg[e];
+                if (l == 0 && row_ok) a.logits[(size_t)t * a.n + e] = s[0] + a.bg[e];
             }
         }
+    };
+    Piece<X, VEC> nxt[CH], x[CH];
+    long t0 = (long)blockIdx.x * S::GROUPS, step = 0;
+    load(nxt, t0 + g);
+    for (; t0 + S::GROUPS <= a.T; t0 += stride) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) x[c] = nxt[c];
+        load(nxt, t0 + g + stride);
+        work(x, t0 + g, true, step++);
+        if ((step & (S::LANES - 1)) == 0) flush(step);
+    }
+    if (S::GROUPS > 1 && t0 < a.T) {
+        work(nxt, t0 + g, t0 + g < a.T, step++);
+        flush(step);
+    } else if ((step & (S::LANES - 1)) != 0) {
+        flush(step);
     }
 }
 
@@ -112,7 +137,10 @@ int launch_norm_rows(const NormArgs &a, hipStream_t st) {
         const long cap = 1024 * 256 / S::THREADS;
         const long steps = (a.T + S::GROUPS * cap - 1) / (S::GROUPS * cap);
         const long blocks = (a.T + S::GROUPS * steps - 1) / (S::GROUPS * steps);
-        train_norm_kernel<X, Y, S, decltype(route)::value><<<dim3((unsigned)blocks), dim3(S::THREADS), 0, st>>>(a);
+        if (a.y && a.mean && a.rstd)
+            train_norm_kernel<X, Y, S, decltype(route)::value, true><<<dim3((unsigned)blocks), dim3(S::THREADS), 0, st>>>(a);
+        else
+            train_norm_kernel<X, Y, S, decltype(route)::value, false><<<dim3((unsigned)blocks), dim3(S::THREADS), 0, st>>>(a);
         return check_launch("sa_layernorm");
     };
     auto with = [&](auto route) { return [&rows, route](auto shape) { return rows(shape, route); }; };
@@ -128,37 +156,45 @@ namespace {
 
 using namespace sa;
 
-// The parts' sums, in fp64 and in ascending order: 16 threads to four columns.
+// The parts' sums in fp64, in a fixed order: 64 threads to four columns, whose loads (8 to a thread at most) are all in flight at once.
+constexpr int kSumColumns = 16;              // of a workgroup
 __global__ __launch_bounds__(256) void norm_grad_sum_kernel(NormGradArgs a, int parts) {
-    constexpr int kSlices = 16;
-    __shared__ double red[kSlices][64];
+    constexpr int kSlices = 256 / (kSumColumns / 4);
+    static_assert(kSlices * 8 >= kMaxGradParts, "a thread adds up 8 parts");
+    __shared__ double red[4][kSumColumns];
     const int n = a.dlogits ? a.n : 0, columns = padded_columns(a.E), all = (2 + n) * columns;
-    const int slice = threadIdx.x >> 4, quad = threadIdx.x & 15, at = (int)blockIdx.x * 64 + quad * 4;
-    const bool last = blockIdx.x == gridDim.x - 1;           // has room for the router's bias behind the columns
-    double s[4] = {0.0, 0.0, 0.0, 0.0};
-    const float *from = nullptr;
-    size_t step = 0;
-    if (at < all) from = a.partial + at, step = (size_t)all;
-    else if (last && quad >= 14 && a.dbg) from = a.partial_dbg + (quad - 14) * 4, step = kMaxExperts;
-    if (from) {
-#pragma unroll 8
-        for (int k = slice; k < parts; k += kSlices) {
-            const float4 v = *reinterpret_cast<const float4 *>(from + k * step);
-            s[0] += v.x, s[1] += v.y, s[2] += v.z, s[3] += v.w;
-        }
-    }
+    const int slice = threadIdx.x / 4, quad = threadIdx.x & 3, at = (int)blockIdx.x * kSumColumns + quad * 4;
+    const bool last = blockIdx.x == gridDim.x - 1;           // the router's bias is behind the columns, in the last 8 places
+    const float *from = a.partial;
+    size_t step = (size_t)all;
+    bool any = at < all;
+    if (any) from += at;
+    else if (last && quad >= 2 && a.dbg) any = true, from = a.partial_dbg + (quad - 2) * 4, step = kMaxExperts;
+    float4 v[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) red[slice][quad * 4 + i] = s[i];
+    for (int k = 0; k < 8; ++k) {
+        const int part = slice + k * kSlices;
+        v[k] = any && part < parts ? *reinterpret_cast<const float4 *>(from + part * step) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s[0] += v[k].x, s[1] += v[k].y, s[2] += v[k].z, s[3] += v[k].w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int off = 4; off < 64; off *= 2) s[i] += __shfl_xor(s[i], off, 64);
+        if ((threadIdx.x & 63) < 4) red[threadIdx.x >> 6][quad * 4 + i] = s[i];
+    }
     __syncthreads();
-    if (threadIdx.x >= 64) return;
-    double sum = 0.0;
-    for (int k = 0; k < kSlices; ++k) sum += red[k][threadIdx.x];
-    const int i = (int)blockIdx.x * 64 + threadIdx.x, q = i / columns, j = i % columns;
+    if (threadIdx.x >= kSumColumns) return;
+    const double sum = (red[0][threadIdx.x] + red[1][threadIdx.x]) + (red[2][threadIdx.x] + red[3][threadIdx.x]);
+    const int i = (int)blockIdx.x * kSumColumns + threadIdx.x, q = i / columns, j = i % columns;
+    const int bias = (int)threadIdx.x - (kSumColumns - kMaxExperts);
     float *out = nullptr;
     if (i < all) {
         if (j < a.E) out = q == 0 ? a.dgamma + j : q == 1 ? a.dbeta + j : a.dwg ? a.dwg + (size_t)j * n + (q - 2) : nullptr;
-    } else if (last && a.dbg && threadIdx.x >= 56 && (int)threadIdx.x - 56 < n) {
-        out = a.dbg + (threadIdx.x - 56);
+    } else if (last && a.dbg && bias >= 0 && bias < n) {
+        out = a.dbg + bias;
     }
     if (out) *out = (a.accumulate ? *out : 0.0f) + (float)sum;
 }
@@ -210,7 +246,7 @@ struct RunNormGrad {
                 a.weights = rows, a.by_expert = padded_columns(a.E), a.by_column = 1;
                 if (!a.mean && a.dwg) {
                     NormArgs f{};
-                    f.x = a.x, f.T = a.T, f.E = a.E, f.eps = a.eps;
+                    f.x = a.x, f.T = a.T, f.E = a.E, f.eps = a.eps, f.gamma = a.gamma, f.beta = a.gamma;
                     f.mean = reinterpret_cast<float *>(ws + L.mean), f.rstd = reinterpret_cast<float *>(ws + L.rstd);
                     rc = launch_norm_rows<X, Y>(f, st);
                     if (rc != SA_OK) return rc;
@@ -221,7 +257,7 @@ struct RunNormGrad {
         int parts = 0;
         const int rc = launch_norm_grad_rows<X, Y>(a, &parts, st);
         if (rc != SA_OK || !a.dgamma) return rc;
-        const int blocks = ((2 + n) * padded_columns(a.E) + kMaxExperts + 63) / 64;
+        const int blocks = ((2 + n) * padded_columns(a.E) + kMaxExperts + kSumColumns - 1) / kSumColumns;
         norm_grad_sum_kernel<<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a, parts);
         return check_launch("sa_layernorm_backward(sums)");
     }

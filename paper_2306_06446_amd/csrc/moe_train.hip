@@ -342,11 +342,11 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradArgs a) {
                 float out[VEC];
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) {
-                    const float dk = k >= skip[c] ? d[c][k] : 0.0f;
-                    if (dot) s = k >= skip[c] ? __builtin_fmaf(dk, v[c][k], s) : s;
-                    out[k] = gate * dk;
+                    if (dot) s = k >= skip[c] ? __builtin_fmaf(d[c][k], v[c][k], s) : s;
+                    out[k] = gate * d[c][k];
                 }
-                if (a.dsrc && skip[c] < VEC) store_piece<X, VEC>(dsrc + at[c], out, skip[c]);
+                // elements that two lanes hold are written by both, the same bits
+                if (a.dsrc) store_piece<X, VEC>(dsrc + at[c], out);
             }
         }
         if (!dot) continue;

@@ -33,22 +33,15 @@ __device__ inline T rounded(float f) {
     return (T)f;
 }
 
-// To memory; only elements first.. are this lane's.
 template <class T, int V>
-__device__ inline void store_piece(T *p, const float (&f)[V], int first) {
+__device__ inline void store_piece(T *p, const float (&f)[V]) {
     if constexpr (V == 1) {
-        if (first == 0) *p = rounded<T>(f[0]);
+        *p = rounded<T>(f[0]);
     } else {
-        if (first == 0) {
-            typename Piece<T, V>::vec v;
+        typename Piece<T, V>::vec v;
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = rounded<T>(f[i]);
-            *reinterpret_cast<typename Piece<T, V>::vec *>(p) = v;
-        } else {
-#pragma unroll
-            for (int i = 1; i < V; ++i)
-                if (i >= first) p[i] = rounded<T>(f[i]);
-        }
+        for (int i = 0; i < V; ++i) v[i] = rounded<T>(f[i]);
+        *reinterpret_cast<typename Piece<T, V>::vec *>(p) = v;
     }
 }
 
@@ -58,8 +51,8 @@ constexpr int row_vec() { return sizeof(X) == 2 && sizeof(Y) == 2 ? 8 : 4; }
 
 // A row of E elements on LANES lanes, CH pieces of VEC elements each; lane l's piece c begins at VEC (c LANES + l).  A piece that
 // would reach past the row's end (the last one of a row that VEC does not divide, and those behind it) begins VEC before the end
-// instead, so that no load needs a choice; its first elements (`skip` of them, VEC or more where all) are another lane's.  The first FULL
-// pieces of a lane are whole in every row that comes here.
+// instead: no load or store needs a choice, elements that two lanes hold are computed and written by both, the same bits.  Only sums
+// over the row ask whether an element is a lane's own.  The first FULL pieces of a lane are whole in every row that comes here.
 template <int VEC_, int CH_, int LANES_, int FULL_>
 struct RowShape {
     static constexpr int VEC = VEC_, CH = CH_, LANES = LANES_, FULL = FULL_;
@@ -80,8 +73,7 @@ struct RowPlace {
             skip[c] = j - at[c];
         }
     }
-    __device__ inline bool mine(int c, int i) const { return c < S::FULL || i >= skip[c]; }
-    __device__ inline bool any(int c) const { return c < S::FULL || skip[c] < S::VEC; }
+    __device__ inline float own(int c, int i, float v) const { return c < S::FULL || i >= skip[c] ? v : 0.0f; }
 };
 
 // Sums of a row over its lanes, N at a time, in all of them.  Rows of several wavefronts exchange theirs in LDS; two buffers in turn, so that
