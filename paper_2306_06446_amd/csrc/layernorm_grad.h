@@ -44,18 +44,20 @@ struct GradPlan {
     static constexpr bool AHEAD = ELEMS * (2 + HELD + 1 + HELD + 2) + 2 * ROW + 48 < 256;
 };
 
+constexpr int kGradWaves = 4;                // of a workgroup of rows of up to as many wavefronts
 template <class X, class Y, class S, int ROUTE>
-__global__ __launch_bounds__(S::THREADS) void norm_grad_kernel(NormGradArgs a) {
+__global__ __launch_bounds__(S::WIDE ? 512 : 64 * kGradWaves) void norm_grad_kernel(NormGradArgs a) {
     using Plan = GradPlan<X, Y, S, ROUTE>;
     constexpr int VEC = S::VEC, CH = S::CH, HELD = Plan::HELD, Q = 2 + HELD;
     constexpr bool AHEAD = Plan::AHEAD;
     constexpr int PC = HELD ? CH : 1, PR = HELD ? HELD : 1;
-    __shared__ float red[S::LANES > 64 ? 2 : 1][2][S::WAVES];
-    __shared__ float side[S::GROUPS > 1 ? S::THREADS * CH * VEC : 1], side_dl[S::GROUPS][PR];
-    const int g = threadIdx.x / S::LANES, l = threadIdx.x % S::LANES;
-    const RowPlace<S> p(l, a.E);
+    __shared__ float red[S::WIDE ? 2 : 1][2][8];
+    __shared__ float side[64 * kGradWaves * CH * VEC], side_dl[64 * kGradWaves / S::PERIOD][PR];      // of several groups
+    const RowPlace<S> p(a.E);
+    constexpr int GROUPS = 64 * kGradWaves / S::LANES;
+    const int g = p.g, groups = S::WIDE ? p.groups : GROUPS;
     const float per = 1.0f / (float)a.E;
-    RowSums<S, 2> sums{red};
+    RowSums<S, 2> sums(red, p);
     float gm[CH][VEC], w[PR][PC][VEC];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -72,7 +74,7 @@ __global__ __launch_bounds__(S::THREADS) void norm_grad_kernel(NormGradArgs a) {
 #pragma unroll
     for (int e = 0; e < PR; ++e) dl_sum[e] = 0.0f;
 
-    const long stride = (long)gridDim.x * S::GROUPS;
+    const long stride = (long)gridDim.x * groups;
     auto clamped = [&](long t) { return t < a.T ? t : a.T - 1; };
     auto work = [&](const GradRow<X, Y, S, ROUTE> &r, long t, bool row_ok) {
         float mean = r.mean, rstd = r.rstd, s[2];
@@ -148,15 +150,15 @@ __global__ __launch_bounds__(S::THREADS) void norm_grad_kernel(NormGradArgs a) {
     // Every step stores the same number of pieces: a wait for the next row then leaves the last row's stores in flight (loads and stores
     // are counted by one counter, in order).  Rows that are not there come in a last step of their own.
     GradRow<X, Y, S, ROUTE> nxt;
-    long t0 = (long)blockIdx.x * S::GROUPS;
+    long t0 = (long)blockIdx.x * groups;
     if constexpr (AHEAD) nxt.load(a, p, clamped(t0 + g));
-    for (; t0 + S::GROUPS <= a.T; t0 += stride) {
+    for (; t0 + groups <= a.T; t0 += stride) {
         if constexpr (!AHEAD) nxt.load(a, p, t0 + g);
         const GradRow<X, Y, S, ROUTE> r = nxt;
         if constexpr (AHEAD) nxt.load(a, p, clamped(t0 + g + stride));
         work(r, t0 + g, true);
     }
-    if (S::GROUPS > 1 && t0 < a.T) {
+    if (t0 < a.T) {
         if constexpr (!AHEAD) nxt.load(a, p, clamped(t0 + g));
         work(nxt, t0 + g, t0 + g < a.T);
     }
@@ -180,34 +182,32 @@ __global__ __launch_bounds__(S::THREADS) void norm_grad_kernel(NormGradArgs a) {
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
         if (q >= 2 + n) continue;
-        if constexpr (S::GROUPS == 1) {
+        if (groups == 1) {
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
-                store_piece<float, VEC>(part + (size_t)q * columns + p.at[c], acc[q][c]);
+            for (int c = 0; c < CH; ++c) store_piece<float, VEC>(part + (size_t)q * columns + p.at[c], acc[q][c]);
         } else {
+            const int width = p.lanes * CH * VEC;
             __syncthreads();
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
-                store_piece<float, VEC>(side + g * S::COLUMNS + p.at[c], acc[q][c]);
+            for (int c = 0; c < CH; ++c) store_piece<float, VEC>(side + g * width + p.at[c], acc[q][c]);
             __syncthreads();
-            for (int j = threadIdx.x; j < a.E; j += S::THREADS) {
+            for (int j = threadIdx.x; j < a.E; j += (int)blockDim.x) {
                 float s = side[j];
-#pragma unroll
-                for (int k = 1; k < S::GROUPS; ++k) s += side[k * S::COLUMNS + j];
+                for (int k = 1; k < groups; ++k) s += side[k * width + j];
                 part[(size_t)q * columns + j] = s;
             }
         }
     }
     if constexpr (HELD > 0) {
         __syncthreads();
-        if (l == 0) {
+        if (p.l == 0) {
 #pragma unroll
             for (int e = 0; e < HELD; ++e) side_dl[g][e] = dl_sum[e];
         }
         __syncthreads();
         if ((int)threadIdx.x < HELD) {
             float s = 0.0f;
-            for (int k = 0; k < S::GROUPS; ++k) s += side_dl[k][threadIdx.x];
+            for (int k = 0; k < groups; ++k) s += side_dl[k][threadIdx.x];
             a.partial_dbg[(size_t)blockIdx.x * kMaxExperts + threadIdx.x] = s;
         }
     }
@@ -258,20 +258,16 @@ __global__ __launch_bounds__(256) void norm_grad_router_kernel(NormGradArgs a, l
     }
 }
 
-// Parts of the rows: in as few as keep every CU busy (2 workgroups to each, by their registers), the same number of steps in each.
-template <class S>
-int grad_parts(long T) {
-    const long cap = S::THREADS == 256 ? kMaxGradParts : kMaxGradParts / 2;
-    const long steps = (T + S::GROUPS * cap - 1) / (S::GROUPS * cap);
-    return (int)((T + S::GROUPS * steps - 1) / (S::GROUPS * steps));
-}
-
 template <class X, class Y>
 int launch_norm_grad_rows(const NormGradArgs &a, int *parts, hipStream_t st) {
     constexpr int VEC = row_vec<X, Y>();
     auto rows = [&](auto shape, auto route) {
         using S = decltype(shape);
-        *parts = grad_parts<S>(a.T);
+        // 8 wavefronts to a CU, their registers: two workgroups, or one of a wide row's; the same number of steps in each
+        const int threads = S::threads(a.E, kGradWaves);
+        const long per_step = S::groups(a.E, kGradWaves) * (threads <= 64 * kGradWaves ? kMaxGradParts : kMaxGradParts / 2);
+        const long steps = (a.T + per_step - 1) / per_step, rows_of = steps * S::groups(a.E, kGradWaves);
+        *parts = (int)((a.T + rows_of - 1) / rows_of);
         if constexpr (decltype(route)::value == kStreamed) {
             if (a.dwg) {
                 // before dx, which may take the place of x
@@ -281,13 +277,13 @@ int launch_norm_grad_rows(const NormGradArgs &a, int *parts, hipStream_t st) {
                 if (rc != SA_OK) return rc;
             }
         }
-        norm_grad_kernel<X, Y, S, decltype(route)::value><<<dim3((unsigned)*parts), dim3(S::THREADS), 0, st>>>(a);
+        norm_grad_kernel<X, Y, S, decltype(route)::value><<<dim3((unsigned)*parts), dim3((unsigned)threads), 0, st>>>(a);
         return check_launch("sa_layernorm_backward(rows)");
     };
     auto with = [&](auto route) { return [&rows, route](auto shape) { return rows(shape, route); }; };
     if (!a.dlogits) return by_shape<VEC>(a.E, with(std::integral_constant<int, 0>()));
     if (a.n == 2) return by_shape<VEC>(a.E, with(std::integral_constant<int, 2>()));
-    if (a.E > kMaxRoute8Columns) return by_wide_shape<VEC>(a.E, with(std::integral_constant<int, kStreamed>()));
+    if (a.E > kMaxRoute8Columns) return by_wide_shape<VEC>(with(std::integral_constant<int, kStreamed>()));
     return by_shape_route8<VEC>(a.E, with(std::integral_constant<int, kMaxExperts>()));
 }
 

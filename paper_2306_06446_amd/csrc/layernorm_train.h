@@ -49,14 +49,10 @@ __host__ __device__ inline int padded_columns(int E) { return (E + 3) / 4 * 4; }
 // kStreamed: weights from memory row by row, sums elsewhere.
 constexpr int kStreamed = 1;
 
-// The shape of a row of E elements.  Up to 16 elements to a lane (as many registers as leave two workgroups to a CU with their gradients'
-// sums), fewer lanes for narrow rows, so that a wavefront works on several; wider rows take 2, 4, 8 wavefronts.
+// The shape of a row of E elements.  Up to 16 elements to a lane (with a gradient's sums, as many registers as leave two wavefronts to a
+// SIMD), fewer lanes for narrow rows, so that a wavefront works on several; wider rows take several wavefronts.
 template <int VEC, class F>
-int by_wide_shape(int E, F &&f) {
-    constexpr int C = 16 / VEC;
-    if (E <= 4096) return f(RowShape<VEC, C, 256, C / 2>());
-    return f(RowShape<VEC, C, 512, C / 2>());
-}
+int by_wide_shape(F &&f) { return f(RowShape<VEC, 16 / VEC, kWide, 8 / VEC>()); }
 template <int VEC, class F>
 int by_shape(int E, F &&f) {
     if (E < VEC) return f(RowShape<1, 1, 16, 0>());
@@ -68,18 +64,16 @@ int by_shape(int E, F &&f) {
         if (E <= 192 * VEC) return f(RowShape<VEC, 3, 64, 2>());
         if (E <= 256 * VEC) return f(RowShape<VEC, 4, 64, 3>());
     }
-    if (E <= 2048) return f(RowShape<VEC, 16 / VEC, 128, 8 / VEC>());
-    return by_wide_shape<VEC>(E, f);
+    return by_wide_shape<VEC>(f);
 }
 // With a router of up to 8 experts: 8 elements to a lane, whose 64 weights and 64 sums are registers too.  Wider rows would want more
 // of them than there are.
 constexpr int kMaxRoute8Columns = 2048;
 template <int VEC, class F>
 int by_shape_route8(int E, F &&f) {
-    constexpr int C = 8 / VEC;
     if (E < VEC) return f(RowShape<1, 1, 16, 0>());
-    if (E <= 512) return f(RowShape<VEC, C, 64, 0>());
-    return f(RowShape<VEC, C, 256, 0>());
+    if (E <= 512) return f(RowShape<VEC, 8 / VEC, 64, 0>());
+    return f(RowShape<VEC, 8 / VEC, kWide, 0>());
 }
 
 // A piece of a parameter row, and of the router's weights [E, n]: N experts, zeros behind the n there are.

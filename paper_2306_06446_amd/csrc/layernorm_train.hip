@@ -8,14 +8,15 @@
 namespace sa {
 
 // TRAIN: y, mean and rstd are all wanted (else each is asked about).
+constexpr int kNormWaves = 4;                // of a workgroup of rows of one wavefront or less
 template <class X, class Y, class S, int ROUTE, bool TRAIN>
-__global__ __launch_bounds__(S::THREADS) void train_norm_kernel(NormArgs a) {
+__global__ __launch_bounds__(S::WIDE ? 512 : 64 * kNormWaves) void train_norm_kernel(NormArgs a) {
     constexpr int VEC = S::VEC, CH = S::CH, HELD = ROUTE > kStreamed ? ROUTE : 0, PR = HELD ? HELD : 1, PC = HELD ? CH : 1;
-    __shared__ float red[S::LANES > 64 ? PR : 1][2][S::WAVES];
-    const int g = threadIdx.x / S::LANES, l = threadIdx.x % S::LANES;
-    const RowPlace<S> p(l, a.E);
+    __shared__ float red[S::WIDE ? PR : 1][2][8];
+    const RowPlace<S> p(a.E);
+    const int g = p.g, l = p.l, groups = S::WIDE ? p.groups : 64 * kNormWaves / S::LANES;
     const float per = 1.0f / (float)a.E;
-    RowSums<S, 1> sum{red};
+    RowSums<S, PR> sum(red, p);
     float gm[CH][VEC], bt[CH][VEC], w[PR][PC][VEC], bias[PR];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -31,21 +32,21 @@ __global__ __launch_bounds__(S::THREADS) void train_norm_kernel(NormArgs a) {
     }
 #pragma unroll
     for (int e = 0; e < HELD; ++e) bias[e] = a.bg[HELD == 2 || e < a.n ? e : 0];
-    const long stride = (long)gridDim.x * S::GROUPS;
+    const long stride = (long)gridDim.x * groups;
     auto load = [&](Piece<X, VEC> (&x)[CH], long t) {
         const X *row = static_cast<const X *>(a.x) + (size_t)(t < a.T ? t : a.T - 1) * a.E;
 #pragma unroll
         for (int c = 0; c < CH; ++c) x[c].load(row + p.at[c]);
     };
-    // What there is one of to a row is kept, a step to a lane, and leaves for LANES rows at a time: every step then stores the same
+    // What there is one of to a row is kept, a step to a lane, and leaves for PERIOD rows at a time: every step then stores the same
     // number of pieces, and a wait for the next row leaves the last row's stores in flight (one counter, in order).
     float kept_mean = 0.0f, kept_rstd = 0.0f, kept[PR];
 #pragma unroll
     for (int e = 0; e < PR; ++e) kept[e] = 0.0f;
-    const long t_first = (long)blockIdx.x * S::GROUPS + g;
-    auto flush = [&](long steps) {       // the last 1 to LANES of `steps` steps
-        const long k = (steps - 1) / S::LANES * S::LANES + l, t = t_first + k * stride;
-        if (k >= steps || t >= a.T) return;
+    const long t_first = (long)blockIdx.x * groups + g;
+    auto flush = [&](long steps) {       // the last 1 to PERIOD of `steps` steps
+        const long k = (steps - 1) / S::PERIOD * S::PERIOD + l, t = t_first + k * stride;
+        if (l >= S::PERIOD || k >= steps || t >= a.T) return;
         if (TRAIN || a.mean) a.mean[t] = kept_mean;
         if (TRAIN || a.rstd) a.rstd[t] = kept_rstd;
 #pragma unroll
@@ -70,7 +71,7 @@ __global__ __launch_bounds__(S::THREADS) void train_norm_kernel(NormArgs a) {
             }
         sum(s);
         const float rstd = 1.0f / __builtin_sqrtf(__builtin_fmaf(s[0], per, a.eps));
-        const bool keep = (int)(step & (S::LANES - 1)) == l;
+        const bool keep = (int)(step & (S::PERIOD - 1)) == l;
         kept_mean = keep ? mean : kept_mean;
         kept_rstd = keep ? rstd : kept_rstd;
         float y[CH][VEC];
@@ -90,9 +91,7 @@ __global__ __launch_bounds__(S::THREADS) void train_norm_kernel(NormArgs a) {
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) part[e] = __builtin_fmaf(y[c][i], w[e][c][i], part[e]);
             }
-            RowSums<S, HELD> all{red, sum.turn};
-            all(part, HELD == 2 ? 2 : a.n);
-            sum.turn = all.turn;
+            sum(part, HELD == 2 ? 2 : a.n);
 #pragma unroll
             for (int e = 0; e < HELD; ++e) kept[e] = keep ? part[e] + bias[e] : kept[e];
         }
@@ -111,19 +110,19 @@ __global__ __launch_bounds__(S::THREADS) void train_norm_kernel(NormArgs a) {
         }
     };
     Piece<X, VEC> nxt[CH], x[CH];
-    long t0 = (long)blockIdx.x * S::GROUPS, step = 0;
+    long t0 = (long)blockIdx.x * groups, step = 0;
     load(nxt, t0 + g);
-    for (; t0 + S::GROUPS <= a.T; t0 += stride) {
+    for (; t0 + groups <= a.T; t0 += stride) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) x[c] = nxt[c];
         load(nxt, t0 + g + stride);
         work(x, t0 + g, true, step++);
-        if ((step & (S::LANES - 1)) == 0) flush(step);
+        if ((step & (S::PERIOD - 1)) == 0) flush(step);
     }
-    if (S::GROUPS > 1 && t0 < a.T) {
+    if (t0 < a.T) {
         work(nxt, t0 + g, t0 + g < a.T, step++);
         flush(step);
-    } else if ((step & (S::LANES - 1)) != 0) {
+    } else if ((step & (S::PERIOD - 1)) != 0) {
         flush(step);
     }
 }
@@ -133,20 +132,20 @@ int launch_norm_rows(const NormArgs &a, hipStream_t st) {
     constexpr int VEC = row_vec<X, Y>();
     auto rows = [&](auto shape, auto route) {
         using S = decltype(shape);
-        // up to 4 workgroups to a CU, the same number of steps in each
-        const long cap = 1024 * 256 / S::THREADS;
-        const long steps = (a.T + S::GROUPS * cap - 1) / (S::GROUPS * cap);
-        const long blocks = (a.T + S::GROUPS * steps - 1) / (S::GROUPS * steps);
+        // 16 wavefronts to a CU (their registers), each with as many rows as it takes
+        const int threads = S::threads(a.E, kNormWaves);
+        const long groups = S::groups(a.E, kNormWaves), steps = (a.T + groups - 1) / groups, cap = 256 * 1024 / threads;
+        const dim3 grid((unsigned)(steps < cap ? steps : cap)), block((unsigned)threads);
         if (a.y && a.mean && a.rstd)
-            train_norm_kernel<X, Y, S, decltype(route)::value, true><<<dim3((unsigned)blocks), dim3(S::THREADS), 0, st>>>(a);
+            train_norm_kernel<X, Y, S, decltype(route)::value, true><<<grid, block, 0, st>>>(a);
         else
-            train_norm_kernel<X, Y, S, decltype(route)::value, false><<<dim3((unsigned)blocks), dim3(S::THREADS), 0, st>>>(a);
+            train_norm_kernel<X, Y, S, decltype(route)::value, false><<<grid, block, 0, st>>>(a);
         return check_launch("sa_layernorm");
     };
     auto with = [&](auto route) { return [&rows, route](auto shape) { return rows(shape, route); }; };
     if (!a.logits) return by_shape<VEC>(a.E, with(std::integral_constant<int, 0>()));
     if (a.n == 2) return by_shape<VEC>(a.E, with(std::integral_constant<int, 2>()));
-    if (a.E > kMaxRoute8Columns) return by_wide_shape<VEC>(a.E, with(std::integral_constant<int, kStreamed>()));
+    if (a.E > kMaxRoute8Columns) return by_wide_shape<VEC>(with(std::integral_constant<int, kStreamed>()));
     return by_shape_route8<VEC>(a.E, with(std::integral_constant<int, kMaxExperts>()));
 }
 
@@ -160,7 +159,7 @@ using namespace sa;
 constexpr int kSumColumns = 16;              // of a workgroup
 __global__ __launch_bounds__(256) void norm_grad_sum_kernel(NormGradArgs a, int parts) {
     constexpr int kSlices = 256 / (kSumColumns / 4);
-    static_assert(kSlices * 8 >= kMaxGradParts, "a thread adds up 8 parts");
+    constexpr int kEach = kMaxGradParts / kSlices;
     __shared__ double red[4][kSumColumns];
     const int n = a.dlogits ? a.n : 0, columns = padded_columns(a.E), all = (2 + n) * columns;
     const int slice = threadIdx.x / 4, quad = threadIdx.x & 3, at = (int)blockIdx.x * kSumColumns + quad * 4;
@@ -170,15 +169,15 @@ __global__ __launch_bounds__(256) void norm_grad_sum_kernel(NormGradArgs a, int 
     bool any = at < all;
     if (any) from += at;
     else if (last && quad >= 2 && a.dbg) any = true, from = a.partial_dbg + (quad - 2) * 4, step = kMaxExperts;
-    float4 v[8];
+    float4 v[kEach];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < kEach; ++k) {
         const int part = slice + k * kSlices;
         v[k] = any && part < parts ? *reinterpret_cast<const float4 *>(from + part * step) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     }
     double s[4] = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll
-    for (int k = 0; k < 8; ++k) s[0] += v[k].x, s[1] += v[k].y, s[2] += v[k].z, s[3] += v[k].w;
+    for (int k = 0; k < kEach; ++k) s[0] += v[k].x, s[1] += v[k].y, s[2] += v[k].z, s[3] += v[k].w;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
 #pragma unroll

@@ -24,11 +24,8 @@ struct TokenRouting {
 };
 
 template <int E>
-__device__ inline TokenRouting<E> route_token(const float *l, float inv_noise_std) {
+__device__ inline TokenRouting<E> route_token(const float (&v)[E], float inv_noise_std) {
     TokenRouting<E> r;
-    float v[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = l[e];
     float l0 = v[0], l1 = v[1];
     r.first = 0, r.second = 1;
     if (l1 > l0) { const float t = l0; l0 = l1; l1 = t; r.first = 1, r.second = 0; }
@@ -41,10 +38,18 @@ __device__ inline TokenRouting<E> route_token(const float *l, float inv_noise_st
         l0 = best ? v[e] : l0;
     }
     float den = 0.0f;
+    if constexpr (E == 2) {
+        // the larger one's exponential is 1
+        const float x = expf(l1 - l0);
+        r.p[0] = r.first == 0 ? 1.0f : x;
+        r.p[1] = r.first == 0 ? x : 1.0f;
+        den = 1.0f + x;
+    } else {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        r.p[e] = expf(v[e] - l0);
-        den += r.p[e];
+        for (int e = 0; e < E; ++e) {
+            r.p[e] = expf(v[e] - l0);
+            den += r.p[e];
+        }
     }
     const float inv = 1.0f / den;
     float p0 = 0.0f, p1 = 0.0f;
@@ -57,6 +62,22 @@ __device__ inline TokenRouting<E> route_token(const float *l, float inv_noise_st
 #pragma unroll
     for (int e = 0; e < E; ++e) r.z[e] = (r.p[e] - (e == r.first ? p1 : p0)) * inv_noise_std;
     return r;
+}
+
+// Phi(-|z|), off by 1.6e-7 at most (2.6 units of 2^-24), 4e-10 on average: with x = |z| / sqrt(2), exp(x^2) erfc(x) / 2 is smooth and is
+// a polynomial in 1 / (1 + 0.55 x) up to 8.3e-9 (weighted least squares against erfcx in fp64, weights shifted to the largest errors).
+// A library erfc takes five times the instructions, its two branches both, and was most of the sums' time.
+__device__ inline float normal_tail(float z) {
+    const float x = fabsf(z) * 0.70710678118654752f;
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.55f, x, 1.0f));
+    float p = 0.0535219675f;
+    p = __builtin_fmaf(p, t, -0.258346282f);
+    p = __builtin_fmaf(p, t, 0.378522362f);
+    p = __builtin_fmaf(p, t, -0.0193116462f);
+    p = __builtin_fmaf(p, t, 0.194600117f);
+    p = __builtin_fmaf(p, t, 0.151046025f);
+    p = __builtin_fmaf(p, t, -3.25356018e-05f);
+    return expf(-x * x) * p;
 }
 
 struct BalanceArgs {
@@ -83,49 +104,101 @@ __device__ inline double dpp_add_d(double v) {
     return v + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 
-// Sum over a wavefront in all of its lanes, the most distant lanes first (as group_sum<64>, in fp64).
-__device__ inline double wave_sum_d(double v) {
-    v += __shfl_xor(v, 32, 64);
-    v += __shfl_xor(v, 16, 64);
+// Of two values: the upper half of a's lanes (rows) and the lower half of b's change places, and the sum is taken: sums of a in the
+// lower half, of b in the upper one.
+template <bool ROWS>
+__device__ inline double swap_add_d(double a, double b) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, a), w = __builtin_bit_cast(uint64_t, b);
+    const auto lo = ROWS ? __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)w, false, false)
+                         : __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)w, false, false);
+    const auto hi = ROWS ? __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(w >> 32), false, false)
+                         : __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(w >> 32), false, false);
+    return __builtin_bit_cast(double, (uint64_t)hi[0] << 32 | lo[0]) + __builtin_bit_cast(double, (uint64_t)hi[1] << 32 | lo[1]);
+}
+
+// Sum over a row of 16 lanes in all of them.
+__device__ inline double row_sum_d(double v) {
     v = dpp_add_d<0x128>(v);
     v = dpp_add_d<0x124>(v);
     v = dpp_add_d<0x122>(v);
     return dpp_add_d<0x121>(v);
 }
+__device__ inline double wave_sum_d(double v) { return row_sum_d(swap_add_d<true>(swap_add_d<false>(v, v), swap_add_d<false>(v, v))); }
 
-// Sums over the tokens first, first + step, ... of every thread of WAVES wavefronts, in thread 0.. of LDS: red[2 E], cnt[E].
-template <int E, int WAVES>
-struct TokenSums {
-    double red[2 * E][WAVES];
-    int32_t cnt[E][WAVES];
-};
-template <int E, int WAVES>
-__device__ inline void sum_tokens(const BalanceArgs &a, long first, long step, TokenSums<E, WAVES> &s) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    double sp[E], sq[E];
-    int cnt[E];
+// N sums over a wavefront at once, to out[k][wave]: four of them share the steps within rows of lanes, one to each.
+template <int N, int WAVES>
+__device__ inline void wave_sums_d(const double (&v)[N], double (*out)[WAVES], int lane, int wave) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) sp[e] = sq[e] = 0.0, cnt[e] = 0;
-    for (long t = first; t < a.T; t += step) {
-        if (a.valid && a.valid[t] == 0) continue;
-        const TokenRouting<E> r = route_token<E>(a.logits + (size_t)t * E, 1.0f / a.noise_std);
+    for (int k = 0; k < N; k += 4) {
+        const double a = v[k], b = v[k + 1 < N ? k + 1 : k], c = v[k + 2 < N ? k + 2 : k], d = v[k + 3 < N ? k + 3 : k];
+        // rows 0 and 1 of lanes: a and b; rows 2 and 3: c and d
+        const double s = row_sum_d(swap_add_d<true>(swap_add_d<false>(a, c), swap_add_d<false>(b, d)));
+        const int at = k + (lane >> 4);
+        if ((lane & 15) == 0 && at < N) out[at][wave] = s;
+    }
+}
+
+// A thread's share of the sums, tokens added one by one; counts are a wavefront's.
+template <int E>
+struct TokenSums {
+    double v[2 * E];
+    int cnt[E];
+    __device__ inline TokenSums() {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = v[E + e] = 0.0, cnt[e] = 0;
+    }
+    __device__ inline void add(const TokenRouting<E> &r, bool in) {
+        const float both = E == 2 ? normal_tail(r.z[0]) : 0.0f;          // of two experts, z has two signs
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            sp[e] += (double)r.p[e];
-            sq[e] += (double)(0.5f * erfcf(r.z[e] * -0.70710678118654752f));
-            cnt[e] += r.first == e ? 1 : 0;
+            const float tail = E == 2 ? both : normal_tail(r.z[e]), q = e == r.first ? 1.0f - tail : tail;
+            v[e] += in ? (double)r.p[e] : 0.0;
+            v[E + e] += in ? (double)q : 0.0;
+            cnt[e] += __popcll(__ballot(in && r.first == e));
         }
     }
+};
+
+// Workgroup's sums in LDS, a value to a wavefront.
+template <int E, int WAVES>
+struct GroupSums {
+    double v[2 * E][WAVES];
+    int32_t cnt[E][WAVES];
+    __device__ inline void leave(const TokenSums<E> &s) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        wave_sums_d<2 * E, WAVES>(s.v, v, lane, wave);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const double p = wave_sum_d(sp[e]), q = wave_sum_d(sq[e]);
-        int c = cnt[e];
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) c += __shfl_xor(c, off, 64);
-        if (lane == 0) s.red[e][wave] = p, s.red[E + e][wave] = q, s.cnt[e][wave] = c;
+        for (int e = 0; e < E; ++e)
+            if (lane == 0) cnt[e][wave] = s.cnt[e];
+        __syncthreads();
     }
-    __syncthreads();
-}
+    __device__ inline double sum(int i) const {
+        double s = 0.0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) s += v[i][w];
+        return s;
+    }
+    __device__ inline int count(int e) const {
+        int c = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) c += cnt[e][w];
+        return c;
+    }
+};
+
+// A token as it is asked for: what of its logits and its place in the batch can be had before anything is known of the others.
+template <int E>
+struct Token {
+    float l[E];
+    bool valid;
+    __device__ inline void load(const BalanceArgs &a, long t) {
+        const bool there = t < a.T;
+        const size_t at = there ? (size_t)t : 0;
+        valid = there && (!a.valid || a.valid[at] != 0);
+#pragma unroll
+        for (int e = 0; e < E; ++e) l[e] = a.T > 0 ? a.logits[at * E + e] : 0.0f;
+    }
+};
 
 // The losses and, in coeff, the gradients of the sums of p and of q, from the sums u of alpha p and alpha q (LDS).
 template <int E>
@@ -148,41 +221,36 @@ __device__ inline void losses_of(const BalanceArgs &a, const double (&u)[2 * E],
 }
 
 template <int E>
-__device__ inline void grad_tokens(const BalanceArgs &a, long first, long step, const float (&coeff)[2 * E]) {
-    const float peak = 0.39894228040143268f / a.noise_std;
-    float c[E], f0[E];
+__device__ inline void grad_token(const BalanceArgs &a, long t, bool valid, const TokenRouting<E> &r, const float (&density)[E],
+                                  const float (&coeff)[2 * E]) {
+    float *dl = a.dlogits + (size_t)t * E;
+    float up[E], to_first = 0.0f, to_second = 0.0f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) c[e] = coeff[e], f0[e] = coeff[E + e] * peak;
-    for (long t = first; t < a.T; t += step) {
-        float *dl = a.dlogits + (size_t)t * E;
-        if (a.valid && a.valid[t] == 0) {
-            if (!a.accumulate) {
-#pragma unroll
-                for (int e = 0; e < E; ++e) dl[e] = 0.0f;
-            }
-            continue;
-        }
-        const TokenRouting<E> r = route_token<E>(a.logits + (size_t)t * E, 1.0f / a.noise_std);
-        float up[E], to_first = 0.0f, to_second = 0.0f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float f = f0[e] * expf(-0.5f * r.z[e] * r.z[e]);
-            up[e] = c[e] + f;
-            to_second -= e == r.first ? f : 0.0f;
-            to_first -= e == r.first ? 0.0f : f;
-        }
-        float mean = 0.0f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            up[e] += e == r.first ? to_first : e == r.second ? to_second : 0.0f;
-            mean = __builtin_fmaf(r.p[e], up[e], mean);
-        }
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float d = r.p[e] * (up[e] - mean);
-            dl[e] = a.accumulate ? dl[e] + d : d;
-        }
+    for (int e = 0; e < E; ++e) {
+        const float f = coeff[E + e] * density[e];
+        up[e] = coeff[e] + f;
+        to_second -= e == r.first ? f : 0.0f;
+        to_first -= e == r.first ? 0.0f : f;
     }
+    float mean = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        up[e] += e == r.first ? to_first : e == r.second ? to_second : 0.0f;
+        mean = __builtin_fmaf(r.p[e], up[e], mean);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const float d = valid ? r.p[e] * (up[e] - mean) : 0.0f;
+        if (!a.accumulate) dl[e] = d;
+        else if (valid) dl[e] += d;
+    }
+}
+
+template <int E>
+__device__ inline void densities(const TokenRouting<E> &r, float noise_std, float (&out)[E]) {
+    const float peak = 0.39894228040143268f / noise_std;
+#pragma unroll
+    for (int e = 0; e < E; ++e) out[e] = peak * expf(-0.5f * r.z[e] * r.z[e]);
 }
 
 constexpr int kSumThreads = 512, kSumWaves = kSumThreads / 64, kMaxSumParts = 256, kMaxGradBlocks = 512;
@@ -191,66 +259,105 @@ constexpr long kOneLogits = 2048;        // up to this many, all of it in one wo
 
 template <int E>
 __global__ __launch_bounds__(kSumThreads) void balance_sums_kernel(BalanceArgs a) {
-    __shared__ TokenSums<E, kSumWaves> s;
-    sum_tokens<E, kSumWaves>(a, (long)blockIdx.x * kSumThreads + threadIdx.x, (long)a.parts * kSumThreads, s);
-    const int i = threadIdx.x;
-    if (i < 2 * E) {
-        double v = 0.0;
-        for (int w = 0; w < kSumWaves; ++w) v += s.red[i][w];
-        a.partial[(size_t)i * a.parts + blockIdx.x] = v;
-    } else if (i < 3 * E) {
-        int c = 0;
-        for (int w = 0; w < kSumWaves; ++w) c += s.cnt[i - 2 * E][w];
-        a.partial_counts[(size_t)(i - 2 * E) * a.parts + blockIdx.x] = c;
+    __shared__ GroupSums<E, kSumWaves> group;
+    TokenSums<E> s;
+    const long step = (long)gridDim.x * kSumThreads;
+    Token<E> nxt;
+    long t0 = (long)blockIdx.x * kSumThreads;
+    nxt.load(a, t0 + threadIdx.x);
+    for (; t0 < a.T; t0 += step) {
+        const Token<E> x = nxt;
+        nxt.load(a, t0 + step + threadIdx.x);
+        s.add(route_token<E>(x.l, 1.0f / a.noise_std), x.valid);
     }
+    group.leave(s);
+    const int i = threadIdx.x;
+    if (i < 2 * E) a.partial[(size_t)i * a.parts + blockIdx.x] = group.sum(i);
+    else if (i < 3 * E) a.partial_counts[(size_t)(i - 2 * E) * a.parts + blockIdx.x] = group.count(i - 2 * E);
 }
 
-// Every workgroup adds up the parts (a few KB out of the caches) rather than wait for a launch that does.
+// Every workgroup adds up the parts (a few KB out of the caches) rather than wait for a launch that does; its first tokens' routing is
+// computed while they are on the way.
 template <int E>
 __global__ __launch_bounds__(kSumThreads) void balance_grad_kernel(BalanceArgs a) {
     __shared__ double u[2 * E];
-    __shared__ float coeff[2 * E];
+    __shared__ float coeff_of[2 * E];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int v = wave; v < 3 * E; v += kSumWaves) {
-        if (v < 2 * E) {
-            double sum = 0.0;
-            for (int k = lane; k < a.parts; k += 64) sum += a.partial[(size_t)v * a.parts + k];
-            sum = wave_sum_d(sum);
-            if (lane == 0) u[v] = sum * (double)a.alpha[v % E];
-        } else if (blockIdx.x == 0 && a.counts) {
+    constexpr int kEach = kMaxSumParts / 64, kMine = (2 * E + kSumWaves - 1) / kSumWaves;
+    double part[kMine][kEach];
+#pragma unroll
+    for (int m = 0; m < kMine; ++m)
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const int v = wave + m * kSumWaves, at = lane + 64 * k;
+            part[m][k] = v < 2 * E && at < a.parts ? a.partial[(size_t)v * a.parts + at] : 0.0;
+        }
+    const long step = (long)gridDim.x * kSumThreads;
+    long t = (long)blockIdx.x * kSumThreads + threadIdx.x;
+    Token<E> x;
+    x.load(a, t);
+    TokenRouting<E> r = route_token<E>(x.l, 1.0f / a.noise_std);
+    float density[E], coeff[2 * E];
+    densities<E>(r, a.noise_std, density);
+#pragma unroll
+    for (int m = 0; m < kMine; ++m) {
+        const int v = wave + m * kSumWaves;
+        double s = 0.0;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) s += part[m][k];
+        s = wave_sum_d(s);
+        if (lane == 0 && v < 2 * E) u[v] = s * (double)a.alpha[v % E];
+    }
+    if (blockIdx.x == 0 && a.counts) {
+        for (int e = wave; e < E; e += kSumWaves) {
             int c = 0;
-            for (int k = lane; k < a.parts; k += 64) c += a.partial_counts[(size_t)(v - 2 * E) * a.parts + k];
+            for (int k = lane; k < a.parts; k += 64) c += a.partial_counts[(size_t)e * a.parts + k];
 #pragma unroll
             for (int off = 32; off >= 1; off >>= 1) c += __shfl_xor(c, off, 64);
-            if (lane == 0) a.counts[v - 2 * E] = c;
+            if (lane == 0) a.counts[e] = c;
         }
     }
     __syncthreads();
-    losses_of<E>(a, u, coeff, blockIdx.x == 0);
+    losses_of<E>(a, u, coeff_of, blockIdx.x == 0);
     __syncthreads();
-    grad_tokens<E>(a, (long)blockIdx.x * kSumThreads + threadIdx.x, (long)gridDim.x * kSumThreads, coeff);
+#pragma unroll
+    for (int i = 0; i < 2 * E; ++i) coeff[i] = coeff_of[i];
+    while (t < a.T) {
+        const bool valid = x.valid;
+        x.load(a, t + step);
+        grad_token<E>(a, t, valid, r, density, coeff);
+        t += step;
+        if (t >= a.T) break;
+        r = route_token<E>(x.l, 1.0f / a.noise_std);
+        densities<E>(r, a.noise_std, density);
+    }
 }
 
 template <int E>
 __global__ __launch_bounds__(kOneThreads) void balance_one_kernel(BalanceArgs a) {
-    __shared__ TokenSums<E, kOneThreads / 64> s;
+    constexpr int kTokens = (int)((kOneLogits / E + kOneThreads - 1) / kOneThreads);      // of a thread, at most
+    static_assert(kTokens == 1, "a thread has a token at most");
+    __shared__ GroupSums<E, kOneThreads / 64> group;
     __shared__ double u[2 * E];
-    __shared__ float coeff[2 * E];
-    sum_tokens<E, kOneThreads / 64>(a, threadIdx.x, kOneThreads, s);
+    __shared__ float coeff_of[2 * E];
+    Token<E> x;
+    x.load(a, threadIdx.x);
+    const TokenRouting<E> r = route_token<E>(x.l, 1.0f / a.noise_std);
+    TokenSums<E> s;
+    s.add(r, x.valid);
+    group.leave(s);
     const int i = threadIdx.x;
-    if (i < 2 * E) {
-        double v = 0.0;
-        for (int w = 0; w < kOneThreads / 64; ++w) v += s.red[i][w];
-        u[i] = v * (double)a.alpha[i % E];
-    } else if (i < 3 * E && a.counts) {
-        int c = 0;
-        for (int w = 0; w < kOneThreads / 64; ++w) c += s.cnt[i - 2 * E][w];
-        a.counts[i - 2 * E] = c;
-    }
+    if (i < 2 * E) u[i] = group.sum(i) * (double)a.alpha[i % E];
+    else if (i < 3 * E && a.counts) a.counts[i - 2 * E] = group.count(i - 2 * E);
     __syncthreads();
-    losses_of<E>(a, u, coeff, true);
+    losses_of<E>(a, u, coeff_of, true);
     __syncthreads();
-    grad_tokens<E>(a, threadIdx.x, kOneThreads, coeff);
+    if (threadIdx.x >= a.T) return;
+    float density[E], coeff[2 * E];
+    densities<E>(r, a.noise_std, density);
+#pragma unroll
+    for (int k = 0; k < 2 * E; ++k) coeff[k] = coeff_of[k];
+    grad_token<E>(a, threadIdx.x, x.valid, r, density, coeff);
 }
 
 int balance_parts(long T) {
@@ -308,24 +415,24 @@ __device__ inline float max16(float v) {
     return v;
 }
 
-// 16 to 64 lanes to a row, which they walk over in blocks of S::COLUMNS columns; an expert of its routing to a lane.
+// 16 to 64 lanes to a row, which they walk over in blocks of columns; an expert of its routing to a lane.
 template <class Y, class X, class S>
 __global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradArgs a) {
-    constexpr int VEC = S::VEC, CH = S::CH;
+    constexpr int VEC = S::VEC, CH = S::CH, GROUPS = 256 / S::LANES, COLUMNS = S::LANES * VEC * CH;
     const int32_t *rows;
     long n_rows;
     resolve_rows(a.sel, rows, n_rows);
     const int g = threadIdx.x / S::LANES, l = threadIdx.x % S::LANES;
     const bool dot = a.dgate || a.dlogits;
-    const long stride = (long)gridDim.x * S::GROUPS;
-    for (long i = (long)blockIdx.x * S::GROUPS + g; i < n_rows; i += stride) {
+    const long stride = (long)gridDim.x * GROUPS;
+    for (long i = (long)blockIdx.x * GROUPS + g; i < n_rows; i += stride) {
         const size_t r = rows ? (size_t)rows[i] : (size_t)i;
         const float gate = a.gate ? a.gate[r] : 1.0f;
         const Y *dy = static_cast<const Y *>(a.dy) + r * a.E;
         const X *src = static_cast<const X *>(a.src) + (size_t)i * a.E;
         X *dsrc = static_cast<X *>(a.dsrc) + (size_t)i * a.E;
         float s = 0.0f;
-        for (int j0 = 0; j0 < a.E; j0 += S::COLUMNS) {
+        for (int j0 = 0; j0 < a.E; j0 += COLUMNS) {
             Piece<Y, VEC> d[CH];
             Piece<X, VEC> v[CH];
             int at[CH], skip[CH];
@@ -371,7 +478,7 @@ struct RunCombineGrad {
         auto rows = [&](auto shape) {
             using S = decltype(shape);
             // 8 workgroups to a CU; the rows there are may be fewer than max_rows
-            const long blocks = (a.sel.max_rows + S::GROUPS - 1) / S::GROUPS;
+            const long blocks = (a.sel.max_rows + 256 / S::LANES - 1) / (256 / S::LANES);
             combine_grad_kernel<Y, X, S><<<dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, st>>>(a);
             return check_launch("sa_combine_rows_backward");
         };

@@ -53,22 +53,32 @@ constexpr int row_vec() { return sizeof(X) == 2 && sizeof(Y) == 2 ? 8 : 4; }
 // would reach past the row's end (the last one of a row that VEC does not divide, and those behind it) begins VEC before the end
 // instead: no load or store needs a choice, elements that two lanes hold are computed and written by both, the same bits.  Only sums
 // over the row ask whether an element is a lane's own.  The first FULL pieces of a lane are whole in every row that comes here.
+// LANES is 16, 32 or 64, rows side by side in a wavefront, or kWide: the lanes of 2 to 8 wavefronts, as many as the row takes.
+constexpr int kWide = 512;
 template <int VEC_, int CH_, int LANES_, int FULL_>
 struct RowShape {
     static constexpr int VEC = VEC_, CH = CH_, LANES = LANES_, FULL = FULL_;
-    static constexpr int THREADS = LANES <= 256 ? 256 : LANES;
-    static constexpr int GROUPS = THREADS / LANES;           // rows side by side in a workgroup
-    static constexpr int WAVES = THREADS / 64;
-    static constexpr int COLUMNS = VEC * CH * LANES;
+    static constexpr bool WIDE = LANES > 64;
+    static constexpr int PERIOD = WIDE ? 64 : LANES;         // rows whose statistics the lanes of one wavefront can keep
+    static int waves(int E) { return WIDE ? (E + 64 * VEC * CH - 1) / (64 * VEC * CH) : 1; }
+    // rows side by side in a workgroup of up to max_waves wavefronts
+    static int groups(int E, int max_waves) { return WIDE ? (waves(E) < max_waves ? max_waves / waves(E) : 1) : max_waves * 64 / LANES; }
+    static int threads(int E, int max_waves) { return WIDE ? 64 * waves(E) * groups(E, max_waves) : 64 * max_waves; }
 };
 
 template <class S>
 struct RowPlace {
+    int g, l, lanes, groups;             // this lane's row among the workgroup's, and its place in it
     int at[S::CH], skip[S::CH];
-    __device__ inline RowPlace(int l, int E) {
+    __device__ inline RowPlace(int E) {
+        const int waves = S::WIDE ? __builtin_amdgcn_readfirstlane((E + 64 * S::VEC * S::CH - 1) / (64 * S::VEC * S::CH)) : 1;
+        lanes = S::WIDE ? 64 * waves : S::LANES;
+        groups = S::WIDE ? (int)(blockDim.x >> 6) / waves : (int)blockDim.x / S::LANES;
+        g = S::WIDE ? __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6) / waves) : (int)threadIdx.x / S::LANES;
+        l = (int)threadIdx.x - g * lanes;
 #pragma unroll
         for (int c = 0; c < S::CH; ++c) {
-            const int j = (c * S::LANES + l) * S::VEC;
+            const int j = (c * lanes + l) * S::VEC;
             at[c] = c < S::FULL || j + S::VEC <= E ? j : E - S::VEC;
             skip[c] = j - at[c];
         }
@@ -80,28 +90,28 @@ struct RowPlace {
 // one barrier per exchange is enough (a wavefront that writes a buffer again has passed the barrier behind its last reads).
 template <class S, int N>
 struct RowSums {
-    float (*red)[2][S::WAVES];           // [N][2][WAVES] in LDS, where a row has several wavefronts
-    int turn = 0;
-    __device__ inline void operator()(float (&v)[N], int used = N) {
+    float (*red)[2][8];                  // [N][2][wavefronts] in LDS, where a row has several wavefronts
+    int first, waves, turn = 0;
+    __device__ inline RowSums(float (*red_)[2][8], const RowPlace<S> &p) : red(red_), first(p.g * (p.lanes / 64)), waves(p.lanes / 64) {}
+    template <int M>
+    __device__ inline void operator()(float (&v)[M], int used = M) {
+        static_assert(M <= N, "room in LDS");
         constexpr int L = S::LANES < 64 ? S::LANES : 64;
 #pragma unroll
-        for (int k = 0; k < N; ++k)
+        for (int k = 0; k < M; ++k)
             if (k < used) v[k] = group_sum<L>(v[k]);
-        if constexpr (S::LANES > 64) {
-            constexpr int W = S::LANES / 64;
-            const int wave = threadIdx.x >> 6, first = wave / W * W;
+        if constexpr (S::WIDE) {
             if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-                for (int k = 0; k < N; ++k)
-                    if (k < used) red[k][turn][wave] = v[k];
+                for (int k = 0; k < M; ++k)
+                    if (k < used) red[k][turn][threadIdx.x >> 6] = v[k];
             }
             __syncthreads();
 #pragma unroll
-            for (int k = 0; k < N; ++k) {
+            for (int k = 0; k < M; ++k) {
                 if (k >= used) continue;
                 float s = 0.0f;
-#pragma unroll
-                for (int w = 0; w < W; ++w) s += red[k][turn][first + w];
+                for (int w = 0; w < waves; ++w) s += red[k][turn][first + w];
                 v[k] = s;
             }
             turn ^= 1;
