@@ -200,25 +200,40 @@ struct Token {
     }
 };
 
-// The losses and, in coeff, the gradients of the sums of p and of q, from the sums u of alpha p and alpha q (LDS).
+// What the losses are made of, in LDS; alpha and the losses' weights are asked for before the sums are there.
 template <int E>
-__device__ inline void losses_of(const BalanceArgs &a, const double (&u)[2 * E], float (&coeff)[2 * E], bool write) {
-    const int i = threadIdx.x, kind = i / E, e = i % E;
-    if (i < 2 * E) {
-        double sum = 0.0, squares = 0.0, var = 0.0;
+struct Losses {
+    double sum[2 * E];                   // over tokens, of p and of q
+    float alpha[E], weight[2], coeff[2 * E];     // coeff: gradients of the sums
+
+    __device__ inline void begin(const BalanceArgs &a) {
+        const int i = (int)threadIdx.x - 64;             // the second wavefront: the first has its share of the sums
+        if (i >= 0 && i < E) alpha[i] = a.alpha[i];
+        else if (i >= E && i < E + 2) weight[i - E] = a.dlosses[i - E];
+    }
+    // behind a barrier; another one before coeff is read
+    __device__ inline void end(const BalanceArgs &a, bool write) {
+        const int i = threadIdx.x, kind = i / E, e = i % E;
+        if (i >= 2 * E) return;
+        double u[E], total = 0.0, squares = 0.0, var = 0.0, mine = 0.0;
 #pragma unroll
-        for (int k = 0; k < E; ++k) sum += u[kind * E + k], squares += u[kind * E + k] * u[kind * E + k];
-        const double m = sum / E;
+        for (int k = 0; k < E; ++k) {
+            u[k] = sum[kind * E + k] * (double)alpha[k];
+            total += u[k], squares += u[k] * u[k];
+            mine = k == e ? u[k] : mine;
+        }
+        const double m = total / E;
 #pragma unroll
-        for (int k = 0; k < E; ++k) var += (u[kind * E + k] - m) * (u[kind * E + k] - m);
+        for (int k = 0; k < E; ++k) var += (u[k] - m) * (u[k] - m);
+        const double inv = 1.0 / (m * m * E);
         const bool none = m == 0.0;
-        coeff[i] = none ? 0.0f : (float)(2.0 / (E * m * m) * (u[i] - squares / sum) * (double)a.alpha[e] * (double)a.dlosses[kind]);
+        coeff[i] = none ? 0.0f : (float)(2.0 * inv * (mine - squares / total) * (double)alpha[e] * (double)weight[kind]);
         if (write) {
-            if (e == 0) a.losses[kind] = none ? 0.0f : (float)(var / E / (m * m));
-            if (a.sums) a.sums[i] = (float)u[i];
+            if (e == 0) a.losses[kind] = none ? 0.0f : (float)(var * inv);
+            if (a.sums) a.sums[i] = (float)mine;
         }
     }
-}
+};
 
 template <int E>
 __device__ inline void grad_token(const BalanceArgs &a, long t, bool valid, const TokenRouting<E> &r, const float (&density)[E],
@@ -280,8 +295,8 @@ __global__ __launch_bounds__(kSumThreads) void balance_sums_kernel(BalanceArgs a
 // computed while they are on the way.
 template <int E>
 __global__ __launch_bounds__(kSumThreads) void balance_grad_kernel(BalanceArgs a) {
-    __shared__ double u[2 * E];
-    __shared__ float coeff_of[2 * E];
+    __shared__ Losses<E> losses;
+    losses.begin(a);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     constexpr int kEach = kMaxSumParts / 64, kMine = (2 * E + kSumWaves - 1) / kSumWaves;
     double part[kMine][kEach];
@@ -306,7 +321,7 @@ __global__ __launch_bounds__(kSumThreads) void balance_grad_kernel(BalanceArgs a
 #pragma unroll
         for (int k = 0; k < kEach; ++k) s += part[m][k];
         s = wave_sum_d(s);
-        if (lane == 0 && v < 2 * E) u[v] = s * (double)a.alpha[v % E];
+        if (lane == 0 && v < 2 * E) losses.sum[v] = s;
     }
     if (blockIdx.x == 0 && a.counts) {
         for (int e = wave; e < E; e += kSumWaves) {
@@ -318,10 +333,10 @@ __global__ __launch_bounds__(kSumThreads) void balance_grad_kernel(BalanceArgs a
         }
     }
     __syncthreads();
-    losses_of<E>(a, u, coeff_of, blockIdx.x == 0);
+    losses.end(a, blockIdx.x == 0);
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 2 * E; ++i) coeff[i] = coeff_of[i];
+    for (int i = 0; i < 2 * E; ++i) coeff[i] = losses.coeff[i];
     while (t < a.T) {
         const bool valid = x.valid;
         x.load(a, t + step);
@@ -338,8 +353,8 @@ __global__ __launch_bounds__(kOneThreads) void balance_one_kernel(BalanceArgs a)
     constexpr int kTokens = (int)((kOneLogits / E + kOneThreads - 1) / kOneThreads);      // of a thread, at most
     static_assert(kTokens == 1, "a thread has a token at most");
     __shared__ GroupSums<E, kOneThreads / 64> group;
-    __shared__ double u[2 * E];
-    __shared__ float coeff_of[2 * E];
+    __shared__ Losses<E> losses;
+    losses.begin(a);
     Token<E> x;
     x.load(a, threadIdx.x);
     const TokenRouting<E> r = route_token<E>(x.l, 1.0f / a.noise_std);
@@ -347,16 +362,16 @@ __global__ __launch_bounds__(kOneThreads) void balance_one_kernel(BalanceArgs a)
     s.add(r, x.valid);
     group.leave(s);
     const int i = threadIdx.x;
-    if (i < 2 * E) u[i] = group.sum(i) * (double)a.alpha[i % E];
+    if (i < 2 * E) losses.sum[i] = group.sum(i);
     else if (i < 3 * E && a.counts) a.counts[i - 2 * E] = group.count(i - 2 * E);
     __syncthreads();
-    losses_of<E>(a, u, coeff_of, true);
+    losses.end(a, true);
     __syncthreads();
     if (threadIdx.x >= a.T) return;
     float density[E], coeff[2 * E];
     densities<E>(r, a.noise_std, density);
 #pragma unroll
-    for (int k = 0; k < 2 * E; ++k) coeff[k] = coeff_of[k];
+    for (int k = 0; k < 2 * E; ++k) coeff[k] = losses.coeff[k];
     grad_token<E>(a, threadIdx.x, x.valid, r, density, coeff);
 }
 
