@@ -369,7 +369,8 @@ int sa_layernorm(const void *x, int x_type, long T, int E, const float *gamma, c
  * Parameter gradients (fp32 [E], [E], [E, n_experts], [n_experts]): dgamma and dbeta both or neither, dwg and dbg both or
  * neither and only with dlogits and the other two.  accumulate != 0 adds them to what the buffers hold.  beta is read for dwg only.
  * T = 0 leaves sums of nothing (zeros, or with accumulate the buffers as they are).  dx may be dres, dy or x (of the same type).
- * Without parameter gradients no workspace is needed (the query is for calls with them).
+ * Without parameter gradients a workspace is needed only for n_experts > 2 and E > 2048 (the query is for calls with them; the size
+ * that a call without them asks for is in sa_last_error()).
  */
 size_t sa_layernorm_backward_workspace_bytes(long T, int E, int n_experts /* 0: without dlogits */);
 int sa_layernorm_backward(const void *dy, int y_type, const void *x, int x_type, long T, int E, const float *gamma,

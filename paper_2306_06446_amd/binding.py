@@ -581,10 +581,10 @@ def sa_layernorm_backward(dy, x, gamma, beta, eps, mean=None, rstd=None, dres=No
         if n:
             dwg = torch.empty((E, n), dtype=f32, device=dev) if dwg is None else dwg
             dbg = torch.empty(n, dtype=f32, device=dev) if dbg is None else dbg
-        if workspace is None:
-            workspace = _workspace(lib.sa_layernorm_backward_workspace_bytes(T, E, n), dev)
     elif dgamma is not None or dbeta is not None or dwg is not None or dbg is not None:
         raise ValueError("want_params: buffers of parameter gradients are given, but none are wanted")
+    if workspace is None and (want_params or (n > 2 and E > 2048)):
+        workspace = _workspace(lib.sa_layernorm_backward_workspace_bytes(T, E, n), x.device)
     if dy.dtype not in _ROW_TYPES:
         raise ValueError("dy: %s is no type of rows" % dy.dtype)
     _check(lib.sa_layernorm_backward(
@@ -617,7 +617,7 @@ def sa_moe_balance_loss_grad(logits, alpha, noise_std, dlosses, valid=None, loss
     counts = torch.empty(E, dtype=torch.int32, device=dev) if counts is None else counts
     dlogits = torch.empty_like(logits) if dlogits is None else dlogits
     if workspace is None:
-        workspace = _workspace(lib.sa_moe_balance_loss_grad_workspace_bytes(T, E), dev)
+        workspace = _workspace(lib.sa_moe_balance_loss_grad_workspace_bytes(T, E), logits.device)
     if valid is not None and valid.dtype == torch.bool:
         valid = valid.view(torch.uint8)
     _check(lib.sa_moe_balance_loss_grad(

@@ -41,29 +41,40 @@ struct GradPlan {
     static constexpr int HELD = ROUTE > kStreamed ? ROUTE : 0;
     static constexpr int ELEMS = S::VEC * S::CH;
     static constexpr int ROW = ELEMS * (2 * sizeof(X) + sizeof(Y)) / 4;
-    static constexpr bool AHEAD = ELEMS * (2 + HELD + 1 + HELD + 2) + 2 * ROW + 48 < 256;
+    static constexpr int REGISTERS = ELEMS * (2 + HELD + 1 + HELD + 2) + 2 * ROW + 48;
+    static constexpr bool AHEAD = REGISTERS < 256;
+    // A workgroup to a CU, of the wavefronts that its registers have room for: the fewest parts that keep it busy.
+    static constexpr int WAVES = !S::WIDE && REGISTERS <= 136 ? 16 : 8;
+    static constexpr int SIDE = 64 * WAVES * ELEMS;          // a value to each of its elements, in LDS
+    static constexpr int AT_ONCE = SIDE <= 8192 ? 4 : 2;
 };
 
-constexpr int kGradWaves = 4;                // of a workgroup of rows of up to as many wavefronts
 template <class X, class Y, class S, int ROUTE>
-__global__ __launch_bounds__(S::WIDE ? 512 : 64 * kGradWaves) void norm_grad_kernel(NormGradArgs a) {
+__global__ __launch_bounds__((64 * GradPlan<X, Y, S, ROUTE>::WAVES)) void norm_grad_kernel(NormGradArgs a) {
     using Plan = GradPlan<X, Y, S, ROUTE>;
     constexpr int VEC = S::VEC, CH = S::CH, HELD = Plan::HELD, Q = 2 + HELD;
     constexpr bool AHEAD = Plan::AHEAD;
     constexpr int PC = HELD ? CH : 1, PR = HELD ? HELD : 1;
     __shared__ float red[S::WIDE ? 2 : 1][2][8];
-    __shared__ float side[64 * kGradWaves * CH * VEC], side_dl[64 * kGradWaves / S::PERIOD][PR];      // of several groups
+    constexpr int BATCH = Q < Plan::AT_ONCE ? Q : Plan::AT_ONCE;
+    constexpr int SIDE = HELD == kMaxExperts && kRouterTileFloats > BATCH * Plan::SIDE ? kRouterTileFloats : BATCH * Plan::SIDE;
+    __shared__ float side[SIDE], side_dl[64 * Plan::WAVES / S::PERIOD][PR];
     const RowPlace<S> p(a.E);
-    constexpr int GROUPS = 64 * kGradWaves / S::LANES;
-    const int g = p.g, groups = S::WIDE ? p.groups : GROUPS;
+    const int g = p.g, groups = p.groups;
     const float per = 1.0f / (float)a.E;
     RowSums<S, 2> sums(red, p);
+    const long stride = (long)gridDim.x * groups;
+    auto clamped = [&](long t) { return t < a.T ? t : a.T - 1; };
+    GradRow<X, Y, S, ROUTE> nxt;
+    long t0 = (long)blockIdx.x * groups;
+    if constexpr (AHEAD) nxt.load(a, p, clamped(t0 + g));
     float gm[CH][VEC], w[PR][PC][VEC];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         load_columns<VEC>(gm[c], a.gamma + p.at[c]);
-        if constexpr (HELD > 0) load_router<VEC, HELD, PC>(w, c, a.wg + (size_t)p.at[c] * a.n, a.n);
+        if constexpr (HELD == 2) load_router_pair<VEC, PC>(w, c, a.wg + 2 * (size_t)p.at[c]);
     }
+    if constexpr (HELD == kMaxExperts) load_router<S, PR>(w, p, a.wg, a.E, a.n, side);
     float acc[Q][CH][VEC], dl_sum[PR];
 #pragma unroll
     for (int q = 0; q < Q; ++q)
@@ -74,8 +85,6 @@ __global__ __launch_bounds__(S::WIDE ? 512 : 64 * kGradWaves) void norm_grad_ker
 #pragma unroll
     for (int e = 0; e < PR; ++e) dl_sum[e] = 0.0f;
 
-    const long stride = (long)gridDim.x * groups;
-    auto clamped = [&](long t) { return t < a.T ? t : a.T - 1; };
     auto work = [&](const GradRow<X, Y, S, ROUTE> &r, long t, bool row_ok) {
         float mean = r.mean, rstd = r.rstd, s[2];
         if (!a.mean) {
@@ -110,13 +119,16 @@ __global__ __launch_bounds__(S::WIDE ? 512 : 64 * kGradWaves) void norm_grad_ker
             }
         if constexpr (ROUTE == kStreamed) {
             const float *dl = a.dlogits + (size_t)clamped(t) * a.n;
-#pragma unroll 1
+#pragma unroll 2
             for (int e = 0; e < a.n; ++e) {
-                const float *row = a.weights + e * a.by_expert;
+                const float *row = a.weights + (size_t)e * padded_columns(a.E);
 #pragma unroll
-                for (int c = 0; c < CH; ++c)
+                for (int c = 0; c < CH; ++c) {
+                    Piece<float, VEC> v;
+                    v.load(row + p.at[c]);
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) h[c][i] = __builtin_fmaf(dl[e], row[(size_t)(p.at[c] + i) * a.by_column], h[c][i]);
+                    for (int i = 0; i < VEC; ++i) h[c][i] = __builtin_fmaf(dl[e], v[i], h[c][i]);
+                }
             }
         }
 #pragma unroll
@@ -149,9 +161,6 @@ __global__ __launch_bounds__(S::WIDE ? 512 : 64 * kGradWaves) void norm_grad_ker
     };
     // Every step stores the same number of pieces: a wait for the next row then leaves the last row's stores in flight (loads and stores
     // are counted by one counter, in order).  Rows that are not there come in a last step of their own.
-    GradRow<X, Y, S, ROUTE> nxt;
-    long t0 = (long)blockIdx.x * groups;
-    if constexpr (AHEAD) nxt.load(a, p, clamped(t0 + g));
     for (; t0 + groups <= a.T; t0 += stride) {
         if constexpr (!AHEAD) nxt.load(a, p, t0 + g);
         const GradRow<X, Y, S, ROUTE> r = nxt;
@@ -179,22 +188,32 @@ __global__ __launch_bounds__(S::WIDE ? 512 : 64 * kGradWaves) void norm_grad_ker
     }
     // the workgroup's part: its groups' sums in ascending order
     float *part = a.partial + (size_t)blockIdx.x * (2 + n) * columns;
+    if (groups == 1) {
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
-        if (q >= 2 + n) continue;
-        if (groups == 1) {
+        for (int q = 0; q < Q; ++q) {
+            if (q >= 2 + n) continue;
 #pragma unroll
             for (int c = 0; c < CH; ++c) store_piece<float, VEC>(part + (size_t)q * columns + p.at[c], acc[q][c]);
-        } else {
-            const int width = p.lanes * CH * VEC;
+        }
+    } else {
+        const int width = p.lanes * CH * VEC;
+#pragma unroll
+        for (int q0 = 0; q0 < Q; q0 += BATCH) {
             __syncthreads();
 #pragma unroll
-            for (int c = 0; c < CH; ++c) store_piece<float, VEC>(side + g * width + p.at[c], acc[q][c]);
+            for (int q = q0; q < q0 + BATCH && q < Q; ++q)
+#pragma unroll
+                for (int c = 0; c < CH; ++c) store_piece<float, VEC>(side + (q - q0) * Plan::SIDE + g * width + p.at[c], acc[q][c]);
             __syncthreads();
-            for (int j = threadIdx.x; j < a.E; j += (int)blockDim.x) {
-                float s = side[j];
-                for (int k = 1; k < groups; ++k) s += side[k * width + j];
-                part[(size_t)q * columns + j] = s;
+            const int have = 2 + n - q0 < BATCH ? 2 + n - q0 : BATCH;
+            for (int k = threadIdx.x; k < have * columns; k += (int)blockDim.x) {
+                const int q = k / columns, j = k - q * columns;
+                if (j >= a.E) continue;
+                const float *from = side + q * Plan::SIDE + j;
+                float s = from[0];
+#pragma unroll 4
+                for (int r = 1; r < groups; ++r) s += from[r * width];
+                part[(size_t)(q0 + q) * columns + j] = s;
             }
         }
     }
@@ -227,20 +246,34 @@ __global__ __launch_bounds__(256) void norm_grad_router_kernel(NormGradArgs a, l
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[e][i] = 0.0f;
     }
+    constexpr int kRows = 64;            // whose statistics and gradients of logits are fetched at a time
+    __shared__ float mean[kRows], rstd[kRows], dl[kRows][kMaxExperts];
+    for (long r0 = t0; r0 < t1; r0 += kRows) {
+        const int count = (int)(t1 - r0 < kRows ? t1 - r0 : kRows);
+        __syncthreads();
+        for (int k = threadIdx.x; k < kRows * kMaxExperts; k += 256) {
+            const int r = k / kMaxExperts, e = k % kMaxExperts;
+            dl[r][e] = r < count && e < n ? a.dlogits[(size_t)(r0 + r) * n + e] : 0.0f;
+            if (e == 0) {
+                mean[r] = r < count ? a.mean[r0 + r] : 0.0f;
+                rstd[r] = r < count ? a.rstd[r0 + r] : 0.0f;
+            }
+        }
+        __syncthreads();
 #pragma unroll 4
-    for (long t = t0; t < t1; ++t) {
-        Piece<X, 4> x;
-        x.load(static_cast<const X *>(a.x) + (size_t)t * a.E + at);
-        const float mean = a.mean[t], rstd = a.rstd[t];
-        float xh[4];
+        for (int r = 0; r < count; ++r) {
+            Piece<X, 4> x;
+            x.load(static_cast<const X *>(a.x) + (size_t)(r0 + r) * a.E + at);
+            float xh[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) xh[i] = (x[i] - mean) * rstd;
+            for (int i = 0; i < 4; ++i) xh[i] = (x[i] - mean[r]) * rstd[r];
 #pragma unroll
-        for (int e = 0; e < kMaxExperts; ++e) {
-            const float dl = e < n ? a.dlogits[(size_t)t * n + e] : 0.0f;
-            dl_sum[e] += dl;
+            for (int e = 0; e < kMaxExperts; ++e) {
+                const float d = dl[r][e];
+                dl_sum[e] += d;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[e][i] = __builtin_fmaf(xh[i], dl, acc[e][i]);
+                for (int i = 0; i < 4; ++i) acc[e][i] = __builtin_fmaf(xh[i], d, acc[e][i]);
+            }
         }
     }
     float *out = a.partial + ((size_t)part * (2 + n) + 2) * columns + at;
@@ -263,11 +296,13 @@ int launch_norm_grad_rows(const NormGradArgs &a, int *parts, hipStream_t st) {
     constexpr int VEC = row_vec<X, Y>();
     auto rows = [&](auto shape, auto route) {
         using S = decltype(shape);
-        // 8 wavefronts to a CU, their registers: two workgroups, or one of a wide row's; the same number of steps in each
-        const int threads = S::threads(a.E, kGradWaves);
-        const long per_step = S::groups(a.E, kGradWaves) * (threads <= 64 * kGradWaves ? kMaxGradParts : kMaxGradParts / 2);
-        const long steps = (a.T + per_step - 1) / per_step, rows_of = steps * S::groups(a.E, kGradWaves);
-        *parts = (int)((a.T + rows_of - 1) / rows_of);
+        // the same number of steps in each
+        using Plan = GradPlan<X, Y, S, decltype(route)::value>;
+        int waves = Plan::WAVES;                             // fewer where rows are, down to 4: more CUs have some
+        while (waves > 4 && S::waves(a.E) < waves && (long)S::groups(a.E, waves) * kMaxGradParts >= 2 * a.T) waves /= 2;
+        const int threads = S::threads(a.E, waves);
+        const long groups = S::groups(a.E, waves), steps = (a.T + groups * kMaxGradParts - 1) / (groups * kMaxGradParts);
+        *parts = (int)((a.T + groups * steps - 1) / (groups * steps));
         if constexpr (decltype(route)::value == kStreamed) {
             if (a.dwg) {
                 // before dx, which may take the place of x
@@ -283,7 +318,7 @@ int launch_norm_grad_rows(const NormGradArgs &a, int *parts, hipStream_t st) {
     auto with = [&](auto route) { return [&rows, route](auto shape) { return rows(shape, route); }; };
     if (!a.dlogits) return by_shape<VEC>(a.E, with(std::integral_constant<int, 0>()));
     if (a.n == 2) return by_shape<VEC>(a.E, with(std::integral_constant<int, 2>()));
-    if (a.E > kMaxRoute8Columns) return by_wide_shape<VEC>(with(std::integral_constant<int, kStreamed>()));
+    if (a.E > kMaxRoute8Columns) return by_wide_shape<VEC>(a.E, with(std::integral_constant<int, kStreamed>()));
     return by_shape_route8<VEC>(a.E, with(std::integral_constant<int, kMaxExperts>()));
 }
 

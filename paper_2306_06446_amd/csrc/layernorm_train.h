@@ -8,7 +8,7 @@
 namespace sa {
 
 constexpr int kMaxNormColumns = 8192;
-constexpr int kMaxGradParts = 512;           // workgroups whose sums over rows are added up by a second launch
+constexpr int kMaxGradParts = 256;           // workgroups whose sums over rows are added up by a second launch
 
 struct NormArgs {
     const void *x;
@@ -33,9 +33,7 @@ struct NormGradArgs {
     const void *dres;        // or null
     const float *dlogits, *wg;       // null: no router
     int n;
-    const float *weights;    // kStreamed: of expert e, column j at weights[e * by_expert + j * by_column]
-    long by_expert;
-    int by_column;
+    const float *weights;    // kStreamed: wg as [n][columns, a multiple of 4]
     void *dx;
     float *partial;          // [parts][2 + n][columns, a multiple of 4]: dgamma, dbeta, dwg by expert; null: none wanted
     float *partial_dbg;      // [parts][kMaxExperts]
@@ -45,14 +43,28 @@ struct NormGradArgs {
 
 __host__ __device__ inline int padded_columns(int E) { return (E + 3) / 4 * 4; }
 
-// ROUTE: experts whose weights a kernel of the gradient holds in registers, with their sums (0, 2 or kMaxExperts), or
-// kStreamed: weights from memory row by row, sums elsewhere.
+inline int max_grad_parts(long T) { return (int)(T < kMaxGradParts ? T : kMaxGradParts); }
+
+// ROUTE: experts whose weights a kernel holds in registers, the gradient with their sums (0, 2 or kMaxExperts); kStreamed: the gradient
+// has the weights from memory row by row, and the sums come of a launch of their own.
 constexpr int kStreamed = 1;
 
 // The shape of a row of E elements.  Up to 16 elements to a lane (with a gradient's sums, as many registers as leave two wavefronts to a
 // SIMD), fewer lanes for narrow rows, so that a wavefront works on several; wider rows take several wavefronts.
+// Wide rows: 12 elements to a lane of 2, 4 or 8 wavefronts where that is enough, else 16.
+constexpr int kMaxRoute8Columns = 2048;
+template <class F>
+int by_elements(int E, F &&f) {              // of a lane of a row of more than 1024 elements
+    const bool few = E <= 1536 || (E > 2048 && E <= 3072) || (E > 4096 && E <= 6144);
+    return few ? f(std::integral_constant<int, 12>()) : f(std::integral_constant<int, 16>());
+}
 template <int VEC, class F>
-int by_wide_shape(F &&f) { return f(RowShape<VEC, 16 / VEC, kWide, 8 / VEC>()); }
+int by_wide_shape(int E, F &&f) {
+    return by_elements(E, [&](auto elements) {
+        if constexpr (decltype(elements)::value == 12) return f(RowShape<4, 3, kWide, 2>());
+        else return f(RowShape<VEC, 16 / VEC, kWide, 12 / VEC>());
+    });
+}
 template <int VEC, class F>
 int by_shape(int E, F &&f) {
     if (E < VEC) return f(RowShape<1, 1, 16, 0>());
@@ -64,14 +76,15 @@ int by_shape(int E, F &&f) {
         if (E <= 192 * VEC) return f(RowShape<VEC, 3, 64, 2>());
         if (E <= 256 * VEC) return f(RowShape<VEC, 4, 64, 3>());
     }
-    return by_wide_shape<VEC>(f);
+    return by_wide_shape<VEC>(E, f);
 }
-// With a router of up to 8 experts: 8 elements to a lane, whose 64 weights and 64 sums are registers too.  Wider rows would want more
-// of them than there are.
-constexpr int kMaxRoute8Columns = 2048;
+// The gradient with a router of up to 8 experts: 8 elements to a lane, whose 64 weights and 64 sums are registers too.  Wider rows would
+// want more of them than there are.
 template <int VEC, class F>
 int by_shape_route8(int E, F &&f) {
     if (E < VEC) return f(RowShape<1, 1, 16, 0>());
+    if (E <= 128) return f(RowShape<VEC, 8 / VEC, 16, 0>());
+    if (E <= 256) return f(RowShape<VEC, 8 / VEC, 32, 0>());
     if (E <= 512) return f(RowShape<VEC, 8 / VEC, 64, 0>());
     return f(RowShape<VEC, 8 / VEC, kWide, 0>());
 }
@@ -84,21 +97,43 @@ __device__ inline void load_columns(float (&out)[VEC], const float *p) {
 #pragma unroll
     for (int i = 0; i < VEC; ++i) out[i] = v[i];
 }
-template <int VEC, int N, int CH>
-__device__ inline void load_router(float (&out)[N][CH][VEC], int c, const float *p, int n) {
-    if constexpr (N == 2) {
-        Piece<float, 2 * VEC> v;
-        v.load(p);
+template <int VEC, int CH>
+__device__ inline void load_router_pair(float (&out)[2][CH][VEC], int c, const float *p) {
+    Piece<float, 2 * VEC> v;
+    v.load(p);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) out[0][c][i] = v[2 * i], out[1][c][i] = v[2 * i + 1];
-    } else {
+    for (int i = 0; i < VEC; ++i) out[0][c][i] = v[2 * i], out[1][c][i] = v[2 * i + 1];
+}
+// Of up to N experts, zeros behind the n there are: in tiles of columns through LDS (a lane's own weights are 4 n VEC bytes from the next
+// lane's in memory, a line to a lane and load: 12608 x 768 with eight experts took 75 us, 45 of them for this).  Tiles overlap by a
+// piece, so that one of them has the whole of it.
+constexpr int kRouterTile = 2048;
+constexpr int kRouterTileFloats = (kRouterTile * kMaxExperts) / 32 * 33 + 1;
+template <class S, int N>
+__device__ inline void load_router(float (&out)[N][S::CH][S::VEC], const RowPlace<S> &p, const float *wg, int E, int n, float *tile) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i)
+    for (int e = 0; e < N; ++e)
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float v = p[i * n + (e < n ? e : 0)];
-                out[e][c][i] = e < n ? v : 0.0f;
-            }
+        for (int c = 0; c < S::CH; ++c)
+#pragma unroll
+            for (int i = 0; i < S::VEC; ++i) out[e][c][i] = 0.0f;
+    for (int j0 = 0; j0 < E; j0 += kRouterTile - S::VEC) {
+        const int columns = E - j0 < kRouterTile ? E - j0 : kRouterTile;
+        __syncthreads();
+        for (int k = threadIdx.x; k < columns * n; k += (int)blockDim.x) tile[k + k / 32] = wg[(size_t)j0 * n + k];
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < S::CH; ++c) {
+            const int at = p.at[c] - j0;
+            if (at < 0 || at + S::VEC > columns) continue;
+#pragma unroll
+            for (int i = 0; i < S::VEC; ++i)
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const int k = (at + i) * n + e;
+                    if (e < n) out[e][c][i] = tile[k + k / 32];
+                }
+        }
     }
 }
 

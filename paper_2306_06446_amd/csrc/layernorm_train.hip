@@ -11,33 +11,37 @@ namespace sa {
 constexpr int kNormWaves = 4;                // of a workgroup of rows of one wavefront or less
 template <class X, class Y, class S, int ROUTE, bool TRAIN>
 __global__ __launch_bounds__(S::WIDE ? 512 : 64 * kNormWaves) void train_norm_kernel(NormArgs a) {
-    constexpr int VEC = S::VEC, CH = S::CH, HELD = ROUTE > kStreamed ? ROUTE : 0, PR = HELD ? HELD : 1, PC = HELD ? CH : 1;
-    __shared__ float red[S::WIDE ? PR : 1][2][8];
+    constexpr int VEC = S::VEC, CH = S::CH, HELD = ROUTE, PR = HELD ? HELD : 1, PC = HELD ? CH : 1;
+    __shared__ float red[S::WIDE ? PR : 1][2][8], tile[HELD == kMaxExperts ? kRouterTileFloats : 1];
     const RowPlace<S> p(a.E);
     const int g = p.g, l = p.l, groups = S::WIDE ? p.groups : 64 * kNormWaves / S::LANES;
     const float per = 1.0f / (float)a.E;
     RowSums<S, PR> sum(red, p);
-    float gm[CH][VEC], bt[CH][VEC], w[PR][PC][VEC], bias[PR];
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        load_columns<VEC>(gm[c], a.gamma + p.at[c]);
-        load_columns<VEC>(bt[c], a.beta + p.at[c]);
-        if constexpr (HELD > 0) {
-            load_router<VEC, HELD, PC>(w, c, a.wg + (size_t)p.at[c] * a.n, a.n);
-#pragma unroll
-            for (int e = 0; e < HELD; ++e)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) w[e][c][i] = p.own(c, i, w[e][c][i]);
-        }
-    }
-#pragma unroll
-    for (int e = 0; e < HELD; ++e) bias[e] = a.bg[HELD == 2 || e < a.n ? e : 0];
     const long stride = (long)gridDim.x * groups;
     auto load = [&](Piece<X, VEC> (&x)[CH], long t) {
         const X *row = static_cast<const X *>(a.x) + (size_t)(t < a.T ? t : a.T - 1) * a.E;
 #pragma unroll
         for (int c = 0; c < CH; ++c) x[c].load(row + p.at[c]);
     };
+    Piece<X, VEC> nxt[CH], x[CH];
+    long t0 = (long)blockIdx.x * groups;
+    load(nxt, t0 + g);
+    float gm[CH][VEC], bt[CH][VEC], w[PR][PC][VEC], bias[PR];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        load_columns<VEC>(gm[c], a.gamma + p.at[c]);
+        load_columns<VEC>(bt[c], a.beta + p.at[c]);
+        if constexpr (HELD == 2) load_router_pair<VEC, PC>(w, c, a.wg + 2 * (size_t)p.at[c]);
+    }
+    if constexpr (HELD == kMaxExperts) load_router<S, PR>(w, p, a.wg, a.E, a.n, tile);
+#pragma unroll
+    for (int e = 0; e < HELD; ++e)
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) w[e][c][i] = p.own(c, i, w[e][c][i]);
+#pragma unroll
+    for (int e = 0; e < HELD; ++e) bias[e] = a.bg[HELD == 2 || e < a.n ? e : 0];
     // What there is one of to a row is kept, a step to a lane, and leaves for PERIOD rows at a time: every step then stores the same
     // number of pieces, and a wait for the next row leaves the last row's stores in flight (one counter, in order).
     float kept_mean = 0.0f, kept_rstd = 0.0f, kept[PR];
@@ -91,27 +95,12 @@ __global__ __launch_bounds__(S::WIDE ? 512 : 64 * kNormWaves) void train_norm_ke
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) part[e] = __builtin_fmaf(y[c][i], w[e][c][i], part[e]);
             }
-            sum(part, HELD == 2 ? 2 : a.n);
+            sum(part);
 #pragma unroll
             for (int e = 0; e < HELD; ++e) kept[e] = keep ? part[e] + bias[e] : kept[e];
         }
-        if constexpr (ROUTE == kStreamed) {
-#pragma unroll 1
-            for (int e = 0; e < a.n; ++e) {
-                s[0] = 0.0f;
-#pragma unroll
-                for (int c = 0; c < CH; ++c)
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i)
-                        s[0] = __builtin_fmaf(p.own(c, i, y[c][i]), a.wg[(size_t)(p.at[c] + i) * a.n + e], s[0]);
-                sum(s);
-                if (l == 0 && row_ok) a.logits[(size_t)t * a.n + e] = s[0] + a.bg[e];
-            }
-        }
     };
-    Piece<X, VEC> nxt[CH], x[CH];
-    long t0 = (long)blockIdx.x * groups, step = 0;
-    load(nxt, t0 + g);
+    long step = 0;
     for (; t0 + groups <= a.T; t0 += stride) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) x[c] = nxt[c];
@@ -132,9 +121,11 @@ int launch_norm_rows(const NormArgs &a, hipStream_t st) {
     constexpr int VEC = row_vec<X, Y>();
     auto rows = [&](auto shape, auto route) {
         using S = decltype(shape);
-        // 16 wavefronts to a CU (their registers), each with as many rows as it takes
+        // 16 wavefronts to a CU (as many as there is room for), 32 where several wait for each other at every row, 8 with the weights of
+        // many experts, each with as many rows as it takes
         const int threads = S::threads(a.E, kNormWaves);
-        const long groups = S::groups(a.E, kNormWaves), steps = (a.T + groups - 1) / groups, cap = 256 * 1024 / threads;
+        const long groups = S::groups(a.E, kNormWaves), steps = (a.T + groups - 1) / groups;
+        const long cap = 256 * (decltype(route)::value == kMaxExperts ? 512 : S::WIDE ? 2048 : 1024) / threads;
         const dim3 grid((unsigned)(steps < cap ? steps : cap)), block((unsigned)threads);
         if (a.y && a.mean && a.rstd)
             train_norm_kernel<X, Y, S, decltype(route)::value, true><<<grid, block, 0, st>>>(a);
@@ -145,8 +136,7 @@ int launch_norm_rows(const NormArgs &a, hipStream_t st) {
     auto with = [&](auto route) { return [&rows, route](auto shape) { return rows(shape, route); }; };
     if (!a.logits) return by_shape<VEC>(a.E, with(std::integral_constant<int, 0>()));
     if (a.n == 2) return by_shape<VEC>(a.E, with(std::integral_constant<int, 2>()));
-    if (a.E > kMaxRoute8Columns) return by_wide_shape<VEC>(with(std::integral_constant<int, kStreamed>()));
-    return by_shape_route8<VEC>(a.E, with(std::integral_constant<int, kMaxExperts>()));
+    return by_shape<VEC>(a.E, with(std::integral_constant<int, kMaxExperts>()));
 }
 
 }  // namespace sa
@@ -155,7 +145,7 @@ namespace {
 
 using namespace sa;
 
-// The parts' sums in fp64, in a fixed order: 64 threads to four columns, whose loads (8 to a thread at most) are all in flight at once.
+// The parts' sums in fp64, in a fixed order: 64 threads to four columns, whose loads (4 to a thread at most) are all in flight at once.
 constexpr int kSumColumns = 16;              // of a workgroup
 __global__ __launch_bounds__(256) void norm_grad_sum_kernel(NormGradArgs a, int parts) {
     constexpr int kSlices = 256 / (kSumColumns / 4);
@@ -208,17 +198,18 @@ struct GradLayout {
     size_t partial, dbg, weights, mean, rstd, total;
 };
 
-GradLayout grad_layout(long T, int E, int n) {
+bool needs_weights(int E, int n) { return n > 2 && E > kMaxRoute8Columns; }
+GradLayout grad_layout(long T, int E, int n, bool params) {
     GradLayout L;
     auto up = [](size_t bytes) { return (bytes + 255) / 256 * 256; };
-    const size_t parts = (size_t)(T < kMaxGradParts ? T : kMaxGradParts), columns = (size_t)padded_columns(E);
-    const bool streamed = n > 2 && E > kMaxRoute8Columns;
+    const size_t parts = params ? (size_t)max_grad_parts(T) : 0, columns = (size_t)padded_columns(E);
+    const bool streamed = needs_weights(E, n);
     L.partial = 0;
     L.dbg = up(parts * (2 + n) * columns * 4);
     L.weights = L.dbg + up(n ? parts * kMaxExperts * 4 : 0);
     L.mean = L.weights + up(streamed ? n * columns * 4 : 0);
-    L.rstd = L.mean + up(streamed ? (size_t)T * 4 : 0);
-    L.total = L.rstd + up(streamed ? (size_t)T * 4 : 0);
+    L.rstd = L.mean + up(streamed && params ? (size_t)T * 4 : 0);
+    L.total = L.rstd + up(streamed && params ? (size_t)T * 4 : 0);
     return L;
 }
 
@@ -231,26 +222,25 @@ template <class X, class Y>
 struct RunNormGrad {
     static int run(NormGradArgs &a, uint8_t *ws, hipStream_t st) {
         const int n = a.dlogits ? a.n : 0;
-        const bool streamed = n > 2 && a.E > kMaxRoute8Columns;
-        a.weights = a.wg, a.by_expert = 1, a.by_column = n;
+        const bool streamed = needs_weights(a.E, n);
+        const GradLayout L = grad_layout(a.T, a.E, n, a.dgamma != nullptr);
         if (a.dgamma) {
-            const GradLayout L = grad_layout(a.T, a.E, n);
             a.partial = reinterpret_cast<float *>(ws + L.partial);
             a.partial_dbg = reinterpret_cast<float *>(ws + L.dbg);
-            if (streamed) {
-                float *rows = reinterpret_cast<float *>(ws + L.weights);
-                router_rows_kernel<<<dim3((unsigned)((a.E * n + 255) / 256)), dim3(256), 0, st>>>(a.wg, a.E, n, rows);
-                int rc = check_launch("sa_layernorm_backward(router's rows)");
+        }
+        if (streamed) {
+            float *rows = reinterpret_cast<float *>(ws + L.weights);
+            router_rows_kernel<<<dim3((unsigned)((a.E * n + 255) / 256)), dim3(256), 0, st>>>(a.wg, a.E, n, rows);
+            int rc = check_launch("sa_layernorm_backward(router's rows)");
+            if (rc != SA_OK) return rc;
+            a.weights = rows;
+            if (!a.mean && a.dwg) {
+                NormArgs f{};
+                f.x = a.x, f.T = a.T, f.E = a.E, f.eps = a.eps, f.gamma = a.gamma, f.beta = a.gamma;
+                f.mean = reinterpret_cast<float *>(ws + L.mean), f.rstd = reinterpret_cast<float *>(ws + L.rstd);
+                rc = launch_norm_rows<X, Y>(f, st);
                 if (rc != SA_OK) return rc;
-                a.weights = rows, a.by_expert = padded_columns(a.E), a.by_column = 1;
-                if (!a.mean && a.dwg) {
-                    NormArgs f{};
-                    f.x = a.x, f.T = a.T, f.E = a.E, f.eps = a.eps, f.gamma = a.gamma, f.beta = a.gamma;
-                    f.mean = reinterpret_cast<float *>(ws + L.mean), f.rstd = reinterpret_cast<float *>(ws + L.rstd);
-                    rc = launch_norm_rows<X, Y>(f, st);
-                    if (rc != SA_OK) return rc;
-                    a.mean = f.mean, a.rstd = f.rstd;
-                }
+                a.mean = f.mean, a.rstd = f.rstd;
             }
         }
         int parts = 0;
@@ -295,7 +285,7 @@ extern "C" int sa_layernorm(const void *x, int x_type, long T, int E, const floa
 extern "C" size_t sa_layernorm_backward_workspace_bytes(long T, int E, int n_experts) {
     if (T <= 0 || E <= 0 || E > kMaxNormColumns || T >= (1L << 31)) return 0;
     if (n_experts != 0 && (n_experts < 2 || n_experts > sa::kMaxExperts)) return 0;
-    return grad_layout(T, E, n_experts).total;
+    return grad_layout(T, E, n_experts, true).total;
 }
 
 extern "C" int sa_layernorm_backward(const void *dy, int y_type, const void *x, int x_type, long T, int E, const float *gamma,
@@ -331,8 +321,8 @@ extern "C" int sa_layernorm_backward(const void *dy, int y_type, const void *x, 
     SA_REQUIRE(dy && x && gamma && dx, SA_ERR_INVALID, "sa_layernorm_backward: NULL buffer");
     SA_REQUIRE(!route || wg_or_null, SA_ERR_INVALID, "sa_layernorm_backward: dlogits need wg");
     SA_REQUIRE(!dwg_or_null || beta_or_null, SA_ERR_INVALID, "sa_layernorm_backward: dwg needs beta");
-    if (params) {
-        const size_t need = sa_layernorm_backward_workspace_bytes(T, E, route ? n_experts : 0);
+    const size_t need = grad_layout(T, E, route ? n_experts : 0, params).total;
+    if (need > 0) {
         SA_REQUIRE(workspace != nullptr && workspace_bytes >= need, SA_ERR_WORKSPACE,
                    "sa_layernorm_backward: workspace of %zu bytes needed, %zu given", need, workspace_bytes);
     }

@@ -53,14 +53,15 @@ constexpr int row_vec() { return sizeof(X) == 2 && sizeof(Y) == 2 ? 8 : 4; }
 // would reach past the row's end (the last one of a row that VEC does not divide, and those behind it) begins VEC before the end
 // instead: no load or store needs a choice, elements that two lanes hold are computed and written by both, the same bits.  Only sums
 // over the row ask whether an element is a lane's own.  The first FULL pieces of a lane are whole in every row that comes here.
-// LANES is 16, 32 or 64, rows side by side in a wavefront, or kWide: the lanes of 2 to 8 wavefronts, as many as the row takes.
+// LANES is 16, 32 or 64, rows side by side in a wavefront, or kWide: the lanes of 2, 4 or 8 wavefronts, as many as the row takes.  (Of 3, 5, 6
+// or 7 the SIMDs of a CU get unequal shares, and all wait for the largest: 43859 x 4560 fp16 on 5 wavefronts 209 us, on 8 165.)
 constexpr int kWide = 512;
 template <int VEC_, int CH_, int LANES_, int FULL_>
 struct RowShape {
     static constexpr int VEC = VEC_, CH = CH_, LANES = LANES_, FULL = FULL_;
     static constexpr bool WIDE = LANES > 64;
     static constexpr int PERIOD = WIDE ? 64 : LANES;         // rows whose statistics the lanes of one wavefront can keep
-    static int waves(int E) { return WIDE ? (E + 64 * VEC * CH - 1) / (64 * VEC * CH) : 1; }
+    static __host__ __device__ inline int waves(int E) { return !WIDE ? 1 : E <= 128 * VEC * CH ? 2 : E <= 256 * VEC * CH ? 4 : 8; }
     // rows side by side in a workgroup of up to max_waves wavefronts
     static int groups(int E, int max_waves) { return WIDE ? (waves(E) < max_waves ? max_waves / waves(E) : 1) : max_waves * 64 / LANES; }
     static int threads(int E, int max_waves) { return WIDE ? 64 * waves(E) * groups(E, max_waves) : 64 * max_waves; }
@@ -71,7 +72,7 @@ struct RowPlace {
     int g, l, lanes, groups;             // this lane's row among the workgroup's, and its place in it
     int at[S::CH], skip[S::CH];
     __device__ inline RowPlace(int E) {
-        const int waves = S::WIDE ? __builtin_amdgcn_readfirstlane((E + 64 * S::VEC * S::CH - 1) / (64 * S::VEC * S::CH)) : 1;
+        const int waves = S::waves(E);
         lanes = S::WIDE ? 64 * waves : S::LANES;
         groups = S::WIDE ? (int)(blockDim.x >> 6) / waves : (int)blockDim.x / S::LANES;
         g = S::WIDE ? __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6) / waves) : (int)threadIdx.x / S::LANES;

@@ -115,9 +115,9 @@ def test_a_row_that_is_not_finite_stays_alone(sa, E):
     assert torch.equal(dx[rest], grad[0][rest]) and bool(dx[[7, 11]].isnan().all())
 
 
-@pytest.mark.parametrize("E", [60, 1001, 4096])
-def test_outputs_on_request_and_the_same_bits_again(sa, E):
-    s = inputs(70, E, F32, F16, 2, 4)
+@pytest.mark.parametrize("E,n", [(60, 2), (1001, 2), (4096, 2), (100, 5), (1500, 8), (2500, 3), (8190, 8)])
+def test_outputs_on_request_and_the_same_bits_again(sa, E, n):
+    s = inputs(70, E, F32, F16, n, 4)
     y, mean, rstd, logits = sa.sa_layernorm(s["x"], s["gamma"], s["beta"], EPS, y_dtype=F16, wg=s["wg"], bg=s["bg"])
     again = sa.sa_layernorm(s["x"], s["gamma"], s["beta"], EPS, y_dtype=F16, want_stats=False)
     assert torch.equal(again[0], y) and again[1:] == (None, None, None)

@@ -67,6 +67,9 @@ def test_layernorm_backward(lib):
     need = lib.sa_layernorm_backward_workspace_bytes(10, 65, 3)
     assert need > 0 and call(bytes=need - 1) == WORKSPACE and call(workspace=None) == WORKSPACE and call(bytes=need) == HIP
     assert lib.sa_last_error() != b""
+    # a frozen norm of wide rows behind a router of many experts has its weights in another order in the workspace
+    assert call(**{**frozen, "E": 2049}) == WORKSPACE and call(**{**frozen, "E": 2048}) == HIP and call(**{**frozen, "E": 2049, "n": 2}) == HIP
+    assert call(**{**frozen, "E": 2049, "workspace": FAKE, "bytes": 4 * 2052 * 3 + 256}) == HIP
     for sizes in ((0, 64, 0), (-1, 64, 0), (10, 0, 0), (10, 8193, 0), (10, 64, 1), (10, 64, 9), (1 << 31, 64, 0)):
         assert lib.sa_layernorm_backward_workspace_bytes(*sizes) == 0, sizes
     assert call(T=0, accumulate=1) == OK and call(T=0) == HIP        # sums over no rows are zeros, which a launch has to write
