@@ -43,22 +43,25 @@ struct GradPlan {
     static constexpr int ROW = ELEMS * (2 * sizeof(X) + sizeof(Y)) / 4;
     static constexpr int REGISTERS = ELEMS * (2 + HELD + 1 + HELD + 2) + 2 * ROW + 48;
     static constexpr bool AHEAD = REGISTERS < 256;
-    // A workgroup to a CU, of the wavefronts that its registers have room for: the fewest parts that keep it busy.
-    static constexpr int WAVES = !S::WIDE && REGISTERS <= 136 ? 16 : 8;
+    // A workgroup to a CU, of the wavefronts that its registers have room for: the fewest parts that keep it busy.  Wavefronts that share
+    // rows wait for each other at every row: there in workgroups of four, or a row's, of which a CU has two (25000 x 4000 fp16
+    // 129 -> 122 us).
+    static constexpr int WAVES = S::WIDE ? 4 : REGISTERS <= 136 ? 16 : 8;
+    static constexpr int MOST = S::WIDE ? 8 : WAVES;         // of a workgroup
     static constexpr int SIDE = 64 * WAVES * ELEMS;          // a value to each of its elements, in LDS
     static constexpr int AT_ONCE = SIDE <= 8192 ? 4 : 2;
 };
 
 template <class X, class Y, class S, int ROUTE>
-__global__ __launch_bounds__((64 * GradPlan<X, Y, S, ROUTE>::WAVES)) void norm_grad_kernel(NormGradArgs a) {
+__global__ __launch_bounds__((64 * GradPlan<X, Y, S, ROUTE>::MOST)) void norm_grad_kernel(NormGradArgs a) {
     using Plan = GradPlan<X, Y, S, ROUTE>;
     constexpr int VEC = S::VEC, CH = S::CH, HELD = Plan::HELD, Q = 2 + HELD;
     constexpr bool AHEAD = Plan::AHEAD;
     constexpr int PC = HELD ? CH : 1, PR = HELD ? HELD : 1;
-    __shared__ float red[S::WIDE ? 2 : 1][2][8];
+    __shared__ __align__(16) float red[S::WIDE ? 2 : 1][2][8];
     constexpr int BATCH = Q < Plan::AT_ONCE ? Q : Plan::AT_ONCE;
     constexpr int SIDE = HELD == kMaxExperts && kRouterTileFloats > BATCH * Plan::SIDE ? kRouterTileFloats : BATCH * Plan::SIDE;
-    __shared__ float side[SIDE], side_dl[64 * Plan::WAVES / S::PERIOD][PR];
+    __shared__ float side[SIDE], side_dl[64 * Plan::MOST / S::PERIOD][PR];
     const RowPlace<S> p(a.E);
     const int g = p.g, groups = p.groups;
     const float per = 1.0f / (float)a.E;
@@ -67,7 +70,6 @@ __global__ __launch_bounds__((64 * GradPlan<X, Y, S, ROUTE>::WAVES)) void norm_g
     auto clamped = [&](long t) { return t < a.T ? t : a.T - 1; };
     GradRow<X, Y, S, ROUTE> nxt;
     long t0 = (long)blockIdx.x * groups;
-    if constexpr (AHEAD) nxt.load(a, p, clamped(t0 + g));
     float gm[CH][VEC], w[PR][PC][VEC];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -161,6 +163,7 @@ __global__ __launch_bounds__((64 * GradPlan<X, Y, S, ROUTE>::WAVES)) void norm_g
     };
     // Every step stores the same number of pieces: a wait for the next row then leaves the last row's stores in flight (loads and stores
     // are counted by one counter, in order).  Rows that are not there come in a last step of their own.
+    if constexpr (AHEAD) nxt.load(a, p, clamped(t0 + g));
     for (; t0 + groups <= a.T; t0 += stride) {
         if constexpr (!AHEAD) nxt.load(a, p, t0 + g);
         const GradRow<X, Y, S, ROUTE> r = nxt;
@@ -296,12 +299,13 @@ int launch_norm_grad_rows(const NormGradArgs &a, int *parts, hipStream_t st) {
     constexpr int VEC = row_vec<X, Y>();
     auto rows = [&](auto shape, auto route) {
         using S = decltype(shape);
-        // the same number of steps in each
         using Plan = GradPlan<X, Y, S, decltype(route)::value>;
         int waves = Plan::WAVES;                             // fewer where rows are, down to 4: more CUs have some
-        while (waves > 4 && S::waves(a.E) < waves && (long)S::groups(a.E, waves) * kMaxGradParts >= 2 * a.T) waves /= 2;
+        while (waves > 4 && (long)S::groups(a.E, waves) * 256 >= 2 * a.T) waves /= 2;
         const int threads = S::threads(a.E, waves);
-        const long groups = S::groups(a.E, waves), steps = (a.T + groups * kMaxGradParts - 1) / (groups * kMaxGradParts);
+        // two parts to a CU of workgroups of four, but 16 rows to a part or one to a CU; the same number of steps in each
+        const long cap = !S::WIDE || threads > 256 || a.T < 256 * 16 ? 256 : a.T >= 512 * 16 ? 512 : a.T / 16;
+        const long groups = S::groups(a.E, waves), steps = (a.T + groups * cap - 1) / (groups * cap);
         *parts = (int)((a.T + groups * steps - 1) / (groups * steps));
         if constexpr (decltype(route)::value == kStreamed) {
             if (a.dwg) {
@@ -316,9 +320,9 @@ int launch_norm_grad_rows(const NormGradArgs &a, int *parts, hipStream_t st) {
         return check_launch("sa_layernorm_backward(rows)");
     };
     auto with = [&](auto route) { return [&rows, route](auto shape) { return rows(shape, route); }; };
-    if (!a.dlogits) return by_shape<VEC>(a.E, with(std::integral_constant<int, 0>()));
-    if (a.n == 2) return by_shape<VEC>(a.E, with(std::integral_constant<int, 2>()));
-    if (a.E > kMaxRoute8Columns) return by_wide_shape<VEC>(a.E, with(std::integral_constant<int, kStreamed>()));
+    if (!a.dlogits) return by_shape<VEC, VEC == 4>(a.E, with(std::integral_constant<int, 0>()));
+    if (a.n == 2) return by_shape<VEC, VEC == 4>(a.E, with(std::integral_constant<int, 2>()));
+    if (a.E > kMaxRoute8Columns) return by_wide_shape<VEC, VEC == 4>(a.E, with(std::integral_constant<int, kStreamed>()));
     return by_shape_route8<VEC>(a.E, with(std::integral_constant<int, kMaxExperts>()));
 }
 

@@ -8,7 +8,7 @@
 namespace sa {
 
 constexpr int kMaxNormColumns = 8192;
-constexpr int kMaxGradParts = 256;           // workgroups whose sums over rows are added up by a second launch
+constexpr int kMaxGradParts = 512;           // workgroups whose sums over rows are added up by a second launch
 
 struct NormArgs {
     const void *x;
@@ -51,21 +51,15 @@ constexpr int kStreamed = 1;
 
 // The shape of a row of E elements.  Up to 16 elements to a lane (with a gradient's sums, as many registers as leave two wavefronts to a
 // SIMD), fewer lanes for narrow rows, so that a wavefront works on several; wider rows take several wavefronts.
-// Wide rows: 12 elements to a lane of 2, 4 or 8 wavefronts where that is enough, else 16.
+// Wide rows: 12 elements to a lane of 2, 4 or 8 wavefronts where that is enough (FEW), else 16.
 constexpr int kMaxRoute8Columns = 2048;
-template <class F>
-int by_elements(int E, F &&f) {              // of a lane of a row of more than 1024 elements
-    const bool few = E <= 1536 || (E > 2048 && E <= 3072) || (E > 4096 && E <= 6144);
-    return few ? f(std::integral_constant<int, 12>()) : f(std::integral_constant<int, 16>());
-}
-template <int VEC, class F>
+template <int VEC, bool FEW, class F>
 int by_wide_shape(int E, F &&f) {
-    return by_elements(E, [&](auto elements) {
-        if constexpr (decltype(elements)::value == 12) return f(RowShape<4, 3, kWide, 2>());
-        else return f(RowShape<VEC, 16 / VEC, kWide, 12 / VEC>());
-    });
+    if constexpr (FEW)
+        if (E <= 1536 || (E > 2048 && E <= 3072) || (E > 4096 && E <= 6144)) return f(RowShape<4, 3, kWide, 2>());
+    return f(RowShape<VEC, 16 / VEC, kWide, FEW ? 12 / VEC : 8 / VEC>());
 }
-template <int VEC, class F>
+template <int VEC, bool FEW, class F>
 int by_shape(int E, F &&f) {
     if (E < VEC) return f(RowShape<1, 1, 16, 0>());
     if (E <= 16 * VEC) return f(RowShape<VEC, 1, 16, 0>());
@@ -76,7 +70,7 @@ int by_shape(int E, F &&f) {
         if (E <= 192 * VEC) return f(RowShape<VEC, 3, 64, 2>());
         if (E <= 256 * VEC) return f(RowShape<VEC, 4, 64, 3>());
     }
-    return by_wide_shape<VEC>(E, f);
+    return by_wide_shape<VEC, FEW>(E, f);
 }
 // The gradient with a router of up to 8 experts: 8 elements to a lane, whose 64 weights and 64 sums are registers too.  Wider rows would
 // want more of them than there are.

@@ -12,7 +12,7 @@ constexpr int kNormWaves = 4;                // of a workgroup of rows of one wa
 template <class X, class Y, class S, int ROUTE, bool TRAIN>
 __global__ __launch_bounds__(S::WIDE ? 512 : 64 * kNormWaves) void train_norm_kernel(NormArgs a) {
     constexpr int VEC = S::VEC, CH = S::CH, HELD = ROUTE, PR = HELD ? HELD : 1, PC = HELD ? CH : 1;
-    __shared__ float red[S::WIDE ? PR : 1][2][8], tile[HELD == kMaxExperts ? kRouterTileFloats : 1];
+    __shared__ __align__(16) float red[S::WIDE ? PR : 1][2][8], tile[HELD == kMaxExperts ? kRouterTileFloats : 1];
     const RowPlace<S> p(a.E);
     const int g = p.g, l = p.l, groups = S::WIDE ? p.groups : 64 * kNormWaves / S::LANES;
     const float per = 1.0f / (float)a.E;
@@ -134,9 +134,9 @@ int launch_norm_rows(const NormArgs &a, hipStream_t st) {
         return check_launch("sa_layernorm");
     };
     auto with = [&](auto route) { return [&rows, route](auto shape) { return rows(shape, route); }; };
-    if (!a.logits) return by_shape<VEC>(a.E, with(std::integral_constant<int, 0>()));
-    if (a.n == 2) return by_shape<VEC>(a.E, with(std::integral_constant<int, 2>()));
-    return by_shape<VEC>(a.E, with(std::integral_constant<int, kMaxExperts>()));
+    if (!a.logits) return by_shape<VEC, true>(a.E, with(std::integral_constant<int, 0>()));
+    if (a.n == 2) return by_shape<VEC, true>(a.E, with(std::integral_constant<int, 2>()));
+    return by_shape<VEC, true>(a.E, with(std::integral_constant<int, kMaxExperts>()));
 }
 
 }  // namespace sa
@@ -145,7 +145,7 @@ namespace {
 
 using namespace sa;
 
-// The parts' sums in fp64, in a fixed order: 64 threads to four columns, whose loads (4 to a thread at most) are all in flight at once.
+// The parts' sums in fp64, in a fixed order: 64 threads to four columns, whose loads (8 to a thread at most) are all in flight at once.
 constexpr int kSumColumns = 16;              // of a workgroup
 __global__ __launch_bounds__(256) void norm_grad_sum_kernel(NormGradArgs a, int parts) {
     constexpr int kSlices = 256 / (kSumColumns / 4);

@@ -111,9 +111,17 @@ struct RowSums {
 #pragma unroll
             for (int k = 0; k < M; ++k) {
                 if (k >= used) continue;
-                float s = 0.0f;
-                for (int w = 0; w < waves; ++w) s += red[k][turn][first + w];
-                v[k] = s;
+                const float *from = red[k][turn] + first;        // 2, 4 or 8, in loads as wide as that
+                if (waves == 2) {
+                    v[k] = from[0] + from[1];
+                } else {
+                    const float4 a = *reinterpret_cast<const float4 *>(from);
+                    v[k] = (a.x + a.y) + (a.z + a.w);
+                    if (waves == 8) {
+                        const float4 b = *reinterpret_cast<const float4 *>(from + 4);
+                        v[k] += (b.x + b.y) + (b.z + b.w);
+                    }
+                }
             }
             turn ^= 1;
         }
