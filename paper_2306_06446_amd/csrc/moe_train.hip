@@ -16,6 +16,17 @@ using namespace sa;
 
 constexpr int kMaxE = kMaxExperts;
 
+// exp(x), x <= 0, off by 2 units at most down to the smallest normal number, 0 below it and for -infinity (what a softmax loses by that is
+// 1e-38), NaN for NaN: 2^t of the rounded product t = x / ln 2, and the product's rounding to first order.  Half of expf's instructions.
+__device__ inline float exp_of(float x) {
+    x = x < -104.0f ? -104.0f : x;
+    const float t = x * 1.44269504f, r = __builtin_fmaf(x, 1.92596303e-8f, __builtin_fmaf(x, 1.44269504f, -t));
+    const float e = __builtin_amdgcn_exp2f(t);
+    return __builtin_fmaf(e * 0.693147181f, r, e);
+}
+// exp(-x^2), off by 2^-24 at most: the product's rounding counts for nothing where the result is small.
+__device__ inline float exp_minus_square(float x) { return __builtin_amdgcn_exp2f(x * x * -1.44269504f); }
+
 // A token's routing: p, and for each expert the normal deviate of its distance to the best of the others.
 template <int E>
 struct TokenRouting {
@@ -38,29 +49,18 @@ __device__ inline TokenRouting<E> route_token(const float (&v)[E], float inv_noi
         l0 = best ? v[e] : l0;
     }
     float den = 0.0f;
-    if constexpr (E == 2) {
-        // the larger one's exponential is 1
-        const float x = expf(l1 - l0);
-        r.p[0] = r.first == 0 ? 1.0f : x;
-        r.p[1] = r.first == 0 ? x : 1.0f;
-        den = 1.0f + x;
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            r.p[e] = expf(v[e] - l0);
-            den += r.p[e];
-        }
-    }
-    const float inv = 1.0f / den;
-    float p0 = 0.0f, p1 = 0.0f;
+    const float x1 = exp_of(l1 - l0);    // the largest one's exponential is 1
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        r.p[e] *= inv;
-        p0 = e == r.first ? r.p[e] : p0;
-        p1 = e == r.second ? r.p[e] : p1;
+        r.p[e] = E == 2 ? (e == r.first ? 1.0f : x1) : exp_of(v[e] - l0);
+        den += r.p[e];
     }
+    const float p0 = __builtin_amdgcn_rcpf(den), p1 = x1 * p0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) r.z[e] = (r.p[e] - (e == r.first ? p1 : p0)) * inv_noise_std;
+    for (int e = 0; e < E; ++e) {
+        r.p[e] *= p0;
+        r.z[e] = (r.p[e] - (e == r.first ? p1 : p0)) * inv_noise_std;
+    }
     return r;
 }
 
@@ -77,7 +77,7 @@ __device__ inline float normal_tail(float z) {
     p = __builtin_fmaf(p, t, 0.194600117f);
     p = __builtin_fmaf(p, t, 0.151046025f);
     p = __builtin_fmaf(p, t, -3.25356018e-05f);
-    return expf(-x * x) * p;
+    return exp_minus_square(x) * p;
 }
 
 struct BalanceArgs {
@@ -85,7 +85,7 @@ struct BalanceArgs {
     long T;
     const uint8_t *valid;
     const float *alpha;
-    float noise_std;
+    float inv_noise_std, peak;           // 1 / std, 1 / (sqrt(2 pi) std)
     const float *dlosses;
     float *losses, *sums;
     int32_t *counts;
@@ -186,17 +186,24 @@ struct GroupSums {
     }
 };
 
-// A token as it is asked for: what of its logits and its place in the batch can be had before anything is known of the others.
+// A token as it is asked for: what of its logits and its place in the batch can be had before anything is known of the others.  No load
+// waits for another one's outcome: tokens that are not there read the first one's.
 template <int E>
 struct Token {
-    float l[E];
+    float l[E], old[E];                  // old: what the gradient is added to
     bool valid;
-    __device__ inline void load(const BalanceArgs &a, long t) {
+    __device__ inline void load(const BalanceArgs &a, long t, bool accumulate) {
         const bool there = t < a.T;
         const size_t at = there ? (size_t)t : 0;
-        valid = there && (!a.valid || a.valid[at] != 0);
+        const uint8_t *mask = a.valid ? a.valid : reinterpret_cast<const uint8_t *>(a.logits);
+        const uint8_t v = mask[at];
 #pragma unroll
-        for (int e = 0; e < E; ++e) l[e] = a.T > 0 ? a.logits[at * E + e] : 0.0f;
+        for (int e = 0; e < E; ++e) l[e] = a.logits[at * E + e];
+        if (accumulate) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) old[e] = a.dlogits[at * E + e];
+        }
+        valid = there && (!a.valid || v != 0);
     }
 };
 
@@ -206,10 +213,17 @@ struct Losses {
     double sum[2 * E];                   // over tokens, of p and of q
     float alpha[E], weight[2], coeff[2 * E];     // coeff: gradients of the sums
 
-    __device__ inline void begin(const BalanceArgs &a) {
-        const int i = (int)threadIdx.x - 64;             // the second wavefront: the first has its share of the sums
-        if (i >= 0 && i < E) alpha[i] = a.alpha[i];
-        else if (i >= E && i < E + 2) weight[i - E] = a.dlosses[i - E];
+    // asks; what came is put down by put, before a barrier
+    struct Asked {
+        float alpha, weight;
+    };
+    static __device__ inline Asked ask(const BalanceArgs &a) {
+        const int i = threadIdx.x < E ? (int)threadIdx.x : 0;
+        return {a.alpha[i], a.dlosses[i & 1]};
+    }
+    __device__ inline void put(const Asked &x) {
+        if (threadIdx.x < E) alpha[threadIdx.x] = x.alpha;
+        if (threadIdx.x < 2) weight[threadIdx.x] = x.weight;
     }
     // behind a barrier; another one before coeff is read
     __device__ inline void end(const BalanceArgs &a, bool write) {
@@ -236,7 +250,7 @@ struct Losses {
 };
 
 template <int E>
-__device__ inline void grad_token(const BalanceArgs &a, long t, bool valid, const TokenRouting<E> &r, const float (&density)[E],
+__device__ inline void grad_token(const BalanceArgs &a, long t, const Token<E> &x, const TokenRouting<E> &r, const float (&density)[E],
                                   const float (&coeff)[2 * E]) {
     float *dl = a.dlogits + (size_t)t * E;
     float up[E], to_first = 0.0f, to_second = 0.0f;
@@ -255,19 +269,20 @@ __device__ inline void grad_token(const BalanceArgs &a, long t, bool valid, cons
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const float d = valid ? r.p[e] * (up[e] - mean) : 0.0f;
-        if (!a.accumulate) dl[e] = d;
-        else if (valid) dl[e] += d;
+        const float d = r.p[e] * (up[e] - mean), none = a.accumulate ? x.old[e] : 0.0f;
+        up[e] = !x.valid ? none : a.accumulate ? x.old[e] + d : d;
     }
+#pragma unroll
+    for (int e = 0; e < E; ++e) dl[e] = up[e];
 }
 
 template <int E>
-__device__ inline void densities(const TokenRouting<E> &r, float noise_std, float (&out)[E]) {
-    const float peak = 0.39894228040143268f / noise_std;
+__device__ inline void densities(const TokenRouting<E> &r, float peak, float (&out)[E]) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) out[e] = peak * expf(-0.5f * r.z[e] * r.z[e]);
+    for (int e = 0; e < E; ++e) out[e] = peak * exp_minus_square(r.z[e] * 0.70710678118654752f);
 }
 
+static_assert(kMaxE <= 8, "an expert to a wavefront of the sums");
 constexpr int kSumThreads = 512, kSumWaves = kSumThreads / 64, kMaxSumParts = 256, kMaxGradBlocks = 512;
 constexpr int kOneThreads = 1024;
 constexpr long kOneLogits = 2048;        // up to this many, all of it in one workgroup
@@ -279,11 +294,11 @@ __global__ __launch_bounds__(kSumThreads) void balance_sums_kernel(BalanceArgs a
     const long step = (long)gridDim.x * kSumThreads;
     Token<E> nxt;
     long t0 = (long)blockIdx.x * kSumThreads;
-    nxt.load(a, t0 + threadIdx.x);
+    nxt.load(a, t0 + threadIdx.x, false);
     for (; t0 < a.T; t0 += step) {
         const Token<E> x = nxt;
-        nxt.load(a, t0 + step + threadIdx.x);
-        s.add(route_token<E>(x.l, 1.0f / a.noise_std), x.valid);
+        nxt.load(a, t0 + step + threadIdx.x, false);
+        s.add(route_token<E>(x.l, a.inv_noise_std), x.valid);
     }
     group.leave(s);
     const int i = threadIdx.x;
@@ -296,41 +311,51 @@ __global__ __launch_bounds__(kSumThreads) void balance_sums_kernel(BalanceArgs a
 template <int E>
 __global__ __launch_bounds__(kSumThreads) void balance_grad_kernel(BalanceArgs a) {
     __shared__ Losses<E> losses;
-    losses.begin(a);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     constexpr int kEach = kMaxSumParts / 64, kMine = (2 * E + kSumWaves - 1) / kSumWaves;
+    const auto asked = Losses<E>::ask(a);
     double part[kMine][kEach];
 #pragma unroll
     for (int m = 0; m < kMine; ++m)
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
             const int v = wave + m * kSumWaves, at = lane + 64 * k;
-            part[m][k] = v < 2 * E && at < a.parts ? a.partial[(size_t)v * a.parts + at] : 0.0;
+            part[m][k] = a.partial[(size_t)(v < 2 * E ? v : 0) * a.parts + (at < a.parts ? at : 0)];
         }
+    // the first workgroup adds up the counts, an expert to a wavefront
+    const bool counting = blockIdx.x == 0 && a.counts && wave < E;
+    int counted[kEach] = {};
+    if (counting) {
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const int at = lane + 64 * k;
+            counted[k] = a.partial_counts[(size_t)wave * a.parts + (at < a.parts ? at : 0)];
+        }
+    }
     const long step = (long)gridDim.x * kSumThreads;
     long t = (long)blockIdx.x * kSumThreads + threadIdx.x;
     Token<E> x;
-    x.load(a, t);
-    TokenRouting<E> r = route_token<E>(x.l, 1.0f / a.noise_std);
+    x.load(a, t, a.accumulate);
+    TokenRouting<E> r = route_token<E>(x.l, a.inv_noise_std);
     float density[E], coeff[2 * E];
-    densities<E>(r, a.noise_std, density);
+    densities<E>(r, a.peak, density);
 #pragma unroll
     for (int m = 0; m < kMine; ++m) {
         const int v = wave + m * kSumWaves;
         double s = 0.0;
 #pragma unroll
-        for (int k = 0; k < kEach; ++k) s += part[m][k];
+        for (int k = 0; k < kEach; ++k) s += lane + 64 * k < a.parts ? part[m][k] : 0.0;
         s = wave_sum_d(s);
         if (lane == 0 && v < 2 * E) losses.sum[v] = s;
     }
-    if (blockIdx.x == 0 && a.counts) {
-        for (int e = wave; e < E; e += kSumWaves) {
-            int c = 0;
-            for (int k = lane; k < a.parts; k += 64) c += a.partial_counts[(size_t)e * a.parts + k];
+    losses.put(asked);
+    if (counting) {
+        int c = 0;
 #pragma unroll
-            for (int off = 32; off >= 1; off >>= 1) c += __shfl_xor(c, off, 64);
-            if (lane == 0) a.counts[e] = c;
-        }
+        for (int k = 0; k < kEach; ++k) c += lane + 64 * k < a.parts ? counted[k] : 0;
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) c += __shfl_xor(c, off, 64);
+        if (lane == 0) a.counts[wave] = c;
     }
     __syncthreads();
     losses.end(a, blockIdx.x == 0);
@@ -338,13 +363,13 @@ __global__ __launch_bounds__(kSumThreads) void balance_grad_kernel(BalanceArgs a
 #pragma unroll
     for (int i = 0; i < 2 * E; ++i) coeff[i] = losses.coeff[i];
     while (t < a.T) {
-        const bool valid = x.valid;
-        x.load(a, t + step);
-        grad_token<E>(a, t, valid, r, density, coeff);
+        const Token<E> now = x;
+        x.load(a, t + step, a.accumulate);
+        grad_token<E>(a, t, now, r, density, coeff);
         t += step;
         if (t >= a.T) break;
-        r = route_token<E>(x.l, 1.0f / a.noise_std);
-        densities<E>(r, a.noise_std, density);
+        r = route_token<E>(x.l, a.inv_noise_std);
+        densities<E>(r, a.peak, density);
     }
 }
 
@@ -354,12 +379,14 @@ __global__ __launch_bounds__(kOneThreads) void balance_one_kernel(BalanceArgs a)
     static_assert(kTokens == 1, "a thread has a token at most");
     __shared__ GroupSums<E, kOneThreads / 64> group;
     __shared__ Losses<E> losses;
-    losses.begin(a);
+    const auto asked = Losses<E>::ask(a);
     Token<E> x;
-    x.load(a, threadIdx.x);
-    const TokenRouting<E> r = route_token<E>(x.l, 1.0f / a.noise_std);
+    if (a.T > 0) x.load(a, threadIdx.x, a.accumulate);
+    else x = Token<E>{};
+    const TokenRouting<E> r = route_token<E>(x.l, a.inv_noise_std);
     TokenSums<E> s;
     s.add(r, x.valid);
+    losses.put(asked);
     group.leave(s);
     const int i = threadIdx.x;
     if (i < 2 * E) losses.sum[i] = group.sum(i);
@@ -369,10 +396,10 @@ __global__ __launch_bounds__(kOneThreads) void balance_one_kernel(BalanceArgs a)
     __syncthreads();
     if (threadIdx.x >= a.T) return;
     float density[E], coeff[2 * E];
-    densities<E>(r, a.noise_std, density);
+    densities<E>(r, a.peak, density);
 #pragma unroll
     for (int k = 0; k < 2 * E; ++k) coeff[k] = losses.coeff[k];
-    grad_token<E>(a, threadIdx.x, x.valid, r, density, coeff);
+    grad_token<E>(a, threadIdx.x, x, r, density, coeff);
 }
 
 int balance_parts(long T) {
@@ -530,7 +557,7 @@ extern "C" int sa_moe_balance_loss_grad(const float *logits, long T, int E, cons
     const size_t need = balance_workspace(T);
     SA_REQUIRE(workspace != nullptr && workspace_bytes >= need, SA_ERR_WORKSPACE,
                "sa_moe_balance_loss_grad: workspace of %zu bytes needed, %zu given", need, workspace_bytes);
-    BalanceArgs a{logits, T, valid_or_null, alpha, noise_std, dlosses, losses, sums_or_null, counts_or_null, dlogits, accumulate};
+    BalanceArgs a{logits, T, valid_or_null, alpha, 1.0f / noise_std, 0.39894228040143268f / noise_std, dlosses, losses, sums_or_null, counts_or_null, dlogits, accumulate};
     a.parts = balance_parts(T);
     a.partial = static_cast<double *>(workspace);
     a.partial_counts = reinterpret_cast<int32_t *>(a.partial + (size_t)a.parts * 2 * kMaxE);
