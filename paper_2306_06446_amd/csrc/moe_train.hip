@@ -283,9 +283,10 @@ __device__ inline void densities(const TokenRouting<E> &r, float peak, float (&o
 }
 
 static_assert(kMaxE <= 8, "an expert to a wavefront of the sums");
-constexpr int kSumThreads = 512, kSumWaves = kSumThreads / 64, kMaxSumParts = 256, kMaxGradBlocks = 512;
-constexpr int kOneThreads = 1024;
-constexpr long kOneLogits = 2048;        // up to this many, all of it in one workgroup
+constexpr int kSumThreads = 512, kSumWaves = kSumThreads / 64, kMaxGradBlocks = 512;
+// Two workgroups to a CU, but one for many experts: every workgroup of the gradient reads 2 E sums of each part.
+constexpr int max_sum_parts(int E) { return E <= 4 ? 512 : 256; }
+constexpr int kOneThreads = 1024;        // up to as many tokens, all of it in one workgroup
 
 template <int E>
 __global__ __launch_bounds__(kSumThreads) void balance_sums_kernel(BalanceArgs a) {
@@ -312,7 +313,7 @@ template <int E>
 __global__ __launch_bounds__(kSumThreads) void balance_grad_kernel(BalanceArgs a) {
     __shared__ Losses<E> losses;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    constexpr int kEach = kMaxSumParts / 64, kMine = (2 * E + kSumWaves - 1) / kSumWaves;
+    constexpr int kEach = max_sum_parts(E) / 64, kMine = (2 * E + kSumWaves - 1) / kSumWaves;
     const auto asked = Losses<E>::ask(a);
     double part[kMine][kEach];
 #pragma unroll
@@ -375,8 +376,6 @@ __global__ __launch_bounds__(kSumThreads) void balance_grad_kernel(BalanceArgs a
 
 template <int E>
 __global__ __launch_bounds__(kOneThreads) void balance_one_kernel(BalanceArgs a) {
-    constexpr int kTokens = (int)((kOneLogits / E + kOneThreads - 1) / kOneThreads);      // of a thread, at most
-    static_assert(kTokens == 1, "a thread has a token at most");
     __shared__ GroupSums<E, kOneThreads / 64> group;
     __shared__ Losses<E> losses;
     const auto asked = Losses<E>::ask(a);
@@ -402,15 +401,15 @@ __global__ __launch_bounds__(kOneThreads) void balance_one_kernel(BalanceArgs a)
     grad_token<E>(a, threadIdx.x, x, r, density, coeff);
 }
 
-int balance_parts(long T) {
-    const long parts = (T + kSumThreads - 1) / kSumThreads;
-    return (int)(parts < kMaxSumParts ? parts : kMaxSumParts);
+int balance_parts(long T, int E) {
+    const long parts = (T + kSumThreads - 1) / kSumThreads, most = max_sum_parts(E);
+    return (int)(parts < most ? parts : most);
 }
-size_t balance_workspace(long T) { return (size_t)balance_parts(T) * kMaxE * (2 * 8 + 4) + 256; }
+size_t balance_workspace(long T, int E) { return (size_t)balance_parts(T, E) * kMaxE * (2 * 8 + 4) + 256; }
 
 template <int E>
 int launch_balance(const BalanceArgs &a, hipStream_t st) {
-    if (a.T * E <= kOneLogits) {
+    if (a.T <= kOneThreads) {
         balance_one_kernel<E><<<dim3(1), dim3(kOneThreads), 0, st>>>(a);
         return check_launch("sa_moe_balance_loss_grad(one launch)");
     }
@@ -536,7 +535,7 @@ struct RunCombineGrad {
 
 extern "C" size_t sa_moe_balance_loss_grad_workspace_bytes(long T, int E) {
     if (T < 0 || T >= (1L << 31) || E < 2 || E > kMaxE) return 0;
-    return balance_workspace(T);
+    return balance_workspace(T, E);
 }
 
 extern "C" int sa_moe_balance_loss_grad(const float *logits, long T, int E, const uint8_t *valid_or_null, const float *alpha,
@@ -554,11 +553,11 @@ extern "C" int sa_moe_balance_loss_grad(const float *logits, long T, int E, cons
                    sa::aligned16(losses) && sa::aligned16(sums_or_null) && sa::aligned16(counts_or_null) && sa::aligned16(dlogits) &&
                    sa::aligned16(workspace),
                SA_ERR_ALIGN, "sa_moe_balance_loss_grad: pointers must be 16-byte aligned");
-    const size_t need = balance_workspace(T);
+    const size_t need = balance_workspace(T, E);
     SA_REQUIRE(workspace != nullptr && workspace_bytes >= need, SA_ERR_WORKSPACE,
                "sa_moe_balance_loss_grad: workspace of %zu bytes needed, %zu given", need, workspace_bytes);
     BalanceArgs a{logits, T, valid_or_null, alpha, 1.0f / noise_std, 0.39894228040143268f / noise_std, dlosses, losses, sums_or_null, counts_or_null, dlogits, accumulate};
-    a.parts = balance_parts(T);
+    a.parts = balance_parts(T, E);
     a.partial = static_cast<double *>(workspace);
     a.partial_counts = reinterpret_cast<int32_t *>(a.partial + (size_t)a.parts * 2 * kMaxE);
     return by_experts(E, [&](auto experts) { return launch_balance<decltype(experts)::value>(a, sa::as_stream(stream)); });
