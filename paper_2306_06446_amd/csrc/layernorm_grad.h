@@ -41,7 +41,7 @@ struct GradPlan {
     static constexpr int HELD = ROUTE > kStreamed ? ROUTE : 0;
     static constexpr int ELEMS = S::VEC * S::CH;
     static constexpr int ROW = ELEMS * (2 * sizeof(X) + sizeof(Y)) / 4;
-    static constexpr int REGISTERS = ELEMS * (2 + HELD + 1 + HELD + 2) + 2 * ROW + 48;
+    static constexpr int REGISTERS = ELEMS * (2 + HELD + 1 + HELD + 2) + 2 * (ROW + HELD) + 48;
     static constexpr bool AHEAD = REGISTERS < 256;
     // A workgroup to a CU, of the wavefronts that its registers have room for: the fewest parts that keep it busy.  Wavefronts that share
     // rows wait for each other at every row: there in workgroups of four, or a row's, of which a CU has two (25000 x 4000 fp16

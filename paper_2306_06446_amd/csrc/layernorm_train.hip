@@ -12,6 +12,9 @@ constexpr int kNormWaves = 4;                // of a workgroup of rows of one wa
 template <class X, class Y, class S, int ROUTE, bool TRAIN>
 __global__ __launch_bounds__(S::WIDE ? 512 : 64 * kNormWaves) void train_norm_kernel(NormArgs a) {
     constexpr int VEC = S::VEC, CH = S::CH, HELD = ROUTE, PR = HELD ? HELD : 1, PC = HELD ? CH : 1;
+    // Of many experts whose rows have whole wavefronts, lane l has the logit of expert l / 8, of every eighth step: eight rows leave at a time.
+    constexpr bool EIGHT = HELD == kMaxExperts && S::LANES >= 64;
+    constexpr int PERIOD = EIGHT ? 8 : S::PERIOD;
     __shared__ __align__(16) float red[S::WIDE ? PR : 1][2][8], tile[HELD == kMaxExperts ? kRouterTileFloats : 1];
     const RowPlace<S> p(a.E);
     const int g = p.g, l = p.l, groups = S::WIDE ? p.groups : 64 * kNormWaves / S::LANES;
@@ -26,7 +29,7 @@ __global__ __launch_bounds__(S::WIDE ? 512 : 64 * kNormWaves) void train_norm_ke
     Piece<X, VEC> nxt[CH], x[CH];
     long t0 = (long)blockIdx.x * groups;
     load(nxt, t0 + g);
-    float gm[CH][VEC], bt[CH][VEC], w[PR][PC][VEC], bias[PR];
+    float gm[CH][VEC], bt[CH][VEC], w[PR][PC][VEC], bias[EIGHT ? 1 : PR];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         load_columns<VEC>(gm[c], a.gamma + p.at[c]);
@@ -40,22 +43,32 @@ __global__ __launch_bounds__(S::WIDE ? 512 : 64 * kNormWaves) void train_norm_ke
         for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int i = 0; i < VEC; ++i) w[e][c][i] = p.own(c, i, w[e][c][i]);
+    const int expert = l >> 3;           // (EIGHT)
+    if constexpr (EIGHT) {
+        bias[0] = a.bg[expert < a.n ? expert : 0];
+    } else {
 #pragma unroll
-    for (int e = 0; e < HELD; ++e) bias[e] = a.bg[HELD == 2 || e < a.n ? e : 0];
+        for (int e = 0; e < HELD; ++e) bias[e] = a.bg[HELD == 2 || e < a.n ? e : 0];
+    }
     // What there is one of to a row is kept, a step to a lane, and leaves for PERIOD rows at a time: every step then stores the same
     // number of pieces, and a wait for the next row leaves the last row's stores in flight (one counter, in order).
-    float kept_mean = 0.0f, kept_rstd = 0.0f, kept[PR];
-#pragma unroll
-    for (int e = 0; e < PR; ++e) kept[e] = 0.0f;
+    float kept_mean = 0.0f, kept_rstd = 0.0f, kept[EIGHT ? 1 : PR] = {};
     const long t_first = (long)blockIdx.x * groups + g;
     auto flush = [&](long steps) {       // the last 1 to PERIOD of `steps` steps
-        const long k = (steps - 1) / S::PERIOD * S::PERIOD + l, t = t_first + k * stride;
-        if (l >= S::PERIOD || k >= steps || t >= a.T) return;
-        if (TRAIN || a.mean) a.mean[t] = kept_mean;
-        if (TRAIN || a.rstd) a.rstd[t] = kept_rstd;
+        if (l >= (EIGHT ? 64 : PERIOD)) return;
+        const long k = (steps - 1) / PERIOD * PERIOD + (l & (PERIOD - 1)), t = t_first + k * stride;
+        if (k >= steps || t >= a.T) return;
+        if (l < PERIOD) {
+            if (TRAIN || a.mean) a.mean[t] = kept_mean;
+            if (TRAIN || a.rstd) a.rstd[t] = kept_rstd;
+        }
+        if constexpr (EIGHT) {
+            if (expert < a.n) a.logits[(size_t)t * a.n + expert] = kept[0];
+        } else {
 #pragma unroll
-        for (int e = 0; e < HELD; ++e)
-            if (HELD == 2 || e < a.n) a.logits[(size_t)t * a.n + e] = kept[e];
+            for (int e = 0; e < HELD; ++e)
+                if (HELD == 2 || e < a.n) a.logits[(size_t)t * a.n + e] = kept[e];
+        }
     };
     auto work = [&](const Piece<X, VEC> (&x)[CH], long t, bool row_ok, long step) {
         float s[1] = {0.0f};
@@ -75,7 +88,7 @@ __global__ __launch_bounds__(S::WIDE ? 512 : 64 * kNormWaves) void train_norm_ke
             }
         sum(s);
         const float rstd = 1.0f / __builtin_sqrtf(__builtin_fmaf(s[0], per, a.eps));
-        const bool keep = (int)(step & (S::PERIOD - 1)) == l;
+        const bool keep = (int)(step & (PERIOD - 1)) == (EIGHT ? l & 7 : l);
         kept_mean = keep ? mean : kept_mean;
         kept_rstd = keep ? rstd : kept_rstd;
         float y[CH][VEC];
@@ -95,9 +108,20 @@ __global__ __launch_bounds__(S::WIDE ? 512 : 64 * kNormWaves) void train_norm_ke
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) part[e] = __builtin_fmaf(y[c][i], w[e][c][i], part[e]);
             }
-            sum(part);
+            if constexpr (EIGHT) {
+                float logit = eight_sums(part);
+                if constexpr (S::WIDE) {
+                    if ((l & 7) == 0) red[(l >> 3) & 7][sum.turn][threadIdx.x >> 6] = logit;
+                    __syncthreads();
+                    logit = sum.of(expert & 7);
+                    sum.turn ^= 1;
+                }
+                kept[0] = keep ? logit + bias[0] : kept[0];
+            } else {
+                sum(part);
 #pragma unroll
-            for (int e = 0; e < HELD; ++e) kept[e] = keep ? part[e] + bias[e] : kept[e];
+                for (int e = 0; e < HELD; ++e) kept[e] = keep ? part[e] + bias[e] : kept[e];
+            }
         }
     };
     long step = 0;
@@ -106,12 +130,12 @@ __global__ __launch_bounds__(S::WIDE ? 512 : 64 * kNormWaves) void train_norm_ke
         for (int c = 0; c < CH; ++c) x[c] = nxt[c];
         load(nxt, t0 + g + stride);
         work(x, t0 + g, true, step++);
-        if ((step & (S::PERIOD - 1)) == 0) flush(step);
+        if ((step & (PERIOD - 1)) == 0) flush(step);
     }
     if (t0 < a.T) {
         work(nxt, t0 + g, t0 + g < a.T, step++);
         flush(step);
-    } else if ((step & (S::PERIOD - 1)) != 0) {
+    } else if ((step & (PERIOD - 1)) != 0) {
         flush(step);
     }
 }

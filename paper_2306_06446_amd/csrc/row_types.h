@@ -1,6 +1,8 @@
 // Rows of the training operators: fp32, fp16 or bf16 in memory, fp32 in registers; which lanes hold which part of a row.
 #pragma once
 
+#include <type_traits>
+
 #include "common.h"
 #include "layernorm.h"
 
@@ -87,6 +89,28 @@ struct RowPlace {
     __device__ inline float own(int c, int i, float v) const { return c < S::FULL || i >= skip[c] ? v : 0.0f; }
 };
 
+// Eight sums over a wavefront, the one of value lane / 8 in each lane: every step adds two values at once, each in half of the lanes.
+__device__ inline float eight_sums(const float (&v)[8]) {
+    auto swap_add = [](float a, float b, auto rows) {
+        const uint32_t u = __builtin_bit_cast(uint32_t, a), w = __builtin_bit_cast(uint32_t, b);
+        const auto r = decltype(rows)::value ? __builtin_amdgcn_permlane16_swap(u, w, false, false) : __builtin_amdgcn_permlane32_swap(u, w, false, false);
+        const uint32_t r0 = r[0], r1 = r[1];
+        return __builtin_bit_cast(float, r0) + __builtin_bit_cast(float, r1);
+    };
+    float h[4], q[2];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) h[k] = swap_add(v[k], v[k + 4], std::false_type());
+#pragma unroll
+    for (int k = 0; k < 2; ++k) q[k] = swap_add(h[k], h[k + 2], std::true_type());
+    const bool upper = threadIdx.x & 8;
+    const float mine = upper ? q[1] : q[0], other = upper ? q[0] : q[1];
+    const int moved = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, other), 0x128, 0xF, 0xF, true);      // row_ror:8
+    float s = mine + __builtin_bit_cast(float, moved);
+    s = dpp_add<0x141>(s);                // row_half_mirror
+    s = dpp_add<0x4E>(s);                 // quad_perm: lanes 2 apart
+    return dpp_add<0xB1>(s);              // lanes 1 apart
+}
+
 // Sums of a row over its lanes, N at a time, in all of them.  Rows of several wavefronts exchange theirs in LDS; two buffers in turn, so that
 // one barrier per exchange is enough (a wavefront that writes a buffer again has passed the barrier behind its last reads).
 template <class S, int N>
@@ -94,6 +118,18 @@ struct RowSums {
     float (*red)[2][8];                  // [N][2][wavefronts] in LDS, where a row has several wavefronts
     int first, waves, turn = 0;
     __device__ inline RowSums(float (*red_)[2][8], const RowPlace<S> &p) : red(red_), first(p.g * (p.lanes / 64)), waves(p.lanes / 64) {}
+    // what the row's wavefronts have left of value k: 2, 4 or 8, in loads as wide as that
+    __device__ inline float of(int k) const {
+        const float *from = red[k][turn] + first;
+        if (waves == 2) return from[0] + from[1];
+        const float4 a = *reinterpret_cast<const float4 *>(from);
+        float s = (a.x + a.y) + (a.z + a.w);
+        if (waves == 8) {
+            const float4 b = *reinterpret_cast<const float4 *>(from + 4);
+            s += (b.x + b.y) + (b.z + b.w);
+        }
+        return s;
+    }
     template <int M>
     __device__ inline void operator()(float (&v)[M], int used = M) {
         static_assert(M <= N, "room in LDS");
@@ -111,17 +147,7 @@ struct RowSums {
 #pragma unroll
             for (int k = 0; k < M; ++k) {
                 if (k >= used) continue;
-                const float *from = red[k][turn] + first;        // 2, 4 or 8, in loads as wide as that
-                if (waves == 2) {
-                    v[k] = from[0] + from[1];
-                } else {
-                    const float4 a = *reinterpret_cast<const float4 *>(from);
-                    v[k] = (a.x + a.y) + (a.z + a.w);
-                    if (waves == 8) {
-                        const float4 b = *reinterpret_cast<const float4 *>(from + 4);
-                        v[k] += (b.x + b.y) + (b.z + b.w);
-                    }
-                }
+                v[k] = of(k);
             }
             turn ^= 1;
         }
