@@ -89,6 +89,15 @@ __global__ __launch_bounds__((64 * GradPlan<X, Y, S, ROUTE>::MOST)) void norm_gr
 
     auto work = [&](const GradRow<X, Y, S, ROUTE> &r, long t, bool row_ok) {
         float mean = r.mean, rstd = r.rstd, s[2];
+        if constexpr (S::WIDE) {
+            // before the row's first barrier: dx may be in the place of any of them
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                arrived(r.dy[c]);
+                arrived(r.x[c]);
+                if (a.dres) arrived(r.res[c]);
+            }
+        }
         if (!a.mean) {
             s[0] = 0.0f;
 #pragma unroll

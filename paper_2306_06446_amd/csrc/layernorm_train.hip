@@ -72,6 +72,10 @@ __global__ __launch_bounds__(S::WIDE ? 512 : 64 * kNormWaves) void train_norm_ke
     };
     auto work = [&](const Piece<X, VEC> (&x)[CH], long t, bool row_ok, long step) {
         float s[1] = {0.0f};
+        if constexpr (S::WIDE) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) arrived(x[c]);      // y may be in the place of x
+        }
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll

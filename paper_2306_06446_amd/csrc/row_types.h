@@ -27,6 +27,14 @@ struct Piece<T, 1> {
     __device__ inline float operator[](int) const { return (float)v; }
 };
 
+// Has the loads of a piece behind it: values that two wavefronts read are there in both before a barrier, behind which one of them may store
+// over them (a result in its operand's place).
+template <class P>
+__device__ inline void arrived(const P &p) {
+    typedef uint32_t words __attribute__((ext_vector_type(sizeof(p.v) / 4)));
+    asm volatile("" : : "v"(__builtin_bit_cast(words, p.v)) : "memory");
+}
+
 // A result in 32 bits to T by one rounding to nearest even.  For fp16 the compiler would fuse the conversion with the operation before it
 // where nothing else reads that, which rounds otherwise on a tie: the same rows would differ between calls with other outputs.
 template <class T>

@@ -167,6 +167,25 @@ def test_dx_takes_the_place_of_what_it_is_made_of(sa, E, place):
     assert torch.equal(sa.sa_layernorm(x, s["gamma"], s["beta"], EPS, y=x)[0], y)
 
 
+@pytest.mark.parametrize("xt,T,E", [(F32, 1500, 5001), (BF16, 2000, 2061), (F16, 3000, 1030), (BF16, 700, 8189), (F32, 4000, 333), (F16, 900, 4100)], ids=str)
+@pytest.mark.parametrize("n", [0, 2, 3])
+def test_in_place_gives_the_same_bits(sa, xt, T, E, n):
+    """Elements at a row's end are computed by two lanes, of wide rows in two wavefronts: both from what was there before."""
+    s = inputs(T, E, xt, xt, n, 21)
+    y, mean, rstd, _ = sa.sa_layernorm(s["x"], s["gamma"], s["beta"], EPS)
+    x = s["x"].clone()
+    assert torch.equal(sa.sa_layernorm(x, s["gamma"], s["beta"], EPS, y=x)[0], y)
+    for stats in (True, False):
+        kw = dict(mean=mean if stats else None, rstd=rstd if stats else None, dlogits=s.get("dlogits"), wg=s.get("wg"))
+        want = sa.sa_layernorm_backward(s["dy"], s["x"], s["gamma"], s["beta"], EPS, dres=s["dres"], **kw)
+        for place in ("dres", "dy", "x"):
+            t = {k: s[k].clone() for k in ("dres", "dy", "x")}
+            got = sa.sa_layernorm_backward(t["dy"], t["x"], s["gamma"], s["beta"], EPS, dres=t["dres"], dx=t[place], **kw)
+            assert got[0] is t[place]
+            for g, w in zip(got, want):
+                assert (g is None and w is None) or torch.equal(g, w), place
+
+
 @pytest.mark.parametrize("T,E,xt,yt", [(3, 5, BF16, BF16), (33, 1001, F16, F16), (70, 4099, F32, BF16), (9, 130, F32, F32)], ids=str)
 def test_nothing_is_written_behind_the_outputs(sa, T, E, xt, yt):
     n, s = 3, inputs(T, E, xt, yt, 3, 2)
