@@ -338,7 +338,9 @@ int sa_layernorm_quant(const float *x, long T, int E, const float *gamma, const 
  * Training of the parts around the Linears: LayerNorm, router, gate and balance loss.  The calls below take rows of several
  * element types; a residual stream (x, dres, dx; dy of the combine) has the type of the rows it meets (y, dy; src, dsrc), or is
  * SA_F32 under rows of any type.  Sums, statistics and parameter gradients are fp32 or wider, an output is rounded once (to
- * nearest even), and every sum has a fixed order: a call repeated gives the same bits.
+ * nearest even), and every sum has a fixed order: a call repeated gives the same bits.  Rows are dense ([T, E], row t at t * E) and
+ * may begin at any element: 16-byte alignment is asked of buffers only.  A workspace belongs to one call from its first launch to
+ * its last: calls on other streams, and captured graphs that may run at the same time, need one each.
  */
 #define SA_F32 0
 #define SA_F16 1
@@ -351,7 +353,7 @@ int sa_layernorm_quant(const float *x, long T, int E, const float *gamma, const 
  *   logits[t, :] = y[t, :] * wg + bg          the router G of Sec. 4.2, of y before it is rounded to y_type
  *   x [T, E] of x_type, y_or_null [T, E] of y_type, mean_or_null and rstd_or_null fp32 [T], gamma, beta fp32 [E],
  *   wg fp32 [E, n_experts], bg fp32 [n_experts], logits_or_null fp32 [T, n_experts], 2 <= n_experts <= 8.
- * Any E from 1 to 8192 (16-byte alignment is asked of the buffers, not of the rows).  y may be x where the types are the same.
+ * Any E from 1 to 8192.  At least one of the outputs.  y may be x where the types are the same.
  */
 int sa_layernorm(const void *x, int x_type, long T, int E, const float *gamma, const float *beta, float eps,
                  void *y_or_null, int y_type, float *mean_or_null, float *rstd_or_null, const float *wg_or_null,
@@ -388,8 +390,8 @@ int sa_layernorm_backward(const void *dy, int y_type, const void *x, int x_type,
  *   valid_or_null uint8 [T]: a token of 0 is padding, counts for nothing, its logits may hold anything and its gradient is 0;
  *   losses fp32 [2]; sums_or_null fp32 [2, E] = IMP then LOAD; counts_or_null int32 [E], tokens whose largest logit is the expert's
  *   (ties to the lowest index, as sa_moe_dispatch counts all tokens); dlogits [T, E] fp32.
- * accumulate != 0 adds the gradient to dlogits (where that of the combine is).  Where no token counts, or the mean of a loss is 0,
- * that loss and its gradient are 0.  2 <= E <= 8, 0 <= T < 2^31, noise_std > 0.  Sums over tokens are fp64 in a fixed order.
+ * accumulate != 0 adds the gradient to dlogits (where that of the combine is); dlogits must not be logits.  Where no token counts, or the mean of a loss is 0,
+ * that loss and its gradient are 0.  2 <= E <= 8, 0 <= T < 2^31, noise_std > 0 with a finite reciprocal.  Sums over tokens are fp64 in a fixed order.
  */
 size_t sa_moe_balance_loss_grad_workspace_bytes(long T, int E);
 int sa_moe_balance_loss_grad(const float *logits, long T, int E, const uint8_t *valid_or_null, const float *alpha,
@@ -478,7 +480,7 @@ int sa_combine_rows(const float *src, const sa_rows *rows, const float *gate_or_
  *   dlogits[r,k] = dgate[r] * p_e * ((k == e) - p_k)
  *   dy of y_type (rows as y has them), src and dsrc_or_null [max_rows, E] of src_type, gate_or_null, dgate_or_null fp32 [T] and
  *   logits_or_null, dlogits_or_null fp32 [T, n_experts].  At least one of the outputs; dlogits needs logits and gate, dgate and
- *   dlogits need src.  Any E >= 1, 2 <= n_experts <= 8.  With perm as rows and no counts, one call does the rows of all experts, src
+ *   dlogits need src.  1 <= E <= 2^30, 2 <= n_experts <= 8.  With perm as rows and no counts, one call does the rows of all experts, src
  *   in the order of perm.  Rows that are not selected are left as they are; a row may be selected once only.  dsrc may be src.
  */
 int sa_combine_rows_backward(const void *dy, int y_type, const void *src_or_null, int src_type, const sa_rows *rows,

@@ -546,8 +546,8 @@ extern "C" int sa_moe_balance_loss_grad(const float *logits, long T, int E, cons
     SA_REQUIRE(T >= 0, SA_ERR_INVALID, "sa_moe_balance_loss_grad: T < 0");
     SA_REQUIRE(T < (1L << 31), SA_ERR_SHAPE, "sa_moe_balance_loss_grad: T >= 2^31");
     SA_REQUIRE(E >= 2 && E <= kMaxE, SA_ERR_SHAPE, "sa_moe_balance_loss_grad: 2 to 8 experts (got %d)", E);
-    SA_REQUIRE(noise_std > 0.0f && __builtin_isfinite(noise_std), SA_ERR_INVALID,
-               "sa_moe_balance_loss_grad: noise_std must be positive and finite");
+    SA_REQUIRE(noise_std > 0.0f && __builtin_isfinite(noise_std) && __builtin_isfinite(1.0f / noise_std), SA_ERR_INVALID,
+               "sa_moe_balance_loss_grad: noise_std must be positive and finite, and so must its reciprocal");
     SA_REQUIRE(alpha && dlosses && losses && (T == 0 || (logits && dlogits)), SA_ERR_INVALID, "sa_moe_balance_loss_grad: NULL buffer");
     SA_REQUIRE(sa::aligned16(logits) && sa::aligned16(valid_or_null) && sa::aligned16(alpha) && sa::aligned16(dlosses) &&
                    sa::aligned16(losses) && sa::aligned16(sums_or_null) && sa::aligned16(counts_or_null) && sa::aligned16(dlogits) &&
@@ -571,7 +571,7 @@ extern "C" int sa_combine_rows_backward(const void *dy, int y_type, const void *
     int rc = sa::validate_rows(rows, &sel);
     if (rc == SA_OK) rc = sa::check_row_types("sa_combine_rows_backward", y_type, src_type);
     if (rc != SA_OK) return rc;
-    SA_REQUIRE(E > 0, SA_ERR_SHAPE, "sa_combine_rows_backward: E must be positive");
+    SA_REQUIRE(E > 0 && E <= (1 << 30), SA_ERR_SHAPE, "sa_combine_rows_backward: E must be positive and at most 2^30");
     SA_REQUIRE(!dlogits_or_null || (n_experts >= 2 && n_experts <= kMaxE), SA_ERR_SHAPE,
                "sa_combine_rows_backward: 2 to 8 experts (got %d)", n_experts);
     if (sel.max_rows == 0) return SA_OK;

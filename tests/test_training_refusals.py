@@ -81,7 +81,7 @@ def test_balance_loss_grad(lib):
         accumulate=0, workspace=FAKE, bytes=1 << 40, stream=None))
     assert call() == HIP and call(valid=None, sums=None, counts=None) == HIP and call(T=0, logits=None, dlogits=None, valid=None) == HIP
     assert call(T=-1) == INVALID and call(T=1 << 31) == SHAPE and call(E=1) == SHAPE and call(E=9) == SHAPE
-    for std in (0.0, -1.0, float("nan"), float("inf")):
+    for std in (0.0, -1.0, float("nan"), float("inf"), 1e-40):
         assert call(noise_std=std) == INVALID, std
     for name in ("logits", "alpha", "dlosses", "losses", "dlogits"):
         assert call(**{name: None}) == INVALID, name
@@ -101,7 +101,7 @@ def test_combine_rows_backward(lib):
     assert call() == HIP and call(gate=None, logits=None, dlogits=None) == HIP and call(src=None, dgate=None, dlogits=None) == HIP
     assert call(rows=rows(None)) == HIP and call(rows=rows(FAKE, FAKE, 7)) == HIP and call(rows=rows(m=0), dy=None) == OK
     assert call(y_type=1, src_type=0) == UNSUPPORTED and call(y_type=9) == INVALID
-    assert call(E=0) == SHAPE and call(n=1) == SHAPE and call(n=9) == SHAPE
+    assert call(E=0) == SHAPE and call(E=(1 << 30) + 1) == SHAPE and call(n=1) == SHAPE and call(n=9) == SHAPE
     assert call(rows=None) == INVALID and call(rows=rows(m=-1)) == INVALID and call(rows=rows(m=1 << 31)) == SHAPE
     assert call(rows=rows(None, FAKE)) == INVALID and call(rows=rows(FAKE, FAKE, 8)) == INVALID
     assert call(dy=None) == INVALID and call(src=None) == INVALID and call(logits=None) == INVALID and call(gate=None) == INVALID
