@@ -165,7 +165,7 @@ __global__ __launch_bounds__((64 * GradPlan<X, Y, S, ROUTE>::MOST)) void norm_gr
                 d[i] = rstd * (h[c][i] * gm[c][i] - c0 - xh[c][i] * c1);
                 if (a.dres) d[i] += r.res[c][i];
             }
-            store_piece<X, VEC>(static_cast<X *>(a.dx) + (size_t)t * a.E + p.at[c], d);
+            stream_piece<X, VEC>(static_cast<X *>(a.dx) + (size_t)t * a.E + p.at[c], d);
         }
 #pragma unroll
         for (int e = 0; e < HELD; ++e) dl_sum[e] += r.dl[e];

@@ -100,7 +100,7 @@ __global__ __launch_bounds__(S::WIDE ? 512 : 64 * kNormWaves) void train_norm_ke
         for (int c = 0; c < CH; ++c) {
 #pragma unroll
             for (int i = 0; i < VEC; ++i) y[c][i] = __builtin_fmaf((x[c][i] - mean) * rstd, gm[c][i], bt[c][i]);
-            if (row_ok && (TRAIN || a.y)) store_piece<Y, VEC>(static_cast<Y *>(a.y) + (size_t)t * a.E + p.at[c], y[c]);
+            if (row_ok && (TRAIN || a.y)) stream_piece<Y, VEC>(static_cast<Y *>(a.y) + (size_t)t * a.E + p.at[c], y[c]);
         }
         if constexpr (HELD > 0) {
             float part[HELD];

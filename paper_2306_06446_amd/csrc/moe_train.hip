@@ -494,7 +494,7 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradArgs a) {
                     out[k] = gate * d[c][k];
                 }
                 // elements that two lanes hold are written by both, the same bits
-                if (a.dsrc) store_piece<X, VEC>(dsrc + at[c], out);
+                if (a.dsrc) stream_piece<X, VEC>(dsrc + at[c], out);
             }
         }
         if (!dot) continue;
