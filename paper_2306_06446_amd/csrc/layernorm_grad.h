@@ -5,8 +5,13 @@
 
 namespace sa {
 
+// Rows of which more are read than half of the memory-side cache are not worth a place in the caches: they cannot all be there from the
+// launches before, and this is their last use.  131072 x 1024 bf16 (805 MB read) 203 -> 189 us, 131072 x 200 bf16 (157 MB) 50.3 -> 49.4; but
+// 12608 x 768 (97 MB, partly there) 30.8 -> 32.8 and 7000 x 300 fp32 (25 MB) 12.5 -> 14.5.
+constexpr size_t kLargeRows = 128ull << 20;
+
 // What a lane holds of a row that is to come: asked for while the row before it is worked on.
-template <class X, class Y, class S, int ROUTE>
+template <class X, class Y, class S, int ROUTE, bool LARGE>
 struct GradRow {
     Piece<Y, S::VEC> dy[S::CH];
     Piece<X, S::VEC> x[S::CH], res[S::CH];
@@ -14,14 +19,18 @@ struct GradRow {
 
     __device__ inline void load(const NormGradArgs &a, const RowPlace<S> &p, long t) {
         const size_t row = (size_t)t * a.E;
+        auto fetch = [](auto &piece, const auto *from) {
+            if constexpr (LARGE) piece.stream(from);
+            else piece.load(from);
+        };
 #pragma unroll
         for (int c = 0; c < S::CH; ++c) {
-            dy[c].load(static_cast<const Y *>(a.dy) + row + p.at[c]);
-            x[c].load(static_cast<const X *>(a.x) + row + p.at[c]);
+            fetch(dy[c], static_cast<const Y *>(a.dy) + row + p.at[c]);
+            fetch(x[c], static_cast<const X *>(a.x) + row + p.at[c]);
         }
         if (a.dres) {
 #pragma unroll
-            for (int c = 0; c < S::CH; ++c) res[c].load(static_cast<const X *>(a.dres) + row + p.at[c]);
+            for (int c = 0; c < S::CH; ++c) fetch(res[c], static_cast<const X *>(a.dres) + row + p.at[c]);
         }
         if (a.mean) mean = a.mean[t], rstd = a.rstd[t];
         if constexpr (ROUTE > kStreamed) {
@@ -52,7 +61,7 @@ struct GradPlan {
     static constexpr int AT_ONCE = SIDE <= 8192 ? 4 : 2;
 };
 
-template <class X, class Y, class S, int ROUTE>
+template <class X, class Y, class S, int ROUTE, bool LARGE>
 __global__ __launch_bounds__((64 * GradPlan<X, Y, S, ROUTE>::MOST)) void norm_grad_kernel(NormGradArgs a) {
     using Plan = GradPlan<X, Y, S, ROUTE>;
     constexpr int VEC = S::VEC, CH = S::CH, HELD = Plan::HELD, Q = 2 + HELD;
@@ -68,7 +77,7 @@ __global__ __launch_bounds__((64 * GradPlan<X, Y, S, ROUTE>::MOST)) void norm_gr
     RowSums<S, 2> sums(red, p);
     const long stride = (long)gridDim.x * groups;
     auto clamped = [&](long t) { return t < a.T ? t : a.T - 1; };
-    GradRow<X, Y, S, ROUTE> nxt;
+    GradRow<X, Y, S, ROUTE, LARGE> nxt;
     long t0 = (long)blockIdx.x * groups;
     float gm[CH][VEC], w[PR][PC][VEC];
 #pragma unroll
@@ -87,7 +96,7 @@ __global__ __launch_bounds__((64 * GradPlan<X, Y, S, ROUTE>::MOST)) void norm_gr
 #pragma unroll
     for (int e = 0; e < PR; ++e) dl_sum[e] = 0.0f;
 
-    auto work = [&](const GradRow<X, Y, S, ROUTE> &r, long t, bool row_ok) {
+    auto work = [&](const GradRow<X, Y, S, ROUTE, LARGE> &r, long t, bool row_ok) {
         float mean = r.mean, rstd = r.rstd, s[2];
         if constexpr (S::WIDE) {
             // before the row's first barrier: dx may be in the place of any of them
@@ -175,7 +184,7 @@ __global__ __launch_bounds__((64 * GradPlan<X, Y, S, ROUTE>::MOST)) void norm_gr
     if constexpr (AHEAD) nxt.load(a, p, clamped(t0 + g));
     for (; t0 + groups <= a.T; t0 += stride) {
         if constexpr (!AHEAD) nxt.load(a, p, t0 + g);
-        const GradRow<X, Y, S, ROUTE> r = nxt;
+        const GradRow<X, Y, S, ROUTE, LARGE> r = nxt;
         if constexpr (AHEAD) nxt.load(a, p, clamped(t0 + g + stride));
         work(r, t0 + g, true);
     }
@@ -325,7 +334,11 @@ int launch_norm_grad_rows(const NormGradArgs &a, int *parts, hipStream_t st) {
                 if (rc != SA_OK) return rc;
             }
         }
-        norm_grad_kernel<X, Y, S, decltype(route)::value><<<dim3((unsigned)*parts), dim3((unsigned)threads), 0, st>>>(a);
+        const dim3 grid((unsigned)*parts), block((unsigned)threads);
+        if ((size_t)a.T * a.E * (sizeof(Y) + (a.dres ? 2 : 1) * sizeof(X)) > kLargeRows)
+            norm_grad_kernel<X, Y, S, decltype(route)::value, true><<<grid, block, 0, st>>>(a);
+        else
+            norm_grad_kernel<X, Y, S, decltype(route)::value, false><<<grid, block, 0, st>>>(a);
         return check_launch("sa_layernorm_backward(rows)");
     };
     auto with = [&](auto route) { return [&rows, route](auto shape) { return rows(shape, route); }; };

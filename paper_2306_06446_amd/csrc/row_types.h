@@ -18,12 +18,14 @@ struct Piece {
     typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
     vec v;
     __device__ inline void load(const T *p) { v = *reinterpret_cast<const vec *>(p); }
+    __device__ inline void stream(const T *p) { v = __builtin_nontemporal_load(reinterpret_cast<const vec *>(p)); }      // not for the caches to keep
     __device__ inline float operator[](int i) const { return (float)v[i]; }
 };
 template <class T>
 struct Piece<T, 1> {
     T v;
     __device__ inline void load(const T *p) { v = *p; }
+    __device__ inline void stream(const T *p) { v = *p; }
     __device__ inline float operator[](int) const { return (float)v; }
 };
 
