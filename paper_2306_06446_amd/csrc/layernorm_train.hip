@@ -3,6 +3,13 @@
 //   xh = (x - mean) rstd,  y = xh gamma + beta,  logits = y wg + bg
 //   h = dy + dlogits wg^T,  g = h gamma,  dx = dres + rstd (g - <g> - xh <g xh>),  <.> the mean over the row
 //   dgamma = sum_t h xh,  dbeta = sum_t h,  dwg = sum_t y dlogits,  dbg = sum_t dlogits
+//
+// The forward pass: a row stays in the registers of the lanes that share it (row_types.h), so x is read once: mean, centred squares, results.
+// What bounds it: memory, 4 to 8 bytes an element; a wavefront keeps a row ahead in flight and waits for no store.  Measured: 12608 x 768
+// fp32 to fp16 with the router of two 10.3 us (5.7 TB/s, part of it out of the memory-side cache; 37 as a workgroup to a row that reads it
+// three times), 100000 x 1024 bf16 73 us (5.6), 35714 x 5600 fp16 161 (4.9), 5003 x 4099 bf16, rows that begin anywhere, 18.5 (4.4).
+// Eight experts: 20000 x 768 30 us (3.1 TB/s), 20000 x 8000 bf16 211 (3.0): 8 fused multiplications an element and 96 to 128 weights in a lane's
+// registers leave two wavefronts to a SIMD.
 #include "layernorm_train.h"
 
 namespace sa {
