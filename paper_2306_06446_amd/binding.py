@@ -136,13 +136,11 @@ def _address(t, device, name, shape=None, dtype=None):
     the tensor, another device than the current one is not what the stream works on: refused, like what is not contiguous."""
     if t is None:
         return None
-    if t.get_device() != device or not t.is_contiguous():
-        raise ValueError("%s: a contiguous tensor on GPU %s is needed" % (name, device))
-    if shape is not None and t.shape != shape:
-        raise ValueError("%s: shape %s is needed, not %s" % (name, tuple(shape), tuple(t.shape)))
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError("%s: %s is needed, not %s" % (name, dtype, t.dtype))
-    return t.data_ptr()
+    if t.get_device() == device and t.is_contiguous() and (shape is None or t.shape == shape) and (dtype is None or t.dtype is dtype):
+        return t.data_ptr()
+    raise ValueError("%s: a contiguous tensor on GPU %s%s%s is needed, not %s of %s on %s" % (
+        name, device, "" if shape is None else " of shape %s" % (tuple(shape),), "" if dtype is None else ", %s," % dtype,
+        tuple(t.shape), t.dtype, t.device))
 
 
 def _current_device(t, name, dtypes, dims=2):
