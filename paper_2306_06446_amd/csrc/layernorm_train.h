@@ -77,10 +77,12 @@ int by_shape(int E, F &&f) {
     return by_wide_shape<VEC, FEW>(E, f);
 }
 // The gradient with a router of up to 8 experts: 8 elements to a lane, whose 64 weights and 64 sums are registers too.  Wider rows would
-// want more of them than there are.
+// want more of them than there are.  Up to 64 elements 4 to a lane, all sixteen at work: 131072 x 64 bf16 with eight 39.6 -> 32.9 us, fp32
+// 41.1 -> 36.5; 131072 x 33 fp16 with three 35.6 -> 25.6.
 template <int VEC, class F>
 int by_shape_route8(int E, F &&f) {
     if (E < VEC) return f(RowShape<1, 1, 16, 0>());
+    if (E <= 64) return f(RowShape<4, 1, 16, 0>());
     if (E <= 128) return f(RowShape<VEC, 8 / VEC, 16, 0>());
     if (E <= 256) return f(RowShape<VEC, 8 / VEC, 32, 0>());
     if (E <= 512) return f(RowShape<VEC, 8 / VEC, 64, 0>());
