@@ -533,6 +533,9 @@ struct RunCombineGrad {
             return check_launch("sa_combine_rows_backward");
         };
         if (a.E < VEC) return rows(RowShape<1, 1, 16, 0>());
+        // with 8 elements to a lane, half of the lanes or more would repeat what others do: 10^6 x 64 fp16 112 -> 109 us, 300000 x 17 28.7 -> 23.8
+        if constexpr (VEC == 8)
+            if (a.E <= 64) return rows(RowShape<4, 1, 16, 0>());
         if (a.E <= 16 * VEC) return rows(RowShape<VEC, 1, 16, 0>());
         if (a.E <= 32 * VEC) return rows(RowShape<VEC, 1, 32, 0>());
         if (a.E <= 64 * VEC) return rows(RowShape<VEC, 1, 64, 0>());
