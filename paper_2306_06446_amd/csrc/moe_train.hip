@@ -57,8 +57,9 @@ __device__ inline TokenRouting<E> route_token(const float (&v)[E], float inv_noi
         r.first = best ? e : r.first;
         l0 = best ? v[e] : l0;
     }
-    float den = 0.0f;
-    const float x1 = exp_of(l1 - l0);    // the largest one's exponential is 1
+    // of two experts, the largest one's exponential is 1; where it is infinite, l0 - l0 is the NaN that a softmax has there
+    float den = E == 2 ? l0 - l0 : 0.0f;
+    const float x1 = exp_of(l1 - l0);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         r.p[e] = E == 2 ? (e == r.first ? 1.0f : x1) : exp_of(v[e] - l0);
