@@ -637,9 +637,10 @@ def sa_combine_rows_backward(dy, src, rows=None, counts=None, expert=0, max_rows
     f32 = torch.float32
     if max_rows is None:
         max_rows = src.shape[0]
-    new = torch.empty if rows is None and counts is None and max_rows == T else torch.zeros
+    first_rows = rows is None and counts is None             # of dy's T rows and of src's, each may have more
     if dsrc is None and want_dsrc:
-        dsrc = new((src.shape[0], E), dtype=src.dtype, device=dev)
+        dsrc = (torch.empty if first_rows and max_rows == src.shape[0] else torch.zeros)((src.shape[0], E), dtype=src.dtype, device=dev)
+    new = torch.empty if first_rows and max_rows == T else torch.zeros
     if dgate is None:
         dgate = new(T, dtype=f32, device=dev)
     n = 0 if logits is None else logits.shape[1]
