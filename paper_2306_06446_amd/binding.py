@@ -650,6 +650,8 @@ def sa_combine_rows_backward(dy, src, rows=None, counts=None, expert=0, max_rows
         raise ValueError("src: %s is no type of rows" % src.dtype)
     if max_rows > src.shape[0] or (rows is None and max_rows > T) or (rows is not None and counts is None and max_rows > rows.numel()):
         raise ValueError("max_rows: %d rows are more than there are" % max_rows)
+    if counts is not None and not 0 <= expert < counts.numel():
+        raise ValueError("expert: %d is none of the %d that counts has" % (expert, counts.numel()))
     r = SaRows(_address(rows, dev, "rows", None, torch.int32), _address(counts, dev, "counts", None, torch.int32), expert, max_rows)
     _check(lib.sa_combine_rows_backward(
         _address(dy, dev, "dy"), _ROW_TYPES[dy.dtype], _address(src, dev, "src", (src.shape[0], E)), _ROW_TYPES[src.dtype], ctypes.byref(r),
