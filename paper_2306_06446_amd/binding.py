@@ -154,6 +154,21 @@ def _current_device(t, name, dtypes, dims=2):
     return index, torch._C._cuda_getCurrentRawStream(index)
 
 
+def _experts(t, name):
+    """The experts that a matrix of theirs has a column for, 0 without one."""
+    if t is None:
+        return 0
+    if t.dim() != 2:
+        raise ValueError("%s: 2 dimensions are needed, not %s" % (name, tuple(t.shape)))
+    return t.shape[1]
+
+
+def _row_type(dtype, name):
+    if dtype not in _ROW_TYPES:
+        raise ValueError("%s: %s is no type of rows" % (name, dtype))
+    return _ROW_TYPES[dtype]
+
+
 def _workspace(nbytes, device):
     return torch.empty(max(int(nbytes), 16), dtype=torch.uint8, device=device)
 
@@ -539,16 +554,17 @@ def sa_layernorm(x, gamma, beta, eps, y_dtype=None, want_y=True, want_stats=True
     lib = load_library()
     dev, stream = _current_device(x, "x", _ROW_TYPES)
     T, E = x.shape
+    y_dtype = y.dtype if y is not None else y_dtype if y_dtype and want_y else x.dtype
+    y_type = _row_type(y_dtype, "y")
     if y is None and want_y:
-        y = torch.empty((T, E), dtype=y_dtype or x.dtype, device=dev)
+        y = torch.empty((T, E), dtype=y_dtype, device=dev)
     if want_stats:
         mean = torch.empty(T, dtype=torch.float32, device=dev) if mean is None else mean
         rstd = torch.empty(T, dtype=torch.float32, device=dev) if rstd is None else rstd
-    n = 0 if wg is None else wg.shape[1]
+    n = _experts(wg, "wg")
     if logits is None and wg is not None:
         logits = torch.empty((T, n), dtype=torch.float32, device=dev)
     f32 = torch.float32
-    y_type = _ROW_TYPES[x.dtype if y is None else y.dtype]
     _check(lib.sa_layernorm(
         _address(x, dev, "x"), _ROW_TYPES[x.dtype], T, E, _address(gamma, dev, "gamma", (E,), f32), _address(beta, dev, "beta", (E,), f32),
         eps, _address(y, dev, "y", (T, E)), y_type, _address(mean, dev, "mean", (T,), f32), _address(rstd, dev, "rstd", (T,), f32),
@@ -568,7 +584,7 @@ def sa_layernorm_backward(dy, x, gamma, beta, eps, mean=None, rstd=None, dres=No
     dev, stream = _current_device(x, "x", _ROW_TYPES)
     T, E = x.shape
     f32 = torch.float32
-    n = 0 if dlogits is None else dlogits.shape[-1]
+    n = _experts(dlogits, "dlogits")
     if dx is None:
         dx = torch.empty_like(x)
     if want_params:
@@ -583,10 +599,9 @@ def sa_layernorm_backward(dy, x, gamma, beta, eps, mean=None, rstd=None, dres=No
         raise ValueError("want_params: buffers of parameter gradients are given, but none are wanted")
     if workspace is None and (want_params or (n > 2 and E > 2048)):
         workspace = _workspace(lib.sa_layernorm_backward_workspace_bytes(T, E, n), x.device)
-    if dy.dtype not in _ROW_TYPES:
-        raise ValueError("dy: %s is no type of rows" % dy.dtype)
+    y_type = _row_type(dy.dtype, "dy")
     _check(lib.sa_layernorm_backward(
-        _address(dy, dev, "dy", (T, E)), _ROW_TYPES[dy.dtype], _address(x, dev, "x"), _ROW_TYPES[x.dtype], T, E,
+        _address(dy, dev, "dy", (T, E)), y_type, _address(x, dev, "x"), _ROW_TYPES[x.dtype], T, E,
         _address(gamma, dev, "gamma", (E,), f32), _address(beta, dev, "beta", (E,), f32), eps, _address(mean, dev, "mean", (T,), f32),
         _address(rstd, dev, "rstd", (T,), f32), _address(dres, dev, "dres", (T, E), x.dtype), _address(dlogits, dev, "dlogits", (T, n), f32),
         _address(wg, dev, "wg", (E, n), f32) if n else None, n, _address(dx, dev, "dx", (T, E), x.dtype),
@@ -643,18 +658,17 @@ def sa_combine_rows_backward(dy, src, rows=None, counts=None, expert=0, max_rows
     new = torch.empty if first_rows and max_rows == T else torch.zeros
     if dgate is None:
         dgate = new(T, dtype=f32, device=dev)
-    n = 0 if logits is None else logits.shape[1]
+    n = _experts(logits, "logits")
     if dlogits is None and logits is not None:
         dlogits = new((T, n), dtype=f32, device=dev)
-    if src.dtype not in _ROW_TYPES:
-        raise ValueError("src: %s is no type of rows" % src.dtype)
+    src_type = _row_type(src.dtype, "src")
     if max_rows > src.shape[0] or (rows is None and max_rows > T) or (rows is not None and counts is None and max_rows > rows.numel()):
         raise ValueError("max_rows: %d rows are more than there are" % max_rows)
     if counts is not None and not 0 <= expert < counts.numel():
         raise ValueError("expert: %d is none of the %d that counts has" % (expert, counts.numel()))
     r = SaRows(_address(rows, dev, "rows", None, torch.int32), _address(counts, dev, "counts", None, torch.int32), expert, max_rows)
     _check(lib.sa_combine_rows_backward(
-        _address(dy, dev, "dy"), _ROW_TYPES[dy.dtype], _address(src, dev, "src", (src.shape[0], E)), _ROW_TYPES[src.dtype], ctypes.byref(r),
+        _address(dy, dev, "dy"), _ROW_TYPES[dy.dtype], _address(src, dev, "src", (src.shape[0], E)), src_type, ctypes.byref(r),
         _address(gate, dev, "gate", (T,), f32), _address(logits, dev, "logits", (T, n), f32), n, E,
         _address(dsrc, dev, "dsrc", src.shape, src.dtype), _address(dgate, dev, "dgate", (T,), f32),
         _address(dlogits, dev, "dlogits", (T, n), f32), stream))

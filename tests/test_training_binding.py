@@ -40,3 +40,29 @@ def test_combine_backward_refuses_counts_that_do_not_reach_the_expert(lib):
         with pytest.raises(ValueError):
             call(short, expert)
     assert len(lib.calls) == 3
+
+
+def test_layernorm_refuses_what_is_no_type_or_shape_of_its_arguments(lib):
+    """As other wrong arguments are refused: by a ValueError that names the argument."""
+    x, v = torch.zeros(4, 8), torch.zeros(8)
+    stats = dict(mean=torch.zeros(4), rstd=torch.zeros(4), dx=torch.zeros(4, 8), want_params=False)
+    binding.sa_layernorm(x, v, v, 1e-6, y=torch.zeros(4, 8), want_stats=False)
+    binding.sa_layernorm_backward(x, x, v, v, 1e-6, **stats)
+    binding.sa_layernorm(x, v, v, 1e-6, want_y=False, y_dtype=torch.float64, **{k: stats[k] for k in ("mean", "rstd")})      # of no rows
+    assert len(lib.calls) == 3
+    for f, name in ((lambda: binding.sa_layernorm(x, v, v, 1e-6, y=torch.zeros(4, 8).double(), want_stats=False), "y"),
+                    (lambda: binding.sa_layernorm(x, v, v, 1e-6, y=torch.zeros(4, 8, dtype=torch.int32), want_stats=False), "y"),
+                    (lambda: binding.sa_layernorm(x, v, v, 1e-6, y_dtype=torch.float64, want_stats=False), "y"),
+                    (lambda: binding.sa_layernorm(x, v, v, 1e-6, y=x.clone(), want_stats=False, wg=v, bg=v), "wg"),
+                    (lambda: binding.sa_layernorm_backward(x.double(), x, v, v, 1e-6, **stats), "dy"),
+                    (lambda: binding.sa_layernorm_backward(x, x, v, v, 1e-6, dlogits=torch.zeros(4), wg=torch.zeros(8, 4), **stats), "dlogits")):
+        with pytest.raises(ValueError, match="^%s:" % name):
+            f()
+    assert len(lib.calls) == 3
+
+
+def test_combine_backward_refuses_logits_of_one_dimension(lib):
+    x = torch.zeros(4, 8)
+    with pytest.raises(ValueError, match="^logits:"):
+        binding.sa_combine_rows_backward(x, x, gate=torch.ones(4), logits=torch.zeros(4), dsrc=x.clone(), dgate=torch.zeros(4))
+    assert not lib.calls
