@@ -391,7 +391,8 @@ int sa_layernorm_backward(const void *dy, int y_type, const void *x, int x_type,
  *   losses fp32 [2]; sums_or_null fp32 [2, E] = IMP then LOAD; counts_or_null int32 [E], tokens whose largest logit is the expert's
  *   (ties to the lowest index, as sa_moe_dispatch counts all tokens); dlogits [T, E] fp32.
  * accumulate != 0 adds the gradient to dlogits (where that of the combine is); dlogits must not be logits.  Where no token counts, or the mean of a loss is 0,
- * that loss and its gradient are 0.  2 <= E <= 8, 0 <= T < 2^31, noise_std > 0 with a finite reciprocal.  Sums over tokens are fp64 in a fixed order.
+ * that loss and its gradient are 0.  A logit of +infinity or NaN in a token that counts makes both losses and the gradient of all tokens that
+ * count NaN; -infinity shuts an expert.  2 <= E <= 8, 0 <= T < 2^31, noise_std > 0 with a finite reciprocal.  Sums over tokens are fp64 in a fixed order.
  */
 size_t sa_moe_balance_loss_grad_workspace_bytes(long T, int E);
 int sa_moe_balance_loss_grad(const float *logits, long T, int E, const uint8_t *valid_or_null, const float *alpha,

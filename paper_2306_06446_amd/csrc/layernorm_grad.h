@@ -4,10 +4,11 @@
 // those of its wavefronts up in LDS, and what it leaves (a part: 2 + n rows of E sums) a second launch adds up in fp64.  One workgroup to a
 // CU, or two of wide rows, so that parts are few: they are written and read again.
 // What bounds it: memory once rows are many (x, dy, dres in, dx out: 131072 x 1024 bf16 189 us, 5.7 TB/s; 25000 x 4000 bf16 150, 5.3;
-// 12608 x 768 fp16 under fp32 with the router of two 30.6 us, 4.4 TB/s over both launches).  Few rows: the two
-// launches' latency, 197 x 192 4.6 + 3.6 us on the device.
+// 12608 x 768 fp16 under fp32 with the router of two 30.7 us, 4.4 TB/s over both launches).  Few rows: the two
+// launches' latency, 197 x 192 4.6 + 3.6 us on the device.  Without statistics, which then are sums more over the row in hand, the same: 131072 x
+// 1024 189 us, 12608 x 768 34.0 against 34.1 with others' rows in the caches; 10 % more behind many experts.
 // Routers of 3 to 8 experts keep 8 elements to a lane (12608 x 768 54 us: no row ahead, and two wavefronts to a
-// SIMD); beyond 2048 columns the weights come from the caches for every row (20000 x 8000 bf16 with eight 520 to 550 us,
+// SIMD); beyond 2048 columns the weights come from the caches for every row (20000 x 8000 bf16 with eight 510 to 550 us,
 // of which dx 420, bound by the 256 KB of weights a row, their sums 87, the parts 28).
 #pragma once
 

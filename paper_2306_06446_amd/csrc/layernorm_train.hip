@@ -8,8 +8,10 @@
 // What bounds it: memory, 4 to 8 bytes an element; a wavefront keeps a row ahead in flight and waits for no store.  Measured: 12608 x 768
 // fp32 to fp16 with the router of two 10.3 us (5.7 TB/s, part of it out of the memory-side cache; 37 as a workgroup to a row that reads it
 // three times), 100000 x 1024 bf16 73 us (5.6), 35714 x 5600 fp16 161 (4.9), 5003 x 4099 bf16, rows that begin anywhere, 18.5 (4.4).
-// Eight experts: 20000 x 768 30 us (3.1 TB/s), 20000 x 8000 bf16 211 (3.0): 8 fused multiplications an element and 96 to 128 weights in a lane's
-// registers leave two wavefronts to a SIMD.
+// Eight experts: 20000 x 768 27 to 30 us (3.1 to 3.4 TB/s), 20000 x 8000 bf16 178 to 211 (3.0 to 3.6), 131072 x 64 bf16 16.4 (2.4): two
+// wavefronts to a SIMD are too few to hide memory behind.  Of rows from 769 elements on the weights take a lane's registers (96 to 128 of them),
+// of narrow ones the tile that they come through takes the LDS (67.6 KB whatever the width); the products themselves are few, 0.25 GFLOP of
+// 20000 x 768.
 #include "layernorm_train.h"
 
 namespace sa {
@@ -156,8 +158,10 @@ int launch_norm_rows(const NormArgs &a, hipStream_t st) {
     constexpr int VEC = row_vec<X, Y>();
     auto rows = [&](auto shape, auto route) {
         using S = decltype(shape);
-        // 16 wavefronts to a CU (as many as there is room for), 32 where several wait for each other at every row, 8 with the weights of
-        // many experts, each with as many rows as it takes
+        // 16 wavefronts to a CU, 32 where several wait for each other at every row (in two rounds where the registers have room for 16), 8
+        // with the weights of many experts, each with as many rows as it takes.  16 is as many as there is room for, up to 128 registers, but
+        // for rows of 16 elements to a lane, fp32 in, with a router of two and not all outputs: 129 to 131 registers, 12 wavefronts, and a
+        // second round for the rest.
         const int threads = S::threads(a.E, kNormWaves);
         const long groups = S::groups(a.E, kNormWaves), steps = (a.T + groups - 1) / groups;
         const long cap = 256 * (decltype(route)::value == kMaxExperts ? 512 : S::WIDE ? 2048 : 1024) / threads;

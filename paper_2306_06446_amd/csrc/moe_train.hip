@@ -7,13 +7,15 @@
 //   with c and f the gradients of the sums of p and q:  a = c + J^T (f phi(d) / std),  J p_i = p_i - p_o(i),  dl = p (a - <p, a>)
 //
 // The loss: every token's gradient needs the sums over all tokens, so logits are read twice, the second time out of the caches: a launch
-// that leaves sums of up to 512 parts in fp64, and one of which every workgroup adds those up.  What bounds it: latency, two launches
-// and a few loads that depend on each other; a million tokens of two experts 11.0 us (16 MB, 3.1 us at the card's rate), 131072 of eight
-// 10.4, of which the instructions of 8 exponentials, distributions and densities a token are some 3.  Up to 1024 tokens one workgroup does
-// all of it: 2.7 us on the device (two launches: 7).
+// that leaves sums of up to 512 parts in fp64, and one of which every workgroup adds those up.  What bounds it: latency.  A million tokens of
+// two experts 11.1 us (16 MB, 3.1 us at a copy's rate), 5.8 and 7.0 of the two launches on the device: some 5 are what two launches take in any
+// case, the rest is four tokens to a thread one behind the other, with one ahead under way.  131072 of eight 10.3, one token to a thread, of
+// which the instructions of 8 exponentials, distributions and densities are some 3.  Up to 1024 tokens one workgroup does all of it: 2.7 us on
+// the device (two launches: 7).
 //
 // The combine's gradient: one pass, a dot product and a product a row.  What bounds it: memory, 12608 x 768 fp16 under fp32 14.6 us
-// (5.3 TB/s), 50021 x 500 bf16, rows of 1000 bytes in the dispatch's order, 29.9 (5.1).
+// (5.3 TB/s), 50021 x 500 bf16, rows of 1000 bytes in the dispatch's order, 29.9 (5.1); fp32 throughout, as the experts here leave it,
+// 12608 x 768 23.9 (4.9), 131072 x 1024 292 (5.5).
 #include <type_traits>
 
 #include "common.h"
