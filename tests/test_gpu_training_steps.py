@@ -81,3 +81,7 @@ def test_sums_over_rows_of_wide_rows_behind_many_experts(sa, xt, yt, n, E, T, st
     s = inputs(T, E, xt, yt, n, E + n)
     mean, rstd = forward(sa, s, yt)
     backward(sa, s, mean, rstd, n, stats)
+
+
+def test_statistics_beyond_32_bits_of_elements(sa):
+    forward(sa, inputs(270001, 8192, BF16, BF16, 2, 2), BF16)        # 2.2e9 of them
