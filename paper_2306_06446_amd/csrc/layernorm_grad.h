@@ -2,7 +2,10 @@
 //
 // A row's two sums need all of it, a column's sums all rows: lanes keep their columns' sums in registers while rows go by, a workgroup adds
 // those of its wavefronts up in LDS, and what it leaves (a part: 2 + n rows of E sums) a second launch adds up in fp64.  One workgroup to a
-// CU, or two of wide rows, so that parts are few: they are written and read again.
+// CU, or two of wide rows, so that parts are few: they are written and read again.  Where a lane would add up more than 512 rows, a sum in fp32
+// loses what it is given once it has grown: launches of ranges of rows instead, each with its parts.  (More parts in one launch go over the
+// rows in as many strides: 2^25 x 64 fp16 3.14 -> 3.68 ms, in ranges 2.98; 300000 x 2500 bf16
+// with three experts, whose parts are twice as many, 2.03 -> 2.08.)
 // What bounds it: memory once rows are many (x, dy, dres in, dx out: 131072 x 1024 bf16 189 us, 5.7 TB/s; 25000 x 4000 bf16 150, 5.3;
 // 12608 x 768 fp16 under fp32 with the router of two 30.7 us, 4.4 TB/s over both launches).  Few rows: the two
 // launches' latency, 197 x 192 4.6 + 3.6 us on the device.  Without statistics, which then are sums more over the row in hand, the same: 131072 x
@@ -325,14 +328,29 @@ __global__ __launch_bounds__(256) void norm_grad_router_kernel(NormGradArgs a, l
     }
 }
 
+// The rows of a from `first` on, `count` of them, whose parts go behind `parts` others.
+template <class X, class Y>
+NormGradArgs some_rows(const NormGradArgs &a, long first, long count, int parts) {
+    NormGradArgs b = a;
+    const size_t at = (size_t)first * a.E;
+    b.T = count;
+    b.dy = static_cast<const Y *>(a.dy) + at, b.x = static_cast<const X *>(a.x) + at, b.dx = static_cast<X *>(a.dx) + at;
+    if (a.dres) b.dres = static_cast<const X *>(a.dres) + at;
+    if (a.mean) b.mean = a.mean + first, b.rstd = a.rstd + first;
+    if (a.dlogits) b.dlogits = a.dlogits + (size_t)first * a.n;
+    if (a.partial) {
+        b.partial = a.partial + (size_t)parts * (2 + a.n) * padded_columns(a.E);
+        b.partial_dbg = a.partial_dbg + (size_t)parts * kMaxExperts;
+    }
+    return b;
+}
+
 template <class X, class Y>
 int launch_norm_grad_rows(const NormGradArgs &a, int *parts, hipStream_t st) {
     constexpr int VEC = row_vec<X, Y>();
-    auto rows = [&](auto shape, auto route) {
+    const bool large = (size_t)a.T * a.E * (sizeof(Y) + (a.dres ? 2 : 1) * sizeof(X)) > kLargeRows;
+    auto range = [&](auto shape, auto route, const NormGradArgs &a, int waves, int *parts) {
         using S = decltype(shape);
-        using Plan = GradPlan<X, Y, S, decltype(route)::value>;
-        int waves = Plan::WAVES;                             // fewer where rows are, down to 4: more CUs have some
-        while (waves > 4 && (long)S::groups(a.E, waves) * 256 >= 2 * a.T) waves /= 2;
         const int threads = S::threads(a.E, waves);
         // two parts to a CU of workgroups of four, but 16 rows to a part or one to a CU; the same number of steps in each (12608 x 768 in
         // 226 workgroups 35.9 us, in 256 of which some have a step less 36.9)
@@ -349,11 +367,28 @@ int launch_norm_grad_rows(const NormGradArgs &a, int *parts, hipStream_t st) {
             }
         }
         const dim3 grid((unsigned)*parts), block((unsigned)threads);
-        if ((size_t)a.T * a.E * (sizeof(Y) + (a.dres ? 2 : 1) * sizeof(X)) > kLargeRows)
+        if (large)
             norm_grad_kernel<X, Y, S, decltype(route)::value, true><<<grid, block, 0, st>>>(a);
         else
             norm_grad_kernel<X, Y, S, decltype(route)::value, false><<<grid, block, 0, st>>>(a);
         return check_launch("sa_layernorm_backward(rows)");
+    };
+    auto rows = [&](auto shape, auto route) {
+        using S = decltype(shape);
+        using Plan = GradPlan<X, Y, S, decltype(route)::value>;
+        int waves = Plan::WAVES;                             // fewer where rows are, down to 4: more CUs have some
+        while (waves > 4 && (long)S::groups(a.E, waves) * 256 >= 2 * a.T) waves /= 2;
+        // ranges of which a lane adds up kMaxGradSteps rows at most; as a range is long wherever there are two, its parts are those of `most` here
+        const long most = (long)S::groups(a.E, waves) * (S::WIDE && S::threads(a.E, waves) <= 256 ? 512 : 256) * kMaxGradSteps;
+        const long ranges = (a.T + most - 1) / most, each = (a.T + ranges - 1) / ranges;
+        *parts = 0;
+        for (long first = 0; first < a.T; first += each) {
+            int more = 0;
+            const int rc = range(shape, route, some_rows<X, Y>(a, first, a.T - first < each ? a.T - first : each, *parts), waves, &more);
+            if (rc != SA_OK) return rc;
+            *parts += more;
+        }
+        return (int)SA_OK;
     };
     auto with = [&](auto route) { return [&rows, route](auto shape) { return rows(shape, route); }; };
     if (!a.dlogits) return by_shape<VEC, VEC == 4>(a.E, with(std::integral_constant<int, 0>()));

@@ -8,7 +8,8 @@
 namespace sa {
 
 constexpr int kMaxNormColumns = 8192;
-constexpr int kMaxGradParts = 512;           // workgroups whose sums over rows are added up by a second launch
+constexpr int kGradParts = 512;              // workgroups of a range of rows, whose sums a last launch adds up
+constexpr int kMaxGradSteps = 512;           // rows of a range that a lane adds up in fp32 (16384 of 0.1 would be off by 1.5e-4)
 
 struct NormArgs {
     const void *x;
@@ -43,7 +44,12 @@ struct NormGradArgs {
 
 __host__ __device__ inline int padded_columns(int E) { return (E + 3) / 4 * 4; }
 
-inline int max_grad_parts(long T) { return (int)(T < kMaxGradParts ? T : kMaxGradParts); }
+// The gradient's parts at most, of any types: a workgroup has 8 rows side by side at least where rows are narrow and this many, else one, and a
+// range has 512 parts of 512 times as many rows, or 256 of half of them.
+inline long max_grad_parts(long T, int E) {
+    const long rows = (long)kGradParts * kMaxGradSteps * (E <= 512 ? 8 : 1);
+    return T < kGradParts ? T : (T + rows - 1) / rows * kGradParts;
+}
 
 // ROUTE: experts whose weights a kernel holds in registers, the gradient with their sums (0, 2 or kMaxExperts); kStreamed: the gradient
 // has the weights from memory row by row, and the sums come of a launch of their own.

@@ -184,11 +184,12 @@ namespace {
 
 using namespace sa;
 
-// The parts' sums in fp64, in a fixed order: 64 threads to four columns, whose loads (8 to a thread at most) are all in flight at once.
+// The parts' sums in fp64, in a fixed order: 64 threads to four columns, whose loads (8 to a thread) are all in flight at once, for up to 512
+// parts at a time.
 constexpr int kSumColumns = 16;              // of a workgroup
 __global__ __launch_bounds__(256) void norm_grad_sum_kernel(NormGradArgs a, int parts) {
     constexpr int kSlices = 256 / (kSumColumns / 4);
-    constexpr int kEach = kMaxGradParts / kSlices;
+    constexpr int kEach = kGradParts / kSlices;
     __shared__ double red[4][kSumColumns];
     const int n = a.dlogits ? a.n : 0, columns = padded_columns(a.E), all = (2 + n) * columns;
     const int slice = threadIdx.x / 4, quad = threadIdx.x & 3, at = (int)blockIdx.x * kSumColumns + quad * 4;
@@ -198,15 +199,17 @@ __global__ __launch_bounds__(256) void norm_grad_sum_kernel(NormGradArgs a, int 
     bool any = at < all;
     if (any) from += at;
     else if (last && quad >= 2 && a.dbg) any = true, from = a.partial_dbg + (quad - 2) * 4, step = kMaxExperts;
-    float4 v[kEach];
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-        const int part = slice + k * kSlices;
-        v[k] = any && part < parts ? *reinterpret_cast<const float4 *>(from + part * step) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    }
     double s[4] = {0.0, 0.0, 0.0, 0.0};
+    for (int first = 0; first < parts; first += kGradParts) {
+        float4 v[kEach];
 #pragma unroll
-    for (int k = 0; k < kEach; ++k) s[0] += v[k].x, s[1] += v[k].y, s[2] += v[k].z, s[3] += v[k].w;
+        for (int k = 0; k < kEach; ++k) {
+            const int part = first + slice + k * kSlices;
+            v[k] = any && part < parts ? *reinterpret_cast<const float4 *>(from + part * step) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) s[0] += v[k].x, s[1] += v[k].y, s[2] += v[k].z, s[3] += v[k].w;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
 #pragma unroll
@@ -241,7 +244,7 @@ bool needs_weights(int E, int n) { return n > 2 && E > kMaxRoute8Columns; }
 GradLayout grad_layout(long T, int E, int n, bool params) {
     GradLayout L;
     auto up = [](size_t bytes) { return (bytes + 255) / 256 * 256; };
-    const size_t parts = params ? (size_t)max_grad_parts(T) : 0, columns = (size_t)padded_columns(E);
+    const size_t parts = params ? (size_t)max_grad_parts(T, E) : 0, columns = (size_t)padded_columns(E);
     const bool streamed = needs_weights(E, n);
     L.partial = 0;
     L.dbg = up(parts * (2 + n) * columns * 4);

@@ -35,9 +35,9 @@ def forward(sa, s, yt):
     return mean, rstd
 
 
-def backward(sa, s, mean, rstd, n, stats):
+def backward(sa, s, mean, rstd, n, stats, **kw):
     got = sa.sa_layernorm_backward(s["dy"], s["x"], s["gamma"], s["beta"], EPS, mean=mean if stats else None, rstd=rstd if stats else None,
-                                   dres=s["dres"], dlogits=s.get("dlogits"), wg=s.get("wg"))
+                                   dres=s["dres"], dlogits=s.get("dlogits"), wg=s.get("wg"), **kw)
     dy, x, gamma, beta, dres, dlogits, wg = doubles(s, "dy", "x", "gamma", "beta", "dres", "dlogits", "wg")
     mean, rstd = (mean.double(), rstd.double()) if stats else tf.norm(x, gamma, beta, EPS)[1:3]
     args = (dy, x, gamma, beta, mean, rstd, dres, dlogits, wg)
@@ -85,3 +85,32 @@ def test_sums_over_rows_of_wide_rows_behind_many_experts(sa, xt, yt, n, E, T, st
 
 def test_statistics_beyond_32_bits_of_elements(sa):
     forward(sa, inputs(270001, 8192, BF16, BF16, 2, 2), BF16)        # 2.2e9 of them
+
+
+@pytest.mark.parametrize("T", [(1 << 28) + 5, (1 << 23) + 77, 40000])
+def test_sums_over_very_many_rows_of_one_sign(sa, T):
+    """As a loss that is a plain sum has them: what a row adds is small against what there is, and rounded the same way again and again.  A lane
+    adds up 512 rows in fp32 at most, a workgroup's 64 groups of lanes follow, the parts are fp64."""
+    f = lambda *v: torch.tensor(v, device="cuda")      # noqa: E731
+    x, dy, dl = f(1.0, -1.0).repeat(T, 1), torch.full((T, 2), 0.1, device="cuda"), torch.full((T, 2), 0.3, device="cuda")
+    gamma, beta = f(1.0, 2.0), f(0.5, -3.0)
+    _, dgamma, dbeta, dwg, dbg = sa.sa_layernorm_backward(dy, x, gamma, beta, EPS, dlogits=dl, wg=torch.zeros(2, 2, device="cuda"))
+    c, d = float(dy[0, 0]), float(dl[0, 0])
+    xh = f(1.0, -1.0).double() / (1.0 + EPS) ** 0.5
+    y = gamma.double() * xh + beta.double()
+    size = (gamma.double() * xh).abs() + beta.double().abs()             # both parts of y by themselves
+    bound = (512 + 64 + 8) * tf.U * T                       # and what makes a row's summands: xh, two products, the output
+    for got, want, of in ((dgamma, T * c * xh, c * xh.abs()), (dbeta, T * c * torch.ones_like(xh), c * torch.ones_like(xh)),
+                          (dwg, (T * d * y)[:, None].repeat(1, 2), (d * size)[:, None].repeat(1, 2)),
+                          (dbg, T * d * torch.ones_like(xh), d * torch.ones_like(xh))):
+        err = (got.double() - want).abs()
+        assert bool((err <= bound * of).all()), (err / want.abs() / tf.U)
+
+
+@pytest.mark.parametrize("xt,yt,E,n,T", [(BF16, BF16, 2049, 3, 300000), (F16, F16, 2051, 0, 300000), (F32, BF16, 1026, 2, 530000)], ids=str)
+def test_sums_over_more_rows_than_parts_of_512(sa, xt, yt, E, n, T):
+    s = inputs(T, E, xt, yt, n, 3)
+    need = sa.sa_layernorm_backward_workspace_bytes(T, E, n)
+    ws = torch.full((need + 1024,), 7, dtype=torch.uint8, device="cuda")
+    backward(sa, s, *sa.sa_layernorm(s["x"], s["gamma"], s["beta"], EPS)[1:3], n, True, workspace=ws[:need])
+    assert bool((ws[need:] == 7).all())
