@@ -488,8 +488,9 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradArgs a) {
         const Y *dy = static_cast<const Y *>(a.dy) + r * a.E;
         const X *src = static_cast<const X *>(a.src) + (size_t)i * a.E;
         X *dsrc = static_cast<X *>(a.dsrc) + (size_t)i * a.E;
-        float s = 0.0f;
+        double blocks = 0.0;                 // a sum in fp32 loses what it is given once it has grown
         for (int j0 = 0; j0 < a.E; j0 += COLUMNS) {
+            float s = 0.0f;
             Piece<Y, VEC> d[CH];
             Piece<X, VEC> v[CH];
             int at[CH], skip[CH];
@@ -512,9 +513,10 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(CombineGradArgs a) {
                 // elements that two lanes hold are written by both, the same bits
                 if (a.dsrc) stream_piece<X, VEC>(dsrc + at[c], out);
             }
+            blocks += (double)s;
         }
         if (!dot) continue;
-        s = group_sum<S::LANES>(s);
+        const float s = group_sum<S::LANES>((float)blocks);
         if (a.dgate && l == 0) a.dgate[r] = s;
         if (a.dlogits) {
             // p_first = 1 / den, the largest exponent being 0

@@ -53,3 +53,14 @@ def test_load_of_experts_that_are_hardly_ever_chosen(sa, T, n, std):
     bound = 1.01 * (q * rel).sum(0) / n + tf.U * want + 2.0 ** -126      # what is below the smallest normal number is 0
     err = (got - want).abs()
     assert bool((err <= bound).all()), (err / want, bound / want)
+
+
+@pytest.mark.parametrize("E", [768, 4099, (1 << 18) + 5, (1 << 24) + 3])
+@pytest.mark.parametrize("yt,st", [(torch.float32, torch.float32), (torch.float32, torch.float16), (torch.bfloat16, torch.bfloat16)], ids=str)
+def test_gate_of_long_rows_of_one_sign(sa, yt, st, E):
+    """A dot product whose terms are all alike: what is added is rounded the same way again and again where it is small against the sum.
+    Here 8 terms at a time are added up in fp32, those sums in fp64, and the up to 64 lanes' in fp32."""
+    dy, src = torch.full((3, E), 0.3, device="cuda").to(yt), torch.full((3, E), 0.7, device="cuda").to(st)
+    dgate = sa.sa_combine_rows_backward(dy, src, want_dsrc=False)[1]
+    want = E * float(dy[0, 0]) * float(src[0, 0])
+    assert bool(((dgate.double() - want).abs() <= (8 + 1 + 6) * tf.U * want).all()), (dgate.double() / want - 1) / tf.U
