@@ -134,6 +134,50 @@ int sa_linear_attention_01(const uint64_t *q_codes, const uint64_t *k_codes, con
                            void *stream);
 
 /*
+ * Linear attention in the order of the tokens, with a decay for each head: the form of Q(K^T V) for sequences that are read one token after
+ * the other.  For each sequence and key/value head, from S_{-1} = state_in (or zeros):
+ *   S_t = exp(log_decay) * S_{t-1} + k_t v_t^T,   out_t = scale * q_t^T S_t,   state_out = S of the last token
+ *   q [T, H, d], k [T, Hk, d], v [T, Hk, dv], out [T, H, dv], all of one type (SA_F32, SA_F16, SA_BF16); token t's heads begin at element
+ *   t * stride and follow each other densely: a tensor's own rows (stride heads * width), or a block of columns of wider ones, as a fused
+ *   projection leaves them.  H is a multiple of Hk: heads h * H / Hk to (h + 1) * H / Hk - 1 share the keys, values and state of head h.
+ *   log_decay fp32 [Hk], 0 or less (-infinity: a head that sees its own token only).
+ * Tokens of B sequences lie one behind the other: T / B of each, or, with offsets_or_null int32 [B + 1] ascending from 0 to T (in device memory),
+ * those from offsets[b] to offsets[b + 1] - 1; a sequence may be empty.  Rows of out that no sequence has are left as they are.
+ *   state_in_or_null, state_out_or_null fp32 [places, Hk, d, dv]: sequence b has place b, or, with slots_or_null int32 [B], place slots[b] of
+ *   n_slots; a sequence whose slot is none of them begins with zeros and leaves no state.  The two may be the same memory; a slot may be
+ *   named once only.  An empty sequence leaves the state it began with.
+ * d and dv are multiples of 8, up to 128; B * Hk <= 65535.  Rows begin at multiples of 16 bytes.  Sums and states are fp32 in a fixed order (the
+ * same call gives the same bits), q, k and v enter them exactly and out is rounded once.  An infinity or NaN in a token makes results
+ * of its sequence NaN from 63 tokens before it on.  out may not overlap an input.
+ * The workspace is as long as sequences and heads are too few to fill the GPU (the query returns 0 otherwise); offsets count as ragged.
+ */
+size_t sa_decay_attention_workspace_bytes(long T, int B, int H, int Hk, int d, int dv, int ragged);
+int sa_decay_attention(const void *q, long q_stride, const void *k, long k_stride, const void *v, long v_stride, int type,
+                       const float *log_decay, long T, int B, const int32_t *offsets_or_null, int H, int Hk, int d, int dv, float scale,
+                       const float *state_in_or_null, float *state_out_or_null, const int32_t *slots_or_null, int n_slots, void *out,
+                       long out_stride, void *workspace, size_t workspace_bytes, void *stream);
+/*
+ * The same for one token of each of B sequences: the step of a decoder.  q [B, H, d], k [B, Hk, d], v [B, Hk, dv], out [B, H, dv] with a row's
+ * stride each, states and slots as above, both states needed (in place where they are the same memory).  Other slots' states are not touched.
+ */
+int sa_decay_attention_step(const void *q, long q_stride, const void *k, long k_stride, const void *v, long v_stride, int type,
+                            const float *log_decay, long B, int H, int Hk, int d, int dv, float scale, const float *state_in,
+                            float *state_out, const int32_t *slots_or_null, int n_slots, void *out, long out_stride, void *stream);
+/*
+ * The gradient of sa_decay_attention for constant decays, from dout (as out) and that of state_out:
+ *   R_t = exp(log_decay) * R_{t+1} + scale * q_t dout_t^T   (summed over the heads that share a state; behind the last token: dstate_out or zeros)
+ *   dq_t = scale * S_t dout_t,   dk_t = R_t v_t,   dv_t = R_t^T k_t,   dstate_in = exp(log_decay) * R_0
+ * dq, dk, dv as q, k and v, of the same type; state_in_or_null as in the forward call (S is computed again), dstate_out_or_null and
+ * dstate_in_or_null fp32 [B, Hk, d, dv].  No output may overlap an input or another output.  Sequences, types and sizes as above.
+ */
+size_t sa_decay_attention_backward_workspace_bytes(long T, int B, int H, int Hk, int d, int dv, int ragged);
+int sa_decay_attention_backward(const void *dout, long dout_stride, const void *q, long q_stride, const void *k, long k_stride,
+                                const void *v, long v_stride, int type, const float *log_decay, long T, int B,
+                                const int32_t *offsets_or_null, int H, int Hk, int d, int dv, float scale, const float *state_in_or_null,
+                                const float *dstate_out_or_null, void *dq, long dq_stride, void *dk, long dk_stride, void *dv_rows,
+                                long dv_stride, float *dstate_in_or_null, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Depthwise 3x3 convolution over the token grid of the V branch (Sec. 4.1: a
  * light depthwise convolution on V in parallel to the attention), stride 1,
  * zero padding:  v, out fp32 [B, gh, gw, E] (tokens row-major over the grid,

@@ -31,6 +31,8 @@ EXPORTS = [
     "sa_block_forward", "sa_moe_linear_workspace_bytes", "sa_moe_linear", "sa_probe_mfma", "sa_layer_workspace_bytes", "sa_layer_forward",
     "sa_layernorm", "sa_layernorm_backward_workspace_bytes", "sa_layernorm_backward", "sa_moe_balance_loss_grad_workspace_bytes",
     "sa_moe_balance_loss_grad", "sa_combine_rows_backward",
+    "sa_decay_attention_workspace_bytes", "sa_decay_attention", "sa_decay_attention_step",
+    "sa_decay_attention_backward_workspace_bytes", "sa_decay_attention_backward",
 ]
 
 _ROW_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}      # SA_F32, SA_F16, SA_BF16
@@ -94,6 +96,11 @@ def load_library():
         lib.sa_layernorm_backward.argtypes = (P, I, P, I, L, I, P, P, F, P, P, P, P, P, I, P, P, P, P, P, I, P, Z, P)
         lib.sa_moe_balance_loss_grad.argtypes = (P, L, I, P, P, F, P, P, P, P, P, I, P, Z, P)
         lib.sa_combine_rows_backward.argtypes = (P, I, P, I, P, P, P, I, I, P, P, P, P)
+        for name in ("sa_decay_attention_workspace_bytes", "sa_decay_attention_backward_workspace_bytes"):
+            getattr(lib, name).restype, getattr(lib, name).argtypes = Z, (L, I, I, I, I, I, I)
+        lib.sa_decay_attention.argtypes = (P, L, P, L, P, L, I, P, L, I, P, I, I, I, I, F, P, P, P, I, P, L, P, Z, P)
+        lib.sa_decay_attention_step.argtypes = (P, L, P, L, P, L, I, P, L, I, I, I, I, F, P, P, P, I, P, L, P)
+        lib.sa_decay_attention_backward.argtypes = (P, L, P, L, P, L, P, L, I, P, L, I, P, I, I, I, I, F, P, P, P, L, P, L, P, L, P, P, Z, P)
         _lib = lib
     return _lib
 
@@ -673,6 +680,140 @@ def sa_combine_rows_backward(dy, src, rows=None, counts=None, expert=0, max_rows
         _address(dsrc, dev, "dsrc", src.shape, src.dtype), _address(dgate, dev, "dgate", (T,), f32),
         _address(dlogits, dev, "dlogits", (T, n), f32), stream))
     return dsrc, dgate, dlogits
+
+
+def _heads(t, device, name, shape, dtype):
+    """The address of tokens' heads, [B, N, heads, width] or [T, heads, width], and the elements from token to token: a token's heads are
+    dense, tokens may be rows of a wider matrix."""
+    if t.get_device() != device or t.shape != shape or t.dtype is not dtype:
+        raise ValueError("%s: a tensor on GPU %s of shape %s, %s, is needed, not %s of %s on %s" % (
+            name, device, tuple(shape), dtype, tuple(t.shape), t.dtype, t.device))
+    if t.is_contiguous():
+        return t.data_ptr(), shape[-2] * shape[-1]
+    strides, (heads, width) = t.stride(), shape[-2:]
+    stride, tokens = heads * width, 1
+    for n, s in zip(reversed(shape[:-2]), reversed(strides[:-2])):
+        if n > 1 and tokens == 1:
+            stride = s
+        elif n > 1 and s != tokens * stride:
+            stride = -1
+            break
+        tokens *= n
+    if strides[-1] != 1 or (heads > 1 and strides[-2] != width) or stride < heads * width:
+        raise ValueError("%s: heads that are dense and tokens at one distance are needed, not strides %s of %s" % (name, strides, tuple(shape)))
+    return t.data_ptr(), stride
+
+
+def _sequences(q, k, v, offsets, device):
+    """(tokens' dimensions, T, B, H, Hk, d, dv) of q, k and v."""
+    if k.dim() != q.dim() or v.dim() != q.dim():
+        raise ValueError("k, v: %d dimensions are needed, as q has" % q.dim())
+    lead = tuple(q.shape[:-2])
+    if offsets is not None:
+        if offsets.dim() != 1 or offsets.numel() < 1:
+            raise ValueError("offsets: one dimension of B + 1 are needed, not %s" % (tuple(offsets.shape),))
+        _address(offsets, device, "offsets", None, torch.int32)
+        T, B = lead[0], offsets.numel() - 1
+    else:
+        T, B = lead[0] * lead[1], lead[0]
+    return lead, T, B, q.shape[-2], k.shape[-2], q.shape[-1], v.shape[-1]
+
+
+def _states(name, t, device, places, Hk, d, dv):
+    """The address of a buffer of states."""
+    return _address(t, device, name, (places, Hk, d, dv), torch.float32)
+
+
+def _slots(slots, B, device, *states):
+    """The slots' address and how many places the states have: one size for all of them."""
+    if slots is None:
+        return None, B
+    sizes = {s.shape[0] for s in states if s is not None and s.dim() == 4}
+    if len(sizes) > 1:
+        raise ValueError("state_in, state_out: one number of places is needed, not %s" % sorted(sizes))
+    return _address(slots, device, "slots", (B,), torch.int32), sizes.pop() if sizes else 0
+
+
+def sa_decay_attention_workspace_bytes(T, B, H, Hk, d, dv, ragged=False):
+    return load_library().sa_decay_attention_workspace_bytes(T, B, H, Hk, d, dv, int(bool(ragged)))
+
+
+def sa_decay_attention(q, k, v, log_decay, scale, offsets=None, state_in=None, slots=None, want_state=False, out=None, state_out=None,
+                       workspace=None):
+    """Causal linear attention with a decay for each key/value head: returns (out, state_out), state_out None where neither it is given nor
+    want_state.  q [B, N, H, d], k [B, N, Hk, d], v [B, N, Hk, dv], or, with offsets int32 [B + 1], sequences one behind the other:
+    [T, heads, width].  state_in, state_out [B, Hk, d, dv], or the places of a cache of which sequence b has number slots[b]; state_out may be
+    state_in."""
+    lib = load_library()
+    dev, stream = _current_device(q, "q", _ROW_TYPES, 4 if offsets is None else 3)
+    lead, T, B, H, Hk, d, dv = _sequences(q, k, v, offsets, dev)
+    if state_out is None and want_state:
+        if slots is not None:
+            raise ValueError("want_state: the cache that the slots belong to is needed as state_out")
+        state_out = torch.empty((B, Hk, d, dv), dtype=torch.float32, device=dev)
+    slots_at, places = _slots(slots, B, dev, state_in, state_out)
+    if out is None:
+        out = (torch.empty if offsets is None else torch.zeros)(lead + (H, dv), dtype=q.dtype, device=dev)
+    if workspace is None:
+        workspace = _workspace(lib.sa_decay_attention_workspace_bytes(T, B, H, Hk, d, dv, int(offsets is not None)), q.device)
+    _check(lib.sa_decay_attention(
+        *_heads(q, dev, "q", lead + (H, d), q.dtype), *_heads(k, dev, "k", lead + (Hk, d), q.dtype), *_heads(v, dev, "v", lead + (Hk, dv), q.dtype),
+        _ROW_TYPES[q.dtype], _address(log_decay, dev, "log_decay", (Hk,), torch.float32), T, B, None if offsets is None else offsets.data_ptr(),
+        H, Hk, d, dv, scale, _states("state_in", state_in, dev, places, Hk, d, dv), _states("state_out", state_out, dev, places, Hk, d, dv),
+        slots_at, places, *_heads(out, dev, "out", lead + (H, dv), q.dtype), _address(workspace, dev, "workspace"),
+        workspace.numel() * workspace.element_size(), stream))
+    return out, state_out
+
+
+def sa_decay_attention_step(q, k, v, log_decay, scale, state_in, slots=None, out=None, state_out=None):
+    """sa_decay_attention for one token of each sequence: q [B, H, d], k [B, Hk, d], v [B, Hk, dv]; returns (out, state_out).  The states
+    are changed in place where no state_out is given."""
+    lib = load_library()
+    dev, stream = _current_device(q, "q", _ROW_TYPES, 3)
+    if k.dim() != 3 or v.dim() != 3:
+        raise ValueError("k, v: 3 dimensions are needed")
+    (B, H, d), Hk, dv = q.shape, k.shape[1], v.shape[2]
+    if state_out is None:
+        state_out = state_in
+    slots_at, places = _slots(slots, B, dev, state_in, state_out)
+    if out is None:
+        out = torch.empty((B, H, dv), dtype=q.dtype, device=dev)
+    _check(lib.sa_decay_attention_step(
+        *_heads(q, dev, "q", (B, H, d), q.dtype), *_heads(k, dev, "k", (B, Hk, d), q.dtype), *_heads(v, dev, "v", (B, Hk, dv), q.dtype),
+        _ROW_TYPES[q.dtype], _address(log_decay, dev, "log_decay", (Hk,), torch.float32), B, H, Hk, d, dv, scale,
+        _states("state_in", state_in, dev, places, Hk, d, dv), _states("state_out", state_out, dev, places, Hk, d, dv), slots_at, places,
+        *_heads(out, dev, "out", (B, H, dv), q.dtype), stream))
+    return out, state_out
+
+
+def sa_decay_attention_backward_workspace_bytes(T, B, H, Hk, d, dv, ragged=False):
+    return load_library().sa_decay_attention_backward_workspace_bytes(T, B, H, Hk, d, dv, int(bool(ragged)))
+
+
+def sa_decay_attention_backward(dout, q, k, v, log_decay, scale, offsets=None, state_in=None, dstate_out=None, want_dstate=False, dq=None,
+                                dk=None, dv=None, dstate_in=None, workspace=None):
+    """Gradient of sa_decay_attention for constant decays: returns (dq, dk, dv, dstate_in), dstate_in None where neither it is given nor
+    want_dstate.  state_in as the forward call had it ([B, Hk, d, dv]), dstate_out the gradient of its state_out, None for zeros."""
+    lib = load_library()
+    dev, stream = _current_device(q, "q", _ROW_TYPES, 4 if offsets is None else 3)
+    lead, T, B, H, Hk, d, width = _sequences(q, k, v, offsets, dev)
+    new = torch.empty if offsets is None else torch.zeros
+    dq = new(lead + (H, d), dtype=q.dtype, device=dev) if dq is None else dq
+    dk = new(lead + (Hk, d), dtype=q.dtype, device=dev) if dk is None else dk
+    dv = new(lead + (Hk, width), dtype=q.dtype, device=dev) if dv is None else dv
+    if dstate_in is None and want_dstate:
+        dstate_in = torch.empty((B, Hk, d, width), dtype=torch.float32, device=dev)
+    if workspace is None:
+        workspace = _workspace(lib.sa_decay_attention_backward_workspace_bytes(T, B, H, Hk, d, width, int(offsets is not None)), q.device)
+    _check(lib.sa_decay_attention_backward(
+        *_heads(dout, dev, "dout", lead + (H, width), q.dtype), *_heads(q, dev, "q", lead + (H, d), q.dtype),
+        *_heads(k, dev, "k", lead + (Hk, d), q.dtype), *_heads(v, dev, "v", lead + (Hk, width), q.dtype), _ROW_TYPES[q.dtype],
+        _address(log_decay, dev, "log_decay", (Hk,), torch.float32), T, B, None if offsets is None else offsets.data_ptr(), H, Hk, d, width, scale,
+        _states("state_in", state_in, dev, B, Hk, d, width), _states("dstate_out", dstate_out, dev, B, Hk, d, width),
+        *_heads(dq, dev, "dq", lead + (H, d), q.dtype), *_heads(dk, dev, "dk", lead + (Hk, d), q.dtype),
+        *_heads(dv, dev, "dv", lead + (Hk, width), q.dtype), _states("dstate_in", dstate_in, dev, B, Hk, d, width),
+        _address(workspace, dev, "workspace"), workspace.numel() * workspace.element_size(), stream))
+    return dq, dk, dv, dstate_in
 
 
 class Block:
