@@ -28,17 +28,19 @@ template <> struct Terms<f16_t> { static constexpr int RAW = 2, MADE = 2, ORDER_
 template <> struct Terms<float> { static constexpr int RAW = 3, MADE = 3, ORDER_RAW = 2, ORDER = 2; };
 constexpr int kUpdateTerms = 3, kUpdateOrder = 2;
 
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+
 template <int N, class V, int W>
 __device__ inline void split(const float (&x)[W], V (&t)[N]) {
-    float r[W];
 #pragma unroll
-    for (int i = 0; i < W; ++i) r[i] = x[i];
+    for (int i = 0; i < W; i += 2) {
+        f2 r = {x[i], x[i + 1]};
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            t[n][i] = (__bf16)r[i];
-            if (n + 1 < N) r[i] -= (float)t[n][i];
+        for (int n = 0; n < N; ++n) {
+            const b2 h = __builtin_convertvector(r, b2);     // one instruction for two values
+            t[n][i] = h[0], t[n][i + 1] = h[1];
+            if (n + 1 < N) r[0] -= (float)h[0], r[1] -= (float)h[1];
         }
     }
 }
@@ -64,23 +66,35 @@ __device__ inline b4 read_transposed(const __bf16 *p) {
 }
 __device__ inline b8 join(const b4 &a, const b4 &b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
+// Rows of one head, from memory: a base that all lanes share and a 32-bit offset each.  What lies beyond kReach (an offset made kNowhere)
+// reads as zeros and is not written, without a branch.
+constexpr uint32_t kReach = 0x7fffffffu, kNowhere = 0x80000000u;
+__device__ inline __amdgpu_buffer_rsrc_t buffer(const void *p) {
+    const uint64_t u = reinterpret_cast<uint64_t>(p);
+    // (the builtin's result is signed: a low half of 2^31 or more would set all of the high one)
+    const uint32_t high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32)), low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)u);
+    const uint64_t at = (uint64_t)high << 32 | low;
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(at), 0, (int)kReach, 0x00027000);
+}
+
 // 8 elements on their way from memory to LDS.
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 template <class T>
 struct Eight {
-    T v[8];
-    __device__ inline void load(const T *p) {
-        typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<u4 *>(v)[i] = reinterpret_cast<const u4 *>(p)[i];
-    }
-    __device__ inline void zero() {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (T)0.0f;
+    typedef T vec __attribute__((ext_vector_type(8)));
+    vec v;
+    __device__ inline void load(__amdgpu_buffer_rsrc_t from, uint32_t at) {
+        if constexpr (sizeof(T) == 2) {
+            v = __builtin_bit_cast(vec, __builtin_amdgcn_raw_buffer_load_b128(from, (int)at, 0, 0));
+        } else {
+            struct { u4 a, b; } x = {__builtin_amdgcn_raw_buffer_load_b128(from, (int)at, 0, 0), __builtin_amdgcn_raw_buffer_load_b128(from, (int)at, 16, 0)};
+            v = __builtin_bit_cast(vec, x);
+        }
     }
     template <int N>
     __device__ inline void terms(b8 (&t)[N]) const {
         if constexpr (sizeof(T) == 2 && N == 1) {
-            t[0] = __builtin_bit_cast(b8, *this);
+            t[0] = __builtin_bit_cast(b8, v);
         } else {
             float x[8];
 #pragma unroll
@@ -89,6 +103,20 @@ struct Eight {
         }
     }
 };
+template <class T>
+__device__ inline void store_eight(__amdgpu_buffer_rsrc_t to, uint32_t at, const float (&x)[8]) {
+    typename Eight<T>::vec v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = rounded<T>(x[i]);
+    if constexpr (sizeof(T) == 2) {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, v), to, (int)at, 0, 0);
+    } else {
+        struct Two { u4 a, b; };
+        const Two w = __builtin_bit_cast(Two, v);
+        __builtin_amdgcn_raw_buffer_store_b128(w.a, to, (int)at, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(w.b, to, (int)at, 16, 0);
+    }
+}
 
 // Rows of several heads in memory: [tokens][heads][width], tokens `stride` elements apart.
 struct HeadRows {
@@ -97,48 +125,51 @@ struct HeadRows {
     int width;
 };
 
-// Tokens [begin, end) of one sequence, or a segment of it: position i of the recurrence is token first + i (or first - i, where time is reversed).
+// One segment of a sequence: position i of the recurrence is token begin + i (or begin + length - 1 - i, where time is reversed), the segment has
+// those from seg segments on.
 struct Span {
     int seq, unit, seg;      // (unit: the segment's place in the workspace)
-    long begin, length;      // of the whole sequence
+    int begin, length;       // of the whole sequence
 };
 
-// Sequences side by side: T tokens, B sequences of the same length or those between offsets[b] and offsets[b + 1]; segments of `seg`
-// tokens, a multiple of kChunk.  Sequence b's first segment is unit first_unit(b): segments of equal sequences follow each other, in a ragged
-// batch there is a place for each full segment of all tokens and one more for each sequence, which is enough: a sequence from a seg + r
-// to c seg + s has at most c - a + 1 segments.
+// Sequences side by side: T tokens, B sequences of `each` tokens or those between offsets[b] and offsets[b + 1]; segments of `seg` tokens, a
+// multiple of kChunk.  Sequence b's first segment is unit first_unit(b): segments of equal sequences follow each other, in a ragged batch
+// (whose segments are powers of two) there is a place for each full segment of all tokens and one more for each sequence, which is enough: a
+// sequence from a seg + r to c seg + s has at most c - a + 1 segments.
 struct Sequences {
     const int32_t *offsets;  // or null
-    long T;
-    int B;
-    long seg;
+    int T, B, each;
+    int seg, log_seg;
     int per_sequence;        // units of a sequence of an equal batch
-    __host__ __device__ inline long units() const { return offsets != nullptr ? T / seg + B : (long)per_sequence * B; }
-    __device__ inline long offset(int b) const {
-        if (offsets == nullptr) return T / B * b;
-        const long at = offsets[b];
+    __host__ __device__ inline long units() const { return offsets != nullptr ? (long)(T >> log_seg) + B : (long)per_sequence * B; }
+    __device__ inline int offset(int b) const {
+        const int at = offsets[b];
         return at < 0 ? 0 : at > T ? T : at;
     }
-    __device__ inline long first_unit(int b) const { return offsets == nullptr ? (long)per_sequence * b : offset(b) / seg + b; }
     __device__ inline Span of_sequence(int b) const {
         Span s;
         s.seq = b, s.seg = 0;
-        s.begin = offset(b);
-        const long end = offset(b + 1);
-        s.length = end > s.begin ? end - s.begin : 0;
-        s.unit = (int)first_unit(b);
+        if (offsets == nullptr) {
+            s.begin = each * b, s.length = each, s.unit = per_sequence * b;
+        } else {
+            s.begin = __builtin_amdgcn_readfirstlane(offset(b));
+            const int end = __builtin_amdgcn_readfirstlane(offset(b + 1));
+            s.length = end > s.begin ? end - s.begin : 0;
+            s.unit = (s.begin >> log_seg) + b;
+        }
         return s;
     }
     // The sequence that has unit u: the last one whose first unit is not behind u, 64 sequences at a time.
-    __device__ inline Span of_unit(long u) const {
+    __device__ inline Span of_unit(uint32_t u) const {
         int b = 0;
         if (offsets == nullptr) {
-            b = (int)(u / per_sequence);
+            b = per_sequence == 1 ? (int)u : (int)(u / (uint32_t)per_sequence);
         } else {
             int n = B;
             while (n > 1) {
                 const int step = (n + 63) >> 6, lane = (int)(threadIdx.x & 63), at = lane * step;
-                const uint64_t there = __ballot(at < n && first_unit(b + (at < n ? at : 0)) <= u);
+                const int place = b + (at < n ? at : 0);
+                const uint64_t there = __ballot(at < n && (uint32_t)((offset(place) >> log_seg) + place) <= u);
                 const int last = there == 0 ? 0 : 63 - __builtin_clzll(there);
                 b += last * step;
                 n = n - last * step < step ? n - last * step : step;
@@ -146,20 +177,21 @@ struct Sequences {
             b = __builtin_amdgcn_readfirstlane(b);
         }
         Span s = of_sequence(b);
-        s.seg = (int)(u - s.unit);
+        s.seg = (int)u - s.unit;
         s.unit = (int)u;
         return s;
     }
 };
 
-// exp(n g): 1 for n = 0 also where g is -infinity (a head without memory).  The exponent is rounded once, relative to itself: a result of 2^-20 is off
-// by 20 units, one near 1 by one or two.
-__device__ inline float decay_pow(float g, int n) { return n <= 0 ? 1.0f : expf(g * (float)n); }
+// exp(n g), n >= 0, as 2^(n g / ln 2): the exponent is rounded twice, relative to itself, so a result of 2^-20 is off by some 30 units and one near 1 by
+// one or two.  A head without memory (g = -infinity) has 1 for n = 0 and 0 for all others: so has one of -2000.
+__device__ inline float decay_rate(float g) { return (g < -2000.0f ? -2000.0f : g) * 1.44269504f; }
+__device__ inline float decay_pow(float rate, int n) { return __builtin_amdgcn_exp2f(rate * (float)n); }
 
 // A workgroup's share of the launch: workgroups go to the 8 XCDs in turn, neighbours of one list of work belong on one XCD (they read the
 // same keys and values).
-__device__ inline long xcd_place(long total) {
-    const long each = (total + 7) / 8, i = blockIdx.x;
+__device__ inline uint32_t xcd_place(uint32_t total) {
+    const uint32_t each = (total + 7) / 8, i = blockIdx.x;
     return (i & 7) * each + (i >> 3);
 }
 inline long xcd_blocks(long total) { return (total + 7) / 8 * 8; }
@@ -185,6 +217,7 @@ inline int check_heads(const char *what, int type, long T, int H, int Hk, int d,
 inline int check_rows(const char *what, const char *name, const void *p, long stride, int heads, int width, int type) {
     SA_REQUIRE(p != nullptr, SA_ERR_INVALID, "%s: %s is NULL", what, name);
     SA_REQUIRE(stride >= (long)heads * width, SA_ERR_SHAPE, "%s: the rows of %s overlap (stride %ld, %d heads of %d)", what, name, stride, heads, width);
+    SA_REQUIRE(stride < (1L << 22), SA_ERR_UNSUPPORTED, "%s: the tokens of %s are too far apart (stride %ld)", what, name, stride);
     SA_REQUIRE(aligned16(p) && stride % (type == SA_F32 ? 4 : 8) == 0, SA_ERR_ALIGN, "%s: the rows of %s must be 16-byte aligned", what, name);
     return SA_OK;
 }

@@ -33,14 +33,16 @@ struct Role {
 
 struct Args {
     Role role[3];
-    long items[3];           // of the roles before and with this one
+    uint32_t items[3];       // of the roles before and with this one
     int roles;
     Sequences seq;
     const float *g;
     int Hk, dv;              // (dv: columns of a state in memory)
-    long state;              // elements of a state: d dv
+    int state;               // elements of a state: d dv
     const int32_t *slots;
     int places;
+    __device__ inline const float *place(const float *states, int p, int hk) const { return states + ((long)p * Hk + hk) * state; }
+    __device__ inline float *place(float *states, int p, int hk) const { return states + ((long)p * Hk + hk) * state; }
 };
 
 template <class T, int DK>
@@ -51,43 +53,60 @@ struct Shape {
     static constexpr int TILES = DK / 16;
 };
 
-// The rows of one chunk: from memory to registers, from there to LDS.
+// Where a workgroup's tokens are in one tensor: row i of chunk c is token first + c kChunk + i, or first - c kChunk - i.
+struct Tokens {
+    uint64_t base;           // of row 0 of the current chunk, or of row 63 where time is reversed
+    int64_t next;            // bytes to the next chunk
+    uint32_t pitch;          // bytes from token to token
+    bool reverse;
+    template <class T>
+    __device__ inline void set(const HeadRows &r, const Span &sp, int p0, bool reverse_, int head, int col) {
+        reverse = reverse_;
+        pitch = (uint32_t)r.stride * (uint32_t)sizeof(T);
+        const long first = reverse ? (long)sp.begin + sp.length - p0 - kChunk : (long)sp.begin + p0;
+        base = reinterpret_cast<uint64_t>(r.p) + (uint64_t)(first * (long)pitch) + (uint64_t)(head * r.width + col) * sizeof(T);
+        next = (reverse ? -(int64_t)kChunk : (int64_t)kChunk) * (int64_t)pitch;
+    }
+    __device__ inline uint32_t row(int i) const { return (uint32_t)(reverse ? kChunk - 1 - i : i) * pitch; }
+    __device__ inline __amdgpu_buffer_rsrc_t at(uint64_t more = 0) const { return buffer(reinterpret_cast<const void *>(base + more)); }
+};
+
+// The keys and values of one chunk: from memory to registers, from there to LDS.
 template <class T, int DK>
 struct Rows {
     using P = Shape<T, DK>;
     Eight<T> k[P::KPIECES], v[P::VPIECES];
-    __device__ inline void load(const Role &r, long begin, long length, long pos, int n, int head, int c0) {
-        const long dir = r.reverse ? -1 : 1, t0 = r.reverse ? begin + length - 1 - pos : begin + pos;
-        const T *kp = static_cast<const T *>(r.k.p) + (long)head * r.k.width, *vp = static_cast<const T *>(r.v.p) + (long)head * r.v.width + c0;
+    uint32_t kat[P::KPIECES], vat[P::VPIECES];
+    __device__ inline static int krow(int j) { return ((int)threadIdx.x + kThreads * j) / (DK / 8); }
+    __device__ inline static int kcol(int j) { return ((int)threadIdx.x + kThreads * j) % (DK / 8) * 8; }
+    __device__ inline static int vrow(int j) { return ((int)threadIdx.x + kThreads * j) / (kSlice / 8); }
+    __device__ inline static int vcol(int j) { return ((int)threadIdx.x + kThreads * j) % (kSlice / 8) * 8; }
+    __device__ inline void places(const Tokens &kt, int kwidth, const Tokens &vt, int vwidth) {
 #pragma unroll
-        for (int j = 0; j < P::KPIECES; ++j) {
-            const int at = (int)threadIdx.x + kThreads * j, row = at / (DK / 8), col = at % (DK / 8) * 8;
-            if (row < n && col < r.k.width) k[j].load(kp + (t0 + dir * row) * r.k.stride + col);
-            else k[j].zero();
-        }
+        for (int j = 0; j < P::KPIECES; ++j) kat[j] = kcol(j) < kwidth ? kt.row(krow(j)) + kcol(j) * (uint32_t)sizeof(T) : kNowhere;
 #pragma unroll
-        for (int j = 0; j < P::VPIECES; ++j) {
-            const int at = (int)threadIdx.x + kThreads * j, row = at / (kSlice / 8), col = at % (kSlice / 8) * 8;
-            if (row < n && c0 + col < r.v.width) v[j].load(vp + (t0 + dir * row) * r.v.stride + col);
-            else v[j].zero();
-        }
+        for (int j = 0; j < P::VPIECES; ++j) vat[j] = vcol(j) < vwidth ? vt.row(vrow(j)) + vcol(j) * (uint32_t)sizeof(T) : kNowhere;
+    }
+    __device__ inline void load(__amdgpu_buffer_rsrc_t kp, __amdgpu_buffer_rsrc_t vp, int n) {
+#pragma unroll
+        for (int j = 0; j < P::KPIECES; ++j) k[j].load(kp, krow(j) < n ? kat[j] : kNowhere);
+#pragma unroll
+        for (int j = 0; j < P::VPIECES; ++j) v[j].load(vp, vrow(j) < n ? vat[j] : kNowhere);
     }
     __device__ inline void stage(__bf16 (*kl)[kChunk][P::KP], __bf16 (*vl)[kChunk][P::VP]) const {
 #pragma unroll
         for (int j = 0; j < P::KPIECES; ++j) {
-            const int at = (int)threadIdx.x + kThreads * j, row = at / (DK / 8), col = at % (DK / 8) * 8;
             b8 t[P::RAW];
             k[j].terms(t);
 #pragma unroll
-            for (int p = 0; p < P::RAW; ++p) *reinterpret_cast<b8 *>(&kl[p][row][col]) = t[p];
+            for (int p = 0; p < P::RAW; ++p) *reinterpret_cast<b8 *>(&kl[p][krow(j)][kcol(j)]) = t[p];
         }
 #pragma unroll
         for (int j = 0; j < P::VPIECES; ++j) {
-            const int at = (int)threadIdx.x + kThreads * j, row = at / (kSlice / 8), col = at % (kSlice / 8) * 8;
             b8 t[P::RAW];
             v[j].terms(t);
 #pragma unroll
-            for (int p = 0; p < P::RAW; ++p) *reinterpret_cast<b8 *>(&vl[p][row][col]) = t[p];
+            for (int p = 0; p < P::RAW; ++p) *reinterpret_cast<b8 *>(&vl[p][vrow(j)][vcol(j)]) = t[p];
         }
     }
 };
@@ -101,28 +120,42 @@ struct State {
 #pragma unroll
         for (int t = 0; t < P::TILES; ++t) s[t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    template <class F>
-    __device__ inline void each(const Role &r, int dv, int c0, F f) {
+    // Four rows of a lane are side by side in memory where the state lies there transposed.
+    __device__ inline void load(const float *p, bool transposed, int rows, int cols, int dv, int c0) {
         const int lane = (int)threadIdx.x & 63, g = lane >> 4, col = c0 + 16 * ((int)threadIdx.x >> 6) + (lane & 15);
+        clear();
+        if (col >= cols) return;
 #pragma unroll
         for (int t = 0; t < P::TILES; ++t) {
+            const int row = 16 * t + 4 * g;
+            if (row >= rows) continue;
+            if (transposed) {
+                s[t] = *reinterpret_cast<const f4 *>(p + col * dv + row);
+            } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = 16 * t + 4 * g + i;
-                float x = s[t][i];
-                if (row < r.k.width && col < r.v.width) f(r.transposed ? col * dv + row : row * dv + col, x);
-                s[t][i] = x;
+                for (int i = 0; i < 4; ++i) s[t][i] = p[(row + i) * dv + col];
             }
         }
     }
-    __device__ inline void load(const Role &r, const float *p, int dv, int c0) {
-        each(r, dv, c0, [&](int at, float &x) { x = p[at]; });
-    }
-    __device__ inline void store(const Role &r, float *p, int dv, int c0) {
-        each(r, dv, c0, [&](int at, float &x) { p[at] = x; });
+    __device__ inline void store(float *p, bool transposed, int rows, int cols, int dv, int c0) const {
+        const int lane = (int)threadIdx.x & 63, g = lane >> 4, col = c0 + 16 * ((int)threadIdx.x >> 6) + (lane & 15);
+        if (col >= cols) return;
+#pragma unroll
+        for (int t = 0; t < P::TILES; ++t) {
+            const int row = 16 * t + 4 * g;
+            if (row >= rows) continue;
+            if (transposed) {
+                *reinterpret_cast<f4 *>(p + col * dv + row) = s[t];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[(row + i) * dv + col] = s[t][i];
+            }
+        }
     }
     // To LDS as terms, for the product with q: [column of the slice][row].  Columns are in the order in which the product's tiles take them: tile
-    // t, row 4 a + b is column 16 a + 4 t + b, so that a lane's results are 16 columns side by side.
+    // t, row 4 a + b is column 16 a + 4 t + b, so that a lane's results are 16 columns side by side.  The 16 rows of a block change
+    // places with the column's tile (swapped()): the 4 columns of a lane's neighbours would lie in the same banks otherwise.
+    __device__ inline static int swapped(int row, int tile) { return row ^ (16 * (tile & (P::TILES - 1))); }
     __device__ inline void stage(__bf16 (*sl)[kSlice][P::KP]) const {
         const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15, place = 16 * (i >> 2) + 4 * ((int)threadIdx.x >> 6) + (i & 3);
 #pragma unroll
@@ -131,28 +164,26 @@ struct State {
             b4 p[P::MADE];
             split(x, p);
 #pragma unroll
-            for (int n = 0; n < P::MADE; ++n) *reinterpret_cast<b4 *>(&sl[n][place][16 * t + 4 * g]) = p[n];
+            for (int n = 0; n < P::MADE; ++n) *reinterpret_cast<b4 *>(&sl[n][place][swapped(16 * t + 4 * g, i >> 2)]) = p[n];
         }
     }
-    // S = carry S + sum_j weight[j] k_j v_j^T over the chunk in LDS.  Both operands have tokens for the places of the sum:
-    // transposed reads, in the order 32 s + 16 (e / 4) + 4 (l / 16) + e % 4 for element e.
-    __device__ inline void update(const __bf16 (*kl)[kChunk][P::KP], const __bf16 (*vl)[kChunk][P::VP], const float (&weight)[2][2][4]) {
+    // S += sum_j weight[j] k_j v_j^T over the chunk in LDS.  Both operands have tokens for the places of the sum: transposed
+    // reads, in the order 32 s + 16 (e / 4) + 4 (l / 16) + e % 4 for element e.
+    __device__ inline void update(const __bf16 (*kl)[kChunk][P::KP], const __bf16 (*vl)[kChunk][P::VP], const float (&weight)[2][8]) {
         const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15, w = (int)threadIdx.x >> 6, row = 4 * g + (i >> 2), col = 4 * (i & 3);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             float x[8];
+            b8 raw[P::RAW];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                b4 raw[P::RAW];
+            for (int p = 0; p < P::RAW; ++p)
+                raw[p] = join(read_transposed(&vl[p][32 * ks + row][16 * w + col]), read_transposed(&vl[p][32 * ks + 16 + row][16 * w + col]));
 #pragma unroll
-                for (int p = 0; p < P::RAW; ++p) raw[p] = read_transposed(&vl[p][32 * ks + 16 * h + row][16 * w + col]);
+            for (int e = 0; e < 8; ++e) {
+                float y = (float)raw[P::RAW - 1][e];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float y = 0.0f;
-#pragma unroll
-                    for (int p = P::RAW - 1; p >= 0; --p) y = p == P::RAW - 1 ? (float)raw[p][e] : y + (float)raw[p][e];
-                    x[4 * h + e] = y * weight[ks][h][e];
-                }
+                for (int p = P::RAW - 2; p >= 0; --p) y += (float)raw[p][e];
+                x[e] = y * weight[ks][e];
             }
             b8 b[kUpdateTerms];
             split(x, b);
@@ -169,17 +200,15 @@ struct State {
 };
 
 // Decays of a chunk of n tokens on their way into the state, for the tokens that a lane has in State::update.
-__device__ inline void update_weights(float (&weight)[2][2][4], const float *pw, int n, int shift, float factor) {
+__device__ inline void update_weights(float (&weight)[2][8], float rate, int n, int shift, float factor) {
     const int g = ((int)threadIdx.x & 63) >> 4;
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int left = n - shift - (32 * ks + 16 * h + 4 * g + e);
-                weight[ks][h][e] = left >= 0 ? factor * pw[left] : 0.0f;
-            }
+        for (int e = 0; e < 8; ++e) {
+            const int left = n - shift - (32 * ks + 16 * (e >> 2) + 4 * g + (e & 3));
+            weight[ks][e] = left >= 0 ? factor * decay_pow(rate, left) : 0.0f;
+        }
 }
 
 // A sequence's place among the states; -1: none, it begins with zeros and leaves no state.
@@ -189,120 +218,139 @@ __device__ inline int state_place(const Args &a, int seq) {
     return p >= 0 && p < a.places ? p : -1;
 }
 
-__device__ inline const Role &role_of(const Args &a, long &item) {
+__device__ inline const Role &role_of(const Args &a, uint32_t &item) {
     int r = 0;
     while (r + 1 < a.roles && item >= a.items[r]) ++r;
     if (r > 0) item -= a.items[r - 1];
     return a.role[r];
 }
 
+// Wavefronts on a SIMD: as many workgroups as have room for their rows in a CU's LDS, unless that would cost registers.
+template <class T, int DK>
+constexpr int rows_waves() {
+    return std::is_same<T, bf16_t>::value ? (DK <= 32 ? 4 : DK <= 64 ? 3 : 2) : std::is_same<T, f16_t>::value ? (DK <= 32 ? 4 : DK <= 64 ? 2 : 1) : DK <= 32 ? 2 : 1;
+}
+
 // Rows of the result.  A workgroup has one segment, one head and a slice of 64 columns and goes through the chunks one after the other; wavefront w has
 // queries 16 w to 16 w + 15 of a chunk, and columns 16 w to 16 w + 15 of the state.
 template <class T, int DK>
-__global__ __launch_bounds__(kThreads) void decay_rows_kernel(const Args a) {
+__global__ __launch_bounds__(kThreads, (rows_waves<T, DK>())) void decay_rows_kernel(const Args a) {
     using P = Shape<T, DK>;
     __shared__ __attribute__((aligned(16))) __bf16 kl[P::RAW][kChunk][P::KP];
     __shared__ __attribute__((aligned(16))) __bf16 vl[P::RAW][kChunk][P::VP];
     __shared__ __attribute__((aligned(16))) __bf16 sl[P::MADE][kSlice][P::KP];
-    __shared__ float pw[kChunk + 1];
-    long item = xcd_place(a.items[a.roles - 1]);
-    if (item >= a.items[a.roles - 1]) return;
+    const uint32_t total = a.items[a.roles - 1];
+    uint32_t item = xcd_place(total);
+    if (item >= total) return;
     const Role &r = role_of(a, item);
-    const int slices = (r.out.width + kSlice - 1) / kSlice;
+    const int kwidth = r.k.width, vwidth = r.v.width, sums = r.sums, shift = r.shift;
+    const float update = r.update;
+    const bool transposed = r.transposed, reverse = r.reverse;
+    const uint32_t slices = vwidth > kSlice ? 2 : 1;
     const int c0 = (int)(item % slices) * kSlice;
     item /= slices;
-    const int sub = (int)(item % r.outs);
-    item /= r.outs;
-    const int hk = (int)(item % a.Hk);
-    const Span sp = a.seq.of_unit(item / a.Hk);
-    const long p0 = sp.seg * a.seq.seg;
-    const long left = sp.length - p0;
+    int sub = 0;
+    if (r.outs > 1) sub = (int)(item % (uint32_t)r.outs), item /= (uint32_t)r.outs;
+    const int hk = (int)(item % (uint32_t)a.Hk);
+    const Span sp = a.seq.of_unit(item / (uint32_t)a.Hk);
+    const int p0 = sp.seg * a.seq.seg, left = sp.length - p0;
     if (sp.seg < 0 || (left <= 0 && (sp.seg > 0 || r.last == nullptr))) return;
-    const int tokens = (int)(left < a.seq.seg ? left : a.seq.seg);
+    const int tokens = left < a.seq.seg ? left : a.seq.seg;
     const int out_head = hk * r.outs + sub;
 
     const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const float log_decay = a.g[hk];
-    if ((int)threadIdx.x <= kChunk) pw[threadIdx.x] = decay_pow(log_decay, (int)threadIdx.x);
-    State<T, DK> state;
-    state.clear();
-    bool live = false;                   // a state that is not zero
-    const int place = r.first != nullptr || r.last != nullptr ? state_place(a, sp.seq) : -1;
-    if (r.starts != nullptr) {
-        state.load(r, r.starts + ((long)sp.unit * a.Hk + hk) * a.state, a.dv, c0);
-        live = true;
-    } else if (r.first != nullptr && place >= 0) {
-        state.load(r, r.first + ((long)place * a.Hk + hk) * a.state, a.dv, c0);
-        live = true;
-    }
-    const bool keep = r.last != nullptr && place >= 0;
-
+    const int query = 16 * w + i;
+    const float rate = decay_rate(a.g[hk]);
     const int chunks = (tokens + kChunk - 1) / kChunk;
-    Rows<T, DK> rows;
-    Eight<T> q[DK / 32];
     auto in_chunk = [&](int c) { return tokens - c * kChunk < kChunk ? tokens - c * kChunk : kChunk; };
-    auto token = [&](int pos) { return r.reverse ? sp.begin + sp.length - 1 - p0 - pos : sp.begin + p0 + pos; };
-    auto load_q = [&](int c) {
-        const int pos = c * kChunk + 16 * w + i;
-        const T *p = static_cast<const T *>(r.q.p) + token(pos) * r.q.stride + (long)out_head * r.q.width;
+
+    Tokens qt, kt, vt, ot;
+    qt.set<T>(r.q, sp, p0, reverse, out_head, 0);
+    ot.set<T>(r.out, sp, p0, reverse, out_head, c0);
+    kt.set<T>(r.k, sp, p0, reverse, hk * sums, 0);
+    vt.set<T>(r.v, sp, p0, reverse, hk * sums, c0);
+    const uint32_t kmore = (uint32_t)kwidth * (uint32_t)sizeof(T), vmore = (uint32_t)vwidth * (uint32_t)sizeof(T);     // to the next head that is added up
+    const uint32_t qat = qt.row(query) + 8 * g * (uint32_t)sizeof(T), oat = ot.row(query) + 16 * g * (uint32_t)sizeof(T);
+    Rows<T, DK> rows;
+    rows.places(kt, kwidth, vt, vwidth - c0);
+    Eight<T> q[DK / 32];
+    auto load_q = [&](int n) {
+        const __amdgpu_buffer_rsrc_t p = qt.at();
 #pragma unroll
-        for (int s = 0; s < DK / 32; ++s) {
-            const int col = 32 * s + 8 * g;
-            if (pos < tokens && col < r.q.width) q[s].load(p + col);
-            else q[s].zero();
-        }
+        for (int s = 0; s < DK / 32; ++s) q[s].load(p, query < n && 32 * s + 8 * g < kwidth ? qat + 32 * s * (uint32_t)sizeof(T) : kNowhere);
+        qt.base += (uint64_t)qt.next;
     };
     if (chunks > 0) {
-        load_q(0);
-        rows.load(r, sp.begin, sp.length, p0, in_chunk(0), hk * r.sums, c0);
+        load_q(in_chunk(0));
+        rows.load(kt.at(), vt.at(), in_chunk(0));
     }
-    __syncthreads();
 
-    float inside[4][4], weight[2][2][4];
+    State<T, DK> state;
+    bool live = false;                   // a state that is not zero
+    const int place = r.first != nullptr || r.last != nullptr ? state_place(a, sp.seq) : -1;
+    float *const last = r.last != nullptr && place >= 0 ? a.place(r.last, place, hk) : nullptr;
+    if (r.starts != nullptr || (r.first != nullptr && place >= 0)) {
+        state.load(r.starts != nullptr ? a.place(r.starts, sp.unit, hk) : a.place(r.first, place, hk), transposed, kwidth, vwidth, a.dv, c0);
+        live = true;
+    } else {
+        state.clear();
+    }
+
+    float inside[4][4], weight[2][8];
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int far = 16 * (w - t) + i - 4 * g - e;
-            inside[t][e] = far >= 0 ? r.inside * pw[far] : 0.0f;
+            inside[t][e] = far >= 0 ? r.inside * decay_pow(rate, far) : 0.0f;
         }
-    const float into = r.into * pw[16 * w + i + r.shift];
-    update_weights(weight, pw, kChunk, r.shift, r.update);
+    const float into = r.into * decay_pow(rate, query + shift);
+    update_weights(weight, rate, kChunk, shift, update);
+    float carry = decay_pow(rate, kChunk);
 
     f4 o[4];
-    b8 qt[DK / 32][P::RAW];
+    b8 qterms[DK / 32][P::RAW];
     for (int c = 0; c < chunks; ++c) {
         const int n = in_chunk(c);
-        const bool add = c + 1 < chunks || keep;
-        if (n < kChunk && add) update_weights(weight, pw, n, r.shift, r.update);
-        for (int h = 0; h < r.sums; ++h) {
+        const bool more = c + 1 < chunks, add = more || last != nullptr;
+        if (n < kChunk && add) {
+            update_weights(weight, rate, n, shift, update);
+            carry = decay_pow(rate, n);
+        }
+        for (int h = 0; h < sums; ++h) {
             if (c + h > 0) __syncthreads();
             rows.stage(kl, vl);
             if (h == 0) {
                 if (live) state.stage(sl);
 #pragma unroll
-                for (int s = 0; s < DK / 32; ++s) q[s].terms(qt[s]);
-                if (c + 1 < chunks) load_q(c + 1);
+                for (int s = 0; s < DK / 32; ++s) q[s].terms(qterms[s]);
+                if (more) load_q(in_chunk(c + 1));
             }
-            if (h + 1 < r.sums) rows.load(r, sp.begin, sp.length, p0 + (long)c * kChunk, n, hk * r.sums + h + 1, c0);
-            else if (c + 1 < chunks) rows.load(r, sp.begin, sp.length, p0 + (long)(c + 1) * kChunk, in_chunk(c + 1), hk * r.sums, c0);
+            if (h + 1 < sums) {
+                rows.load(kt.at((uint64_t)(h + 1) * kmore), vt.at((uint64_t)(h + 1) * vmore), n);
+            } else if (more) {
+                kt.base += (uint64_t)kt.next, vt.base += (uint64_t)vt.next;
+                rows.load(kt.at(), vt.at(), in_chunk(c + 1));
+            }
             __syncthreads();
             if (h == 0) {
 #pragma unroll
                 for (int t = 0; t < 4; ++t) o[t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
                 if (live) {
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
+                    for (int s = 0; s < DK / 32; ++s) {
 #pragma unroll
-                        for (int s = 0; s < DK / 32; ++s) {
+                        for (int t = 0; t < 4; ++t) {
                             b8 st[P::MADE];
 #pragma unroll
-                            for (int p = 0; p < P::MADE; ++p) st[p] = *reinterpret_cast<const b8 *>(&sl[p][16 * t + i][32 * s + 8 * g]);
-                            product<Terms<T>::ORDER>(o[t], st, qt[s]);
+                            for (int p = 0; p < P::MADE; ++p) st[p] = *reinterpret_cast<const b8 *>(&sl[p][16 * t + i][State<T, DK>::swapped(32 * s + 8 * g, t)]);
+                            product<Terms<T>::ORDER>(o[t], st, qterms[s]);
                         }
+                    }
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[t][e] *= into;
-                    }
                 }
             }
             // (k_j q_i) for 32 keys at a time, which are in the registers of the lanes that have them as the right operand of the product with v
@@ -317,14 +365,18 @@ __global__ __launch_bounds__(kThreads) void decay_rows_kernel(const Args a) {
                     if (t <= w) {
 #pragma unroll
                         for (int d = 0; d < DK / 32; ++d) {
-                            b8 kt[P::RAW];
+                            b8 kterms[P::RAW];
 #pragma unroll
-                            for (int p = 0; p < P::RAW; ++p) kt[p] = *reinterpret_cast<const b8 *>(&kl[p][16 * t + i][32 * d + 8 * g]);
-                            product<Terms<T>::ORDER_RAW>(s, kt, qt[d]);
+                            for (int p = 0; p < P::RAW; ++p) kterms[p] = *reinterpret_cast<const b8 *>(&kl[p][16 * t + i][32 * d + 8 * g]);
+                            product<Terms<T>::ORDER_RAW>(s, kterms, qterms[d]);
                         }
                     }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[4 * half + e] = t < w || (t == w && i >= 4 * g + e) ? s[e] * inside[t][e] : 0.0f;
+                    for (int e = 0; e < 4; ++e) x[4 * half + e] = s[e] * inside[t][e];
+                    if (t == w) {        // a product that is not in the sum may be infinite
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[4 * half + e] = i >= 4 * g + e ? x[4 * half + e] : 0.0f;
+                    }
                 }
                 b8 pt[P::MADE];
                 split(x, pt);
@@ -332,36 +384,32 @@ __global__ __launch_bounds__(kThreads) void decay_rows_kernel(const Args a) {
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     const int col = 16 * (i & 3) + 4 * t;
-                    b8 vt[P::RAW];
+                    b8 vterms[P::RAW];
 #pragma unroll
-                    for (int p = 0; p < P::RAW; ++p) vt[p] = join(read_transposed(&vl[p][row][col]), read_transposed(&vl[p][row + 16][col]));
-                    product<Terms<T>::ORDER>(o[t], vt, pt);
+                    for (int p = 0; p < P::RAW; ++p) vterms[p] = join(read_transposed(&vl[p][row][col]), read_transposed(&vl[p][row + 16][col]));
+                    product<Terms<T>::ORDER>(o[t], vterms, pt);
                 }
             }
             if (add) {
                 if (h == 0 && live) {
-                    const float carry = pw[n];
 #pragma unroll
                     for (int t = 0; t < P::TILES; ++t) state.s[t] *= carry;
                 }
                 state.update(kl, vl, weight);
             }
         }
-        if (add) live = true;
-        const int pos = c * kChunk + 16 * w + i;
-        if (pos < tokens) {
-            T *p = static_cast<T *>(const_cast<void *>(r.out.p)) + token(pos) * r.out.stride + (long)out_head * r.out.width;
-            const int col = c0 + 16 * g;
+        live = live || add;
+        const __amdgpu_buffer_rsrc_t to = ot.at();
+        ot.base += (uint64_t)ot.next;
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                float x[8];
+        for (int half = 0; half < 2; ++half) {
+            float x[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = o[2 * half + e / 4][e % 4];
-                if (col + 8 * half < r.out.width) store_piece<T, 8>(p + col + 8 * half, x);
-            }
+            for (int e = 0; e < 8; ++e) x[e] = o[2 * half + e / 4][e % 4];
+            store_eight<T>(to, query < n && c0 + 16 * g + 8 * half < vwidth ? oat + 8 * half * (uint32_t)sizeof(T) : kNowhere, x);
         }
     }
-    if (keep) state.store(r, r.last + ((long)place * a.Hk + hk) * a.state, a.dv, c0);
+    if (last != nullptr) state.store(last, transposed, kwidth, vwidth, a.dv, c0);
 }
 
 // What each segment adds to the state, from a state of zeros.
@@ -370,78 +418,89 @@ __global__ __launch_bounds__(kThreads) void decay_states_kernel(const Args a) {
     using P = Shape<T, DK>;
     __shared__ __attribute__((aligned(16))) __bf16 kl[P::RAW][kChunk][P::KP];
     __shared__ __attribute__((aligned(16))) __bf16 vl[P::RAW][kChunk][P::VP];
-    __shared__ float pw[kChunk + 1];
-    long item = xcd_place(a.items[a.roles - 1]);
-    if (item >= a.items[a.roles - 1]) return;
+    const uint32_t total = a.items[a.roles - 1];
+    uint32_t item = xcd_place(total);
+    if (item >= total) return;
     const Role &r = role_of(a, item);
-    const int slices = (r.v.width + kSlice - 1) / kSlice;
+    const int kwidth = r.k.width, vwidth = r.v.width, sums = r.sums, shift = r.shift;
+    const float update = r.update;
+    const bool reverse = r.reverse;
+    const uint32_t slices = vwidth > kSlice ? 2 : 1;
     const int c0 = (int)(item % slices) * kSlice;
     item /= slices;
-    const int hk = (int)(item % a.Hk);
-    const Span sp = a.seq.of_unit(item / a.Hk);
-    const long p0 = sp.seg * a.seq.seg, left = sp.length - p0;
+    const int hk = (int)(item % (uint32_t)a.Hk);
+    const Span sp = a.seq.of_unit(item / (uint32_t)a.Hk);
+    const int p0 = sp.seg * a.seq.seg, left = sp.length - p0;
     // the last segment's sum is for the state behind the sequence only
     if (sp.seg < 0 || left <= 0 || (left <= a.seq.seg && r.last == nullptr)) return;
-    const int tokens = (int)(left < a.seq.seg ? left : a.seq.seg), chunks = (tokens + kChunk - 1) / kChunk;
-    const float log_decay = a.g[hk];
-    if ((int)threadIdx.x <= kChunk) pw[threadIdx.x] = decay_pow(log_decay, (int)threadIdx.x);
+    const int tokens = left < a.seq.seg ? left : a.seq.seg, chunks = (tokens + kChunk - 1) / kChunk;
+    const float rate = decay_rate(a.g[hk]);
     State<T, DK> state;
     state.clear();
-    Rows<T, DK> rows;
     auto in_chunk = [&](int c) { return tokens - c * kChunk < kChunk ? tokens - c * kChunk : kChunk; };
-    rows.load(r, sp.begin, sp.length, p0, in_chunk(0), hk * r.sums, c0);
-    __syncthreads();
-    float weight[2][2][4];
-    update_weights(weight, pw, kChunk, r.shift, r.update);
+    Tokens kt, vt;
+    kt.set<T>(r.k, sp, p0, reverse, hk * sums, 0);
+    vt.set<T>(r.v, sp, p0, reverse, hk * sums, c0);
+    const uint32_t kmore = (uint32_t)kwidth * (uint32_t)sizeof(T), vmore = (uint32_t)vwidth * (uint32_t)sizeof(T);
+    Rows<T, DK> rows;
+    rows.places(kt, kwidth, vt, vwidth - c0);
+    rows.load(kt.at(), vt.at(), in_chunk(0));
+    float weight[2][8];
+    update_weights(weight, rate, kChunk, shift, update);
+    float carry = decay_pow(rate, kChunk);
     for (int c = 0; c < chunks; ++c) {
         const int n = in_chunk(c);
-        if (n < kChunk) update_weights(weight, pw, n, r.shift, r.update);
-        for (int h = 0; h < r.sums; ++h) {
+        if (n < kChunk) {
+            update_weights(weight, rate, n, shift, update);
+            carry = decay_pow(rate, n);
+        }
+#pragma unroll
+        for (int t = 0; t < P::TILES; ++t) state.s[t] *= carry;
+        for (int h = 0; h < sums; ++h) {
             if (c + h > 0) __syncthreads();
             rows.stage(kl, vl);
-            if (h + 1 < r.sums) rows.load(r, sp.begin, sp.length, p0 + (long)c * kChunk, n, hk * r.sums + h + 1, c0);
-            else if (c + 1 < chunks) rows.load(r, sp.begin, sp.length, p0 + (long)(c + 1) * kChunk, in_chunk(c + 1), hk * r.sums, c0);
-            __syncthreads();
-            if (h == 0) {
-                const float carry = pw[n];
-#pragma unroll
-                for (int t = 0; t < P::TILES; ++t) state.s[t] *= carry;
+            if (h + 1 < sums) {
+                rows.load(kt.at((uint64_t)(h + 1) * kmore), vt.at((uint64_t)(h + 1) * vmore), n);
+            } else if (c + 1 < chunks) {
+                kt.base += (uint64_t)kt.next, vt.base += (uint64_t)vt.next;
+                rows.load(kt.at(), vt.at(), in_chunk(c + 1));
             }
+            __syncthreads();
             state.update(kl, vl, weight);
         }
     }
-    state.store(r, r.sums_out + ((long)sp.unit * a.Hk + hk) * a.state, a.dv, c0);
+    state.store(a.place(r.sums_out, sp.unit, hk), r.transposed, kwidth, vwidth, a.dv, c0);
 }
 
 // From the segments' sums to the states before them, in their place, and to the state behind the sequence.  A thread has 4 elements.
 __global__ __launch_bounds__(kThreads) void decay_scan_kernel(const Args a) {
     const Role &r = a.role[blockIdx.z];
     const int hk = (int)(blockIdx.y % (unsigned)a.Hk), b = (int)(blockIdx.y / (unsigned)a.Hk);
-    const long at = ((long)blockIdx.x * kThreads + threadIdx.x) * 4;
+    const int at = (int)(blockIdx.x * kThreads + threadIdx.x) * 4;
     if (at >= a.state) return;
     const Span sp = a.seq.of_sequence(b);
     const int place = r.first != nullptr || r.last != nullptr ? state_place(a, b) : -1;
-    const int segs = (int)((sp.length + a.seq.seg - 1) / a.seq.seg);
-    const float log_decay = a.g[hk];
+    const int segs = (sp.length + a.seq.seg - 1) / a.seq.seg;
+    const float rate = decay_rate(a.g[hk]);
     f4 x = f4{0.0f, 0.0f, 0.0f, 0.0f};
-    if (r.first != nullptr && place >= 0) x = *reinterpret_cast<const f4 *>(r.first + ((long)place * a.Hk + hk) * a.state + at);
-    float *p = r.sums_out + ((long)sp.unit * a.Hk + hk) * a.state + at;
-    const long next = a.Hk * a.state;
-    const float whole = decay_pow(log_decay, (int)a.seq.seg);
+    if (r.first != nullptr && place >= 0) x = *reinterpret_cast<const f4 *>(a.place(r.first, place, hk) + at);
+    float *p = a.place(r.sums_out, sp.unit, hk) + at;
+    const long next = (long)a.Hk * a.state;
+    const float whole = decay_pow(rate, a.seq.seg);
     for (int s = 0; s < segs; ++s, p += next) {
         const bool end = s + 1 == segs;
         f4 add = f4{0.0f, 0.0f, 0.0f, 0.0f};
         if (!end || r.last != nullptr) add = *reinterpret_cast<const f4 *>(p);
         *reinterpret_cast<f4 *>(p) = x;
-        x = x * (end ? decay_pow(log_decay, (int)(sp.length - (long)s * a.seq.seg)) : whole) + add;
+        x = x * (end ? decay_pow(rate, sp.length - s * a.seq.seg) : whole) + add;
     }
-    if (r.last != nullptr && place >= 0) *reinterpret_cast<f4 *>(r.last + ((long)place * a.Hk + hk) * a.state + at) = x;
+    if (r.last != nullptr && place >= 0) *reinterpret_cast<f4 *>(a.place(r.last, place, hk) + at) = x;
 }
 
 // ------------------------------------------------------------------------------------------- plan --
 
 struct Plan {
-    long seg = 0;            // 0: one pass
+    int seg = 0;             // 0: one pass
     int per_sequence = 1;
 };
 
@@ -460,17 +519,27 @@ Plan make_plan(long T, int B, int Hk, long outs, bool ragged, bool shared_states
         if (seg < kLeast) seg = kLeast;
     }
     if (ragged && T > kRagged && (seg == 0 || seg > kRagged)) seg = kRagged;
-    if (seg == 0 && shared_states) seg = (T + kChunk - 1) / kChunk * kChunk;
+    if (seg == 0 && shared_states) seg = T;
     if (!ragged && !shared_states && seg >= T / B) seg = 0;
-    p.seg = seg;
-    if (seg > 0) p.per_sequence = (int)((T / B + seg - 1) / seg);
+    if (seg > 0) {
+        if (ragged) {
+            long power = kChunk;
+            while (power < seg && power < (1L << 30)) power *= 2;
+            seg = power;
+        } else {
+            seg = (seg + kChunk - 1) / kChunk * kChunk;
+            p.per_sequence = (int)((T / B + seg - 1) / seg);
+        }
+    }
+    p.seg = (int)(seg < (1L << 30) ? seg : 1L << 30);
     return p;
 }
 
 Sequences sequences(const int32_t *offsets, long T, int B, const Plan &p) {
-    if (p.seg > 0) return Sequences{offsets, T, B, p.seg, p.per_sequence};
-    // one segment to a sequence: unit b is sequence b
-    return Sequences{offsets, T, B, 1L << 31, 1};
+    // one pass: one segment to a sequence, unit b is sequence b
+    Sequences s{offsets, (int)T, B, offsets == nullptr ? (int)(T / B) : 0, p.seg > 0 ? p.seg : 1 << 30, 30, p.per_sequence};
+    while (s.log_seg > 0 && 1 << s.log_seg > s.seg) --s.log_seg;
+    return s;
 }
 
 size_t plan_bytes(const Plan &p, long T, int B, bool ragged, int Hk, int d, int dv) {
@@ -495,13 +564,13 @@ int launch(const char *what, int type, Args a, const Plan &p, int states, hipStr
     int widest = 0;
     for (int r = 0; r < a.roles; ++r) widest = a.role[r].k.width > widest ? a.role[r].k.width : widest;
     long total = 0;
-    for (int r = 0; r < a.roles; ++r) a.items[r] = total += units * a.Hk * a.role[r].outs * slices_of(a.role[r].out.width);
+    for (int r = 0; r < a.roles; ++r) a.items[r] = (uint32_t)(total += units * a.Hk * a.role[r].outs * slices_of(a.role[r].out.width));
     SA_REQUIRE(total < (1L << 31) - 8, SA_ERR_UNSUPPORTED, "%s: too many heads and tokens for one launch", what);
     if (p.seg > 0) {
         Args s = a;
         s.roles = states;
         long sums = 0;
-        for (int r = 0; r < states; ++r) s.items[r] = sums += units * a.Hk * slices_of(s.role[r].v.width);
+        for (int r = 0; r < states; ++r) s.items[r] = (uint32_t)(sums += units * a.Hk * slices_of(s.role[r].v.width));
         const int rc = by_type(type, [&](auto t) {
             return by_width<decltype(t)>(widest, [&](auto k) {
                 decay_states_kernel<decltype(t), decltype(k)::value><<<dim3((unsigned)xcd_blocks(sums)), dim3(kThreads), 0, st>>>(s);
@@ -525,6 +594,7 @@ int check_sequences(const char *what, int type, long T, int B, bool ragged, int 
     SA_TRY(check_heads(what, type, T, H, Hk, d, dv));
     SA_REQUIRE(B >= 0, SA_ERR_INVALID, "%s: B < 0", what);
     SA_REQUIRE(ragged || (B > 0 ? T % B == 0 : T == 0), SA_ERR_SHAPE, "%s: %ld tokens are no %d sequences of the same length", what, T, B);
+    SA_REQUIRE(T < (1L << 30), SA_ERR_UNSUPPORTED, "%s: up to 2^30 tokens a call (got %ld)", what, T);
     SA_REQUIRE((long)B * Hk <= 65535, SA_ERR_UNSUPPORTED, "%s: up to 65535 states a call (got %d x %d)", what, B, Hk);
     return SA_OK;
 }
@@ -567,7 +637,7 @@ extern "C" int sa_decay_attention(const void *q, long q_stride, const void *k, l
     Args a{};
     a.roles = 1;
     a.seq = sequences(offsets_or_null, T, B, p);
-    a.g = log_decay, a.Hk = Hk, a.dv = dv, a.state = (long)d * dv, a.slots = slots_or_null, a.places = n_slots;
+    a.g = log_decay, a.Hk = Hk, a.dv = dv, a.state = d * dv, a.slots = slots_or_null, a.places = n_slots;
     Role &r = a.role[0];
     r.q = {q, q_stride, d}, r.k = {k, k_stride, d}, r.v = {v, v_stride, dv}, r.out = {out, out_stride, dv};
     r.outs = H / Hk, r.sums = 1, r.shift = 1;
@@ -619,7 +689,7 @@ extern "C" int sa_decay_attention_backward(const void *dout, long dout_stride, c
     Args a{};
     a.roles = 3;
     a.seq = sequences(offsets_or_null, T, B, p);
-    a.g = log_decay, a.Hk = Hk, a.dv = dv, a.state = (long)d * dv;
+    a.g = log_decay, a.Hk = Hk, a.dv = dv, a.state = d * dv;
     const HeadRows rq{q, q_stride, d}, rk{k, k_stride, d}, rv{v, v_stride, dv}, ro{dout, dout_stride, dv};
     const int G = H / Hk;
     // dv and dq first: with segments, their roles are also those whose states are summed, R and (transposed) S
