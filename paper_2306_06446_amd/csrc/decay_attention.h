@@ -2,69 +2,114 @@
 // sequences and their segments).
 #pragma once
 
+#include <type_traits>
+#include <utility>
+
 #include "common.h"
 #include "row_types.h"
 
 namespace sa {
 namespace decay {
 
-typedef __bf16 b8 __attribute__((ext_vector_type(8)));
-typedef __bf16 b4 __attribute__((ext_vector_type(4)));
 typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f2 __attribute__((ext_vector_type(2)));
 typedef short s4 __attribute__((ext_vector_type(4)));
+template <class E, int N>
+using Vec = E __attribute__((ext_vector_type(N)));
 
 constexpr int kChunk = 64;               // tokens of a chunk
-constexpr int kSlice = 64;               // columns of the result (and of the state) that a workgroup has
-constexpr int kThreads = 256;
+constexpr int kHalf = 64;                // columns of the result (and of the state) to four wavefronts
 
-// Values as sums of bf16 terms, each the rounding of what the ones before it leave: of an operand in memory as many as hold it exactly (a
-// bf16 value is one, an fp16 value two, an fp32 value three), whatever its magnitude: an fp16 product may be far outside of fp16.
-// What is computed on the way (probabilities, the state) is 2 terms where the result is rounded to 16 bits (off by 2^-18 of itself at most, the result's
-// own rounding is 2^-9 or 2^-12), else 3 (2^-27).  What is added to the fp32 state is 3 terms always.  `ORDER`: products of term i and term j are
-// left out where i + j is above it: 2^-9 (i + j) of the operands' product.
+// Operands of the matrix cores as sums of 16-bit terms, each the rounding of what the ones before it leave.  What is in memory enters exactly: a
+// bf16 or fp16 value is one term of its own type, an fp32 value three of bf16.  What is computed on the way (products q k, the state) is 2 terms where
+// the result is rounded to 16 bits, else 3; what is added to the fp32 state 2 of fp16 or 3 of bf16.  `ORDER`: products of term i and
+// term j are left out where i + j is above it.  A value in two terms of bf16 is off by 2^-18 of itself at most (the result's own rounding is 2^-9),
+// in three by 2^-27, in two of fp16 by 2^-24, if it is not too small for fp16 nor too large: what meets fp16 operands is scaled by a power of
+// two (Scale), one for each sum, that puts its largest term below 2^15.  Terms of 2^-17 of that and more keep their 22 bits, smaller ones
+// are off by 2^-40 of the largest.
 template <class T> struct Terms;
-template <> struct Terms<bf16_t> { static constexpr int RAW = 1, MADE = 2, ORDER_RAW = 0, ORDER = 1; };
-template <> struct Terms<f16_t> { static constexpr int RAW = 2, MADE = 2, ORDER_RAW = 1, ORDER = 1; };
-template <> struct Terms<float> { static constexpr int RAW = 3, MADE = 3, ORDER_RAW = 2, ORDER = 2; };
-constexpr int kUpdateTerms = 3, kUpdateOrder = 2;
+template <> struct Terms<bf16_t> { typedef bf16_t E; static constexpr int RAW = 1, MADE = 2, ADDED = 3, ORDER_RAW = 0, ORDER = 1, ORDER_ADDED = 2; static constexpr bool SCALED = false; };
+template <> struct Terms<f16_t> { typedef f16_t E; static constexpr int RAW = 1, MADE = 2, ADDED = 2, ORDER_RAW = 0, ORDER = 1, ORDER_ADDED = 1; static constexpr bool SCALED = true; };
+template <> struct Terms<float> { typedef bf16_t E; static constexpr int RAW = 3, MADE = 3, ADDED = 3, ORDER_RAW = 2, ORDER = 2, ORDER_ADDED = 2; static constexpr bool SCALED = false; };
 
-typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-typedef float f2 __attribute__((ext_vector_type(2)));
+// f(0), f(1), ... with constants.
+template <class F, int... I>
+__device__ inline void each_of(std::integer_sequence<int, I...>, F f) { (f(std::integral_constant<int, I>()), ...); }
+template <int N, class F>
+__device__ inline void each(F f) { each_of(std::make_integer_sequence<int, N>(), f); }
 
-template <int N, class V, int W>
-__device__ inline void split(const float (&x)[W], V (&t)[N]) {
-#pragma unroll
-    for (int i = 0; i < W; i += 2) {
-        f2 r = {x[i], x[i + 1]};
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const b2 h = __builtin_convertvector(r, b2);     // one instruction for two values
+// Zeros that the compiler does not know as such.  An array that is cleared with known ones is one piece of memory to it, then one vector of 16
+// registers, which moves, and leaves the registers, as a whole: 20 KB of moves to scratch memory a wavefront.
+__device__ inline f4 zeros() {
+    float z = 0.0f;
+    asm("" : "+v"(z));
+    return f4{z, z, z, z};
+}
+
+template <class E, int N, int W>
+__device__ inline void split(const float (&x)[W], Vec<E, W> (&t)[N], float up = 1.0f) {
+    each<W / 2>([&](auto pair) {
+        constexpr int i = 2 * pair;
+        f2 r = {x[i] * up, x[i + 1] * up};
+        each<N>([&](auto term) {
+            constexpr int n = term;
+            const Vec<E, 2> h = __builtin_convertvector(r, Vec<E, 2>);     // one instruction for two values
             t[n][i] = h[0], t[n][i + 1] = h[1];
             if (n + 1 < N) r[0] -= (float)h[0], r[1] -= (float)h[1];
-        }
+        });
+    });
+}
+
+// Powers of two that bring values of magnitude m and less below 2^15, and back.  (Below 2^-112 and for infinities as far as there are such powers.)
+struct Scale {
+    float up, down;
+    __device__ inline explicit Scale(float m) {
+        int e = (int)(__builtin_bit_cast(uint32_t, m) >> 23);
+        e = e < 15 ? 15 : e > 254 ? 254 : e;
+        up = __builtin_bit_cast(float, (uint32_t)(268 - e) << 23);
+        down = __builtin_bit_cast(float, (uint32_t)(e - 14) << 23);
     }
+};
+template <int W>
+__device__ inline float largest(const float (&x)[W], float m = 0.0f) {
+    each<W>([&](auto i) { m = fmaxf(m, fabsf(x[i])); });
+    return m;
+}
+// The largest of the four lanes of a column of the matrix cores' results.
+__device__ inline float column_max(float m) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, m);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const uint32_t r0 = r[0], r1 = r[1];
+    const uint32_t h = __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, r0), __builtin_bit_cast(float, r1)));
+    const auto s = __builtin_amdgcn_permlane16_swap(h, h, false, false);
+    const uint32_t s0 = s[0], s1 = s[1];
+    return fmaxf(__builtin_bit_cast(float, s0), __builtin_bit_cast(float, s1));
 }
 
 // c += A B, 16 x 16 x 32, of operands in NA and NB terms.  Lane l has row (column) l % 16 of A (B) and 8 of the 32 places of the
 // sum, those of l / 16; of c it has rows 4 (l / 16) + r of column l % 16.
-template <int ORDER, int NA, int NB>
-__device__ inline void product(f4 &c, const b8 (&a)[NA], const b8 (&b)[NB]) {
+__device__ inline f4 matrix(const Vec<bf16_t, 8> &a, const Vec<bf16_t, 8> &b, const f4 &c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ inline f4 matrix(const Vec<f16_t, 8> &a, const Vec<f16_t, 8> &b, const f4 &c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+template <int ORDER, class E, int NA, int NB>
+__device__ inline void product(f4 &c, const Vec<E, 8> (&a)[NA], const Vec<E, 8> (&b)[NB]) {
 #pragma unroll
     for (int o = (ORDER < NA + NB - 2 ? ORDER : NA + NB - 2); o >= 0; --o) {
 #pragma unroll
         for (int i = 0; i < NA; ++i) {
-            if (o - i >= 0 && o - i < NB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[o - i], c, 0, 0, 0);
+            if (o - i >= 0 && o - i < NB) c = matrix(a[i], b[o - i], c);
         }
     }
 }
 
 // Four tokens of one column: the 16 lanes of a group point at 4 rows (lane / 4 % 4) and 4 blocks of 4 columns (lane % 4), lane l
 // gets column l % 16 of the 4 rows.
-__device__ inline b4 read_transposed(const __bf16 *p) {
-    const s4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)p);
-    return __builtin_bit_cast(b4, v);
+template <class E>
+__device__ inline Vec<E, 4> read_transposed(const E *p) {
+    const s4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)const_cast<E *>(p));
+    return __builtin_bit_cast(Vec<E, 4>, v);
 }
-__device__ inline b8 join(const b4 &a, const b4 &b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+template <class E>
+__device__ inline Vec<E, 8> join(const Vec<E, 4> &a, const Vec<E, 4> &b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
 // Rows of one head, from memory: a base that all lanes share and a 32-bit offset each.  What lies beyond kReach (an offset made kNowhere)
 // reads as zeros and is not written, without a branch.
@@ -91,14 +136,13 @@ struct Eight {
             v = __builtin_bit_cast(vec, x);
         }
     }
-    template <int N>
-    __device__ inline void terms(b8 (&t)[N]) const {
-        if constexpr (sizeof(T) == 2 && N == 1) {
-            t[0] = __builtin_bit_cast(b8, v);
+    template <class E, int N>
+    __device__ inline void terms(Vec<E, 8> (&t)[N]) const {
+        if constexpr (N == 1) {
+            t[0] = v;
         } else {
             float x[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
+            each<8>([&](auto i) { x[i] = (float)v[(int)i]; });
             split(x, t);
         }
     }

@@ -45,12 +45,18 @@ struct Args {
     __device__ inline float *place(float *states, int p, int hk) const { return states + ((long)p * Hk + hk) * state; }
 };
 
-template <class T, int DK>
+// A kernel for keys of up to DK elements and HALVES * 64 columns of the result: 4 wavefronts to 64 columns.
+template <class T_, int DK_, int HALVES_>
 struct Shape {
-    static constexpr int RAW = Terms<T>::RAW, MADE = Terms<T>::MADE;
-    static constexpr int KP = DK + 8, VP = kSlice + 8;       // pitch: rows begin 4 banks apart
-    static constexpr int KPIECES = DK / 32, VPIECES = kSlice / 32;
+    typedef T_ T;
+    typedef typename Terms<T>::E E;
+    static constexpr int DK = DK_, HALVES = HALVES_, RAW = Terms<T>::RAW, MADE = Terms<T>::MADE, ADDED = Terms<T>::ADDED;
+    static constexpr bool SCALED = Terms<T>::SCALED;
+    static constexpr int THREADS = 256 * HALVES, COLS = kHalf * HALVES;
+    static constexpr int KP = DK + 8, VP = COLS + 8;         // pitch: rows begin 4 banks apart
+    static constexpr int KPIECES = kChunk * DK / 8 / THREADS, VPIECES = kChunk * COLS / 8 / THREADS;
     static constexpr int TILES = DK / 16;
+    static_assert(kChunk * DK / 8 % THREADS == 0 || DK == 32, "a thread has whole pieces of the keys");
 };
 
 // Where a workgroup's tokens are in one tensor: row i of chunk c is token first + c kChunk + i, or first - c kChunk - i.
@@ -72,143 +78,198 @@ struct Tokens {
 };
 
 // The keys and values of one chunk: from memory to registers, from there to LDS.
-template <class T, int DK>
+template <class P>
 struct Rows {
-    using P = Shape<T, DK>;
-    Eight<T> k[P::KPIECES], v[P::VPIECES];
-    uint32_t kat[P::KPIECES], vat[P::VPIECES];
-    __device__ inline static int krow(int j) { return ((int)threadIdx.x + kThreads * j) / (DK / 8); }
-    __device__ inline static int kcol(int j) { return ((int)threadIdx.x + kThreads * j) % (DK / 8) * 8; }
-    __device__ inline static int vrow(int j) { return ((int)threadIdx.x + kThreads * j) / (kSlice / 8); }
-    __device__ inline static int vcol(int j) { return ((int)threadIdx.x + kThreads * j) % (kSlice / 8) * 8; }
+    typedef typename P::T T;
+    typedef typename P::E E;
+    static constexpr int KN = P::KPIECES > 0 ? P::KPIECES : 1, VN = P::VPIECES;      // (keys of 32 elements: half of 512 threads)
+    Eight<T> k[KN], v[VN];
+    uint32_t kat[KN], vat[VN];
+    __device__ inline static int krow(int j) { return ((int)threadIdx.x + P::THREADS * j) / (P::DK / 8); }
+    __device__ inline static int kcol(int j) { return ((int)threadIdx.x + P::THREADS * j) % (P::DK / 8) * 8; }
+    __device__ inline static int vrow(int j) { return ((int)threadIdx.x + P::THREADS * j) / (P::COLS / 8); }
+    __device__ inline static int vcol(int j) { return ((int)threadIdx.x + P::THREADS * j) % (P::COLS / 8) * 8; }
     __device__ inline void places(const Tokens &kt, int kwidth, const Tokens &vt, int vwidth) {
-#pragma unroll
-        for (int j = 0; j < P::KPIECES; ++j) kat[j] = kcol(j) < kwidth ? kt.row(krow(j)) + kcol(j) * (uint32_t)sizeof(T) : kNowhere;
-#pragma unroll
-        for (int j = 0; j < P::VPIECES; ++j) vat[j] = vcol(j) < vwidth ? vt.row(vrow(j)) + vcol(j) * (uint32_t)sizeof(T) : kNowhere;
+        each<KN>([&](auto j_) {
+            constexpr int j = j_;
+            kat[j] = kcol(j) < kwidth ? kt.row(krow(j)) + kcol(j) * (uint32_t)sizeof(T) : kNowhere;
+        });
+        each<VN>([&](auto j_) {
+            constexpr int j = j_;
+            vat[j] = vcol(j) < vwidth ? vt.row(vrow(j)) + vcol(j) * (uint32_t)sizeof(T) : kNowhere;
+        });
     }
     __device__ inline void load(__amdgpu_buffer_rsrc_t kp, __amdgpu_buffer_rsrc_t vp, int n) {
-#pragma unroll
-        for (int j = 0; j < P::KPIECES; ++j) k[j].load(kp, krow(j) < n ? kat[j] : kNowhere);
-#pragma unroll
-        for (int j = 0; j < P::VPIECES; ++j) v[j].load(vp, vrow(j) < n ? vat[j] : kNowhere);
+        each<KN>([&](auto j_) {
+            constexpr int j = j_;
+            k[j].load(kp, krow(j) < n ? kat[j] : kNowhere);
+        });
+        each<VN>([&](auto j_) {
+            constexpr int j = j_;
+            v[j].load(vp, vrow(j) < n ? vat[j] : kNowhere);
+        });
     }
-    __device__ inline void stage(__bf16 (*kl)[kChunk][P::KP], __bf16 (*vl)[kChunk][P::VP]) const {
-#pragma unroll
-        for (int j = 0; j < P::KPIECES; ++j) {
-            b8 t[P::RAW];
+    __device__ inline void stage(E (*kl)[kChunk][P::KP], E (*vl)[kChunk][P::VP]) const {
+        each<KN>([&](auto j_) {
+            constexpr int j = j_;
+            Vec<E, 8> t[P::RAW];
             k[j].terms(t);
-#pragma unroll
-            for (int p = 0; p < P::RAW; ++p) *reinterpret_cast<b8 *>(&kl[p][krow(j)][kcol(j)]) = t[p];
-        }
-#pragma unroll
-        for (int j = 0; j < P::VPIECES; ++j) {
-            b8 t[P::RAW];
+            if (P::KPIECES > 0 || krow(j) < kChunk) {
+                each<P::RAW>([&](auto p_) {
+                    constexpr int p = p_;
+                    *reinterpret_cast<Vec<E, 8> *>(&kl[p][krow(j)][kcol(j)]) = t[p];
+                });
+            }
+        });
+        each<VN>([&](auto j_) {
+            constexpr int j = j_;
+            Vec<E, 8> t[P::RAW];
             v[j].terms(t);
-#pragma unroll
-            for (int p = 0; p < P::RAW; ++p) *reinterpret_cast<b8 *>(&vl[p][vrow(j)][vcol(j)]) = t[p];
-        }
+            each<P::RAW>([&](auto p_) {
+                constexpr int p = p_;
+                *reinterpret_cast<Vec<E, 8> *>(&vl[p][vrow(j)][vcol(j)]) = t[p];
+            });
+        });
     }
 };
 
 // The state of a slice, in registers: wavefront w has columns 16 w to 16 w + 15, lane l rows 16 t + 4 (l / 16) + r of column l % 16.
-template <class T, int DK>
+template <class P>
 struct State {
-    using P = Shape<T, DK>;
+    typedef typename P::E E;
     f4 s[P::TILES];
     __device__ inline void clear() {
-#pragma unroll
-        for (int t = 0; t < P::TILES; ++t) s[t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+        each<P::TILES>([&](auto t_) {
+            constexpr int t = t_;
+            s[t] = zeros();
+        });
     }
     // Four rows of a lane are side by side in memory where the state lies there transposed.
     __device__ inline void load(const float *p, bool transposed, int rows, int cols, int dv, int c0) {
         const int lane = (int)threadIdx.x & 63, g = lane >> 4, col = c0 + 16 * ((int)threadIdx.x >> 6) + (lane & 15);
         clear();
         if (col >= cols) return;
-#pragma unroll
-        for (int t = 0; t < P::TILES; ++t) {
+        each<P::TILES>([&](auto t_) {
+            constexpr int t = t_;
             const int row = 16 * t + 4 * g;
-            if (row >= rows) continue;
+            if (row >= rows) return;
             if (transposed) {
                 s[t] = *reinterpret_cast<const f4 *>(p + col * dv + row);
             } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[t][i] = p[(row + i) * dv + col];
+                each<4>([&](auto i_) {
+                    constexpr int i = i_;
+                    s[t][i] = p[(row + i) * dv + col];
+                });
             }
-        }
+        });
     }
     __device__ inline void store(float *p, bool transposed, int rows, int cols, int dv, int c0) const {
         const int lane = (int)threadIdx.x & 63, g = lane >> 4, col = c0 + 16 * ((int)threadIdx.x >> 6) + (lane & 15);
         if (col >= cols) return;
-#pragma unroll
-        for (int t = 0; t < P::TILES; ++t) {
+        each<P::TILES>([&](auto t_) {
+            constexpr int t = t_;
             const int row = 16 * t + 4 * g;
-            if (row >= rows) continue;
+            if (row >= rows) return;
             if (transposed) {
                 *reinterpret_cast<f4 *>(p + col * dv + row) = s[t];
             } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p[(row + i) * dv + col] = s[t][i];
+                each<4>([&](auto i_) {
+                    constexpr int i = i_;
+                    p[(row + i) * dv + col] = s[t][i];
+                });
             }
-        }
+        });
     }
     // To LDS as terms, for the product with q: [column of the slice][row].  Columns are in the order in which the product's tiles take them: tile
-    // t, row 4 a + b is column 16 a + 4 t + b, so that a lane's results are 16 columns side by side.  The 16 rows of a block change
-    // places with the column's tile (swapped()): the 4 columns of a lane's neighbours would lie in the same banks otherwise.
-    __device__ inline static int swapped(int row, int tile) { return row ^ (16 * (tile & (P::TILES - 1))); }
-    __device__ inline void stage(__bf16 (*sl)[kSlice][P::KP]) const {
-        const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15, place = 16 * (i >> 2) + 4 * ((int)threadIdx.x >> 6) + (i & 3);
-#pragma unroll
-        for (int t = 0; t < P::TILES; ++t) {
-            const float x[4] = {s[t][0], s[t][1], s[t][2], s[t][3]};
-            b4 p[P::MADE];
-            split(x, p);
-#pragma unroll
-            for (int n = 0; n < P::MADE; ++n) *reinterpret_cast<b4 *>(&sl[n][place][swapped(16 * t + 4 * g, i >> 2)]) = p[n];
+    // t, row 4 a + b is column 16 a + 4 t + b of a half, so that a lane's results are 16 columns side by side.  Blocks of 16 rows change
+    // places with the column's tile (swapped()): the 4 columns of a lane's neighbours would lie in the same banks otherwise.  `down`: the
+    // columns' scales.
+    __device__ inline static int swapped(int row, int tile) { return row ^ (16 * (tile & (P::TILES % 4 == 0 ? 3 : P::TILES % 2 == 0 ? 1 : 0))); }
+    __device__ inline void stage(E (*sl)[P::COLS][P::KP], float *down) const {
+        const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15, w = (int)threadIdx.x >> 6;
+        const int place = kHalf * (w >> 2) + 16 * (i >> 2) + 4 * (w & 3) + (i & 3);
+        float up = 1.0f;
+        if constexpr (P::SCALED) {
+            float m = 0.0f;
+            each<P::TILES>([&](auto t_) {
+                constexpr int t = t_;
+                const float x[4] = {s[t][0], s[t][1], s[t][2], s[t][3]};
+                m = largest(x, m);
+            });
+            const Scale scale(column_max(m));
+            up = scale.up;
+            if (g == 0) down[place] = scale.down;
         }
+        each<P::TILES>([&](auto t_) {
+            constexpr int t = t_;
+            const float x[4] = {s[t][0], s[t][1], s[t][2], s[t][3]};
+            Vec<E, 4> p[P::MADE];
+            split(x, p, up);
+            each<P::MADE>([&](auto n_) {
+                constexpr int n = n_;
+                *reinterpret_cast<Vec<E, 4> *>(&sl[n][place][swapped(16 * t + 4 * g, i >> 2)]) = p[n];
+            });
+        });
     }
-    // S += sum_j weight[j] k_j v_j^T over the chunk in LDS.  Both operands have tokens for the places of the sum: transposed
+    // S = carry S + sum_j weight[j] k_j v_j^T over the chunk in LDS.  Both operands have tokens for the places of the sum: transposed
     // reads, in the order 32 s + 16 (e / 4) + 4 (l / 16) + e % 4 for element e.
-    __device__ inline void update(const __bf16 (*kl)[kChunk][P::KP], const __bf16 (*vl)[kChunk][P::VP], const float (&weight)[2][8]) {
+    __device__ inline void update(const E (*kl)[kChunk][P::KP], const E (*vl)[kChunk][P::VP], const float *weight, float carry) {
         const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15, w = (int)threadIdx.x >> 6, row = 4 * g + (i >> 2), col = 4 * (i & 3);
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            float x[8];
-            b8 raw[P::RAW];
-#pragma unroll
-            for (int p = 0; p < P::RAW; ++p)
-                raw[p] = join(read_transposed(&vl[p][32 * ks + row][16 * w + col]), read_transposed(&vl[p][32 * ks + 16 + row][16 * w + col]));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float y = (float)raw[P::RAW - 1][e];
-#pragma unroll
-                for (int p = P::RAW - 2; p >= 0; --p) y += (float)raw[p][e];
-                x[e] = y * weight[ks][e];
-            }
-            b8 b[kUpdateTerms];
-            split(x, b);
-#pragma unroll
-            for (int t = 0; t < P::TILES; ++t) {
-                b8 a[P::RAW];
-#pragma unroll
-                for (int p = 0; p < P::RAW; ++p)
-                    a[p] = join(read_transposed(&kl[p][32 * ks + row][16 * t + col]), read_transposed(&kl[p][32 * ks + 16 + row][16 * t + col]));
-                product<kUpdateOrder>(s[t], a, b);
-            }
+        auto decayed = [&](auto ks, float (&x)[8]) {
+            const f4 w0 = *reinterpret_cast<const f4 *>(&weight[32 * ks + 4 * g]), w1 = *reinterpret_cast<const f4 *>(&weight[32 * ks + 16 + 4 * g]);
+            Vec<E, 8> raw[P::RAW];
+            each<P::RAW>([&](auto p) {
+                raw[p] = join<E>(read_transposed(&vl[p][32 * ks + row][16 * w + col]), read_transposed(&vl[p][32 * ks + 16 + row][16 * w + col]));
+            });
+            each<8>([&](auto e) {
+                float y = (float)raw[P::RAW - 1][(int)e];
+                each<P::RAW - 1>([&](auto p) { y += (float)raw[P::RAW - 2 - p][(int)e]; });
+                x[e] = y * (e < 4 ? w0[e & 3] : w1[e & 3]);
+            });
+        };
+        auto keys = [&](auto ks, auto t, Vec<E, 8> (&a)[P::RAW]) {
+            each<P::RAW>([&](auto p) {
+                a[p] = join<E>(read_transposed(&kl[p][32 * ks + row][16 * t + col]), read_transposed(&kl[p][32 * ks + 16 + row][16 * t + col]));
+            });
+        };
+        if constexpr (P::SCALED) {
+            float x0[8], x1[8];
+            decayed(std::integral_constant<int, 0>(), x0);
+            decayed(std::integral_constant<int, 1>(), x1);
+            const Scale scale(column_max(largest(x1, largest(x0))));
+            Vec<E, 8> b[2][P::ADDED];
+            split(x0, b[0], scale.up);
+            split(x1, b[1], scale.up);
+            each<P::TILES>([&](auto t) {
+                f4 add = zeros();
+                each<2>([&](auto ks) {
+                    Vec<E, 8> a[P::RAW];
+                    keys(ks, t, a);
+                    product<Terms<typename P::T>::ORDER_ADDED>(add, a, b[ks]);
+                });
+                each<4>([&](auto e) { s[t][(int)e] = __builtin_fmaf(add[(int)e], scale.down, s[t][(int)e] * carry); });
+            });
+        } else {
+            each<P::TILES>([&](auto t) { s[t] *= carry; });
+            each<2>([&](auto ks) {
+                float x[8];
+                decayed(ks, x);
+                Vec<E, 8> b[P::ADDED];
+                split(x, b);
+                each<P::TILES>([&](auto t) {
+                    Vec<E, 8> a[P::RAW];
+                    keys(ks, t, a);
+                    product<Terms<typename P::T>::ORDER_ADDED>(s[t], a, b);
+                });
+            });
         }
     }
 };
 
-// Decays of a chunk of n tokens on their way into the state, for the tokens that a lane has in State::update.
-__device__ inline void update_weights(float (&weight)[2][8], float rate, int n, int shift, float factor) {
-    const int g = ((int)threadIdx.x & 63) >> 4;
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int left = n - shift - (32 * ks + 16 * (e >> 2) + 4 * g + (e & 3));
-            weight[ks][e] = left >= 0 ? factor * decay_pow(rate, left) : 0.0f;
-        }
+// Decays of a chunk's n tokens on their way into the state, into LDS: exp(g (n - shift - j)) for token j.
+__device__ inline void stage_weights(float *weight, float rate, int n, int shift, float factor) {
+    const int j = (int)threadIdx.x;
+    if (j < kChunk) weight[j] = n - shift - j >= 0 ? factor * decay_pow(rate, n - shift - j) : 0.0f;
 }
 
 // A sequence's place among the states; -1: none, it begins with zeros and leaves no state.
@@ -226,19 +287,23 @@ __device__ inline const Role &role_of(const Args &a, uint32_t &item) {
 }
 
 // Wavefronts on a SIMD: as many workgroups as have room for their rows in a CU's LDS, unless that would cost registers.
-template <class T, int DK>
+template <class P>
 constexpr int rows_waves() {
-    return std::is_same<T, bf16_t>::value ? (DK <= 32 ? 4 : DK <= 64 ? 3 : 2) : std::is_same<T, f16_t>::value ? (DK <= 32 ? 4 : DK <= 64 ? 2 : 1) : DK <= 32 ? 2 : 1;
+    return P::RAW == 3 ? (P::DK <= 32 ? 2 : P::HALVES) : P::DK <= 32 ? 4 : P::DK <= 64 ? (P::HALVES == 1 ? 3 : 4) : 2;
 }
 
-// Rows of the result.  A workgroup has one segment, one head and a slice of 64 columns and goes through the chunks one after the other; wavefront w has
-// queries 16 w to 16 w + 15 of a chunk, and columns 16 w to 16 w + 15 of the state.
-template <class T, int DK>
-__global__ __launch_bounds__(kThreads, (rows_waves<T, DK>())) void decay_rows_kernel(const Args a) {
-    using P = Shape<T, DK>;
-    __shared__ __attribute__((aligned(16))) __bf16 kl[P::RAW][kChunk][P::KP];
-    __shared__ __attribute__((aligned(16))) __bf16 vl[P::RAW][kChunk][P::VP];
-    __shared__ __attribute__((aligned(16))) __bf16 sl[P::MADE][kSlice][P::KP];
+// Rows of the result.  A workgroup has one segment, one head and a slice of the columns and goes through the chunks one after the other; of each half
+// of the slice, wavefront w has queries 16 w to 16 w + 15 of a chunk, and columns 16 w to 16 w + 15 of the state.
+template <class P>
+__global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kernel(const Args a) {
+    typedef typename P::T T;
+    typedef typename P::E E;
+    constexpr int DK = P::DK;
+    __shared__ __attribute__((aligned(16))) E kl[P::RAW][kChunk][P::KP];
+    __shared__ __attribute__((aligned(16))) E vl[P::RAW][kChunk][P::VP];
+    __shared__ __attribute__((aligned(16))) E sl[P::MADE][P::COLS][P::KP];
+    __shared__ __attribute__((aligned(16))) float down[P::SCALED ? P::COLS : 4];
+    __shared__ __attribute__((aligned(16))) float weight[kChunk], behind[kChunk];      // exp(g (64 - j)) in the latter
     const uint32_t total = a.items[a.roles - 1];
     uint32_t item = xcd_place(total);
     if (item >= total) return;
@@ -246,8 +311,8 @@ __global__ __launch_bounds__(kThreads, (rows_waves<T, DK>())) void decay_rows_ke
     const int kwidth = r.k.width, vwidth = r.v.width, sums = r.sums, shift = r.shift;
     const float update = r.update;
     const bool transposed = r.transposed, reverse = r.reverse;
-    const uint32_t slices = vwidth > kSlice ? 2 : 1;
-    const int c0 = (int)(item % slices) * kSlice;
+    const uint32_t slices = vwidth > P::COLS ? 2 : 1;
+    const int c0 = (int)(item % slices) * P::COLS;
     item /= slices;
     int sub = 0;
     if (r.outs > 1) sub = (int)(item % (uint32_t)r.outs), item /= (uint32_t)r.outs;
@@ -258,8 +323,8 @@ __global__ __launch_bounds__(kThreads, (rows_waves<T, DK>())) void decay_rows_ke
     const int tokens = left < a.seq.seg ? left : a.seq.seg;
     const int out_head = hk * r.outs + sub;
 
-    const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int query = 16 * w + i;
+    const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int w = wave & 3, half = kHalf * (wave >> 2), query = 16 * w + i;
     const float rate = decay_rate(a.g[hk]);
     const int chunks = (tokens + kChunk - 1) / kChunk;
     auto in_chunk = [&](int c) { return tokens - c * kChunk < kChunk ? tokens - c * kChunk : kChunk; };
@@ -270,14 +335,16 @@ __global__ __launch_bounds__(kThreads, (rows_waves<T, DK>())) void decay_rows_ke
     kt.set<T>(r.k, sp, p0, reverse, hk * sums, 0);
     vt.set<T>(r.v, sp, p0, reverse, hk * sums, c0);
     const uint32_t kmore = (uint32_t)kwidth * (uint32_t)sizeof(T), vmore = (uint32_t)vwidth * (uint32_t)sizeof(T);     // to the next head that is added up
-    const uint32_t qat = qt.row(query) + 8 * g * (uint32_t)sizeof(T), oat = ot.row(query) + 16 * g * (uint32_t)sizeof(T);
-    Rows<T, DK> rows;
+    const uint32_t qat = qt.row(query) + 8 * g * (uint32_t)sizeof(T), oat = ot.row(query) + (half + 16 * g) * (uint32_t)sizeof(T);
+    Rows<P> rows;
     rows.places(kt, kwidth, vt, vwidth - c0);
     Eight<T> q[DK / 32];
     auto load_q = [&](int n) {
         const __amdgpu_buffer_rsrc_t p = qt.at();
-#pragma unroll
-        for (int s = 0; s < DK / 32; ++s) q[s].load(p, query < n && 32 * s + 8 * g < kwidth ? qat + 32 * s * (uint32_t)sizeof(T) : kNowhere);
+        each<DK / 32>([&](auto s_) {
+            constexpr int s = s_;
+            q[s].load(p, query < n && 32 * s + 8 * g < kwidth ? qat + 32 * s * (uint32_t)sizeof(T) : kNowhere);
+        });
         qt.base += (uint64_t)qt.next;
     };
     if (chunks > 0) {
@@ -285,7 +352,7 @@ __global__ __launch_bounds__(kThreads, (rows_waves<T, DK>())) void decay_rows_ke
         rows.load(kt.at(), vt.at(), in_chunk(0));
     }
 
-    State<T, DK> state;
+    State<P> state;
     bool live = false;                   // a state that is not zero
     const int place = r.first != nullptr || r.last != nullptr ? state_place(a, sp.seq) : -1;
     float *const last = r.last != nullptr && place >= 0 ? a.place(r.last, place, hk) : nullptr;
@@ -296,35 +363,31 @@ __global__ __launch_bounds__(kThreads, (rows_waves<T, DK>())) void decay_rows_ke
         state.clear();
     }
 
-    float inside[4][4], weight[2][8];
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int far = 16 * (w - t) + i - 4 * g - e;
-            inside[t][e] = far >= 0 ? r.inside * decay_pow(rate, far) : 0.0f;
-        }
+    stage_weights(weight, rate, kChunk < tokens ? kChunk : tokens, shift, update);
+    stage_weights(behind, rate, kChunk, 0, 1.0f);
+    // of the pairs of a query and a key, exp(g (i - j)): within a tile of 16 x 16, and of earlier tiles by way of the tile's first query
+    const float from_first = r.inside * decay_pow(rate, i);
+    f4 inside;
+    each<4>([&](auto e) { inside[(int)e] = i >= 4 * g + e ? r.inside * decay_pow(rate, i - 4 * g - e) : 0.0f; });
     const float into = r.into * decay_pow(rate, query + shift);
-    update_weights(weight, rate, kChunk, shift, update);
     float carry = decay_pow(rate, kChunk);
 
     f4 o[4];
-    b8 qterms[DK / 32][P::RAW];
+    Vec<E, 8> qterms[DK / 32][P::RAW];
     for (int c = 0; c < chunks; ++c) {
         const int n = in_chunk(c);
         const bool more = c + 1 < chunks, add = more || last != nullptr;
-        if (n < kChunk && add) {
-            update_weights(weight, rate, n, shift, update);
-            carry = decay_pow(rate, n);
-        }
+        if (n < kChunk) carry = decay_pow(rate, n);
         for (int h = 0; h < sums; ++h) {
             if (c + h > 0) __syncthreads();
             rows.stage(kl, vl);
             if (h == 0) {
-                if (live) state.stage(sl);
-#pragma unroll
-                for (int s = 0; s < DK / 32; ++s) q[s].terms(qterms[s]);
-                if (more) load_q(in_chunk(c + 1));
+                if (n < kChunk && c > 0) stage_weights(weight, rate, n, shift, update);
+                if (live) state.stage(sl, down);
+                each<DK / 32>([&](auto s_) {
+                    constexpr int s = s_;
+                    q[s].terms(qterms[s]);
+                });
             }
             if (h + 1 < sums) {
                 rows.load(kt.at((uint64_t)(h + 1) * kmore), vt.at((uint64_t)(h + 1) * vmore), n);
@@ -334,90 +397,111 @@ __global__ __launch_bounds__(kThreads, (rows_waves<T, DK>())) void decay_rows_ke
             }
             __syncthreads();
             if (h == 0) {
-#pragma unroll
-                for (int t = 0; t < 4; ++t) o[t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+                each<4>([&](auto t_) {
+                    constexpr int t = t_;
+                    o[t] = zeros();
+                });
                 if (live) {
+                    each<DK / 32>([&](auto s_) {
+                        constexpr int s = s_;
+                        each<4>([&](auto t_) {
+                            constexpr int t = t_;
+                            Vec<E, 8> st[P::MADE];
 #pragma unroll
-                    for (int s = 0; s < DK / 32; ++s) {
-#pragma unroll
-                        for (int t = 0; t < 4; ++t) {
-                            b8 st[P::MADE];
-#pragma unroll
-                            for (int p = 0; p < P::MADE; ++p) st[p] = *reinterpret_cast<const b8 *>(&sl[p][16 * t + i][State<T, DK>::swapped(32 * s + 8 * g, t)]);
+                            for (int p = 0; p < P::MADE; ++p)
+                                st[p] = *reinterpret_cast<const Vec<E, 8> *>(&sl[p][half + 16 * t + i][State<P>::swapped(32 * s + 8 * g, t)]);
                             product<Terms<T>::ORDER>(o[t], st, qterms[s]);
+                        });
+                    });
+                    each<4>([&](auto t_) {
+                        constexpr int t = t_;
+                        if constexpr (P::SCALED) {
+                            o[t] *= *reinterpret_cast<const f4 *>(&down[half + 16 * t + 4 * g]) * into;
+                        } else {
+                            o[t] *= into;
                         }
-                    }
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[t][e] *= into;
+                    });
                 }
             }
-            // (k_j q_i) for 32 keys at a time, which are in the registers of the lanes that have them as the right operand of the product with v
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                if (2 * ks > w) continue;
-                float x[8];
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int t = 2 * ks + half;
-                    f4 s = f4{0.0f, 0.0f, 0.0f, 0.0f};
-                    if (t <= w) {
-#pragma unroll
-                        for (int d = 0; d < DK / 32; ++d) {
-                            b8 kterms[P::RAW];
-#pragma unroll
-                            for (int p = 0; p < P::RAW; ++p) kterms[p] = *reinterpret_cast<const b8 *>(&kl[p][16 * t + i][32 * d + 8 * g]);
-                            product<Terms<T>::ORDER_RAW>(s, kterms, qterms[d]);
-                        }
-                    }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[4 * half + e] = s[e] * inside[t][e];
-                    if (t == w) {        // a product that is not in the sum may be infinite
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) x[4 * half + e] = i >= 4 * g + e ? x[4 * half + e] : 0.0f;
-                    }
+            __builtin_amdgcn_sched_barrier(0);
+            // (k_j q_i), 32 keys at a time in the registers of the lanes that have them as the right operand of the product with v
+            float x[2][8];
+            each<4>([&](auto tile) {
+                constexpr int t = tile;
+                f4 s = f4{0.0f, 0.0f, 0.0f, 0.0f};
+                if (t <= w) {
+                    each<DK / 32>([&](auto d_) {
+                        constexpr int d = d_;
+                        Vec<E, 8> kterms[P::RAW];
+                        each<P::RAW>([&](auto p_) {
+                            constexpr int p = p_;
+                            kterms[p] = *reinterpret_cast<const Vec<E, 8> *>(&kl[p][16 * t + i][32 * d + 8 * g]);
+                        });
+                        product<Terms<T>::ORDER_RAW>(s, kterms, qterms[d]);
+                    });
                 }
-                b8 pt[P::MADE];
-                split(x, pt);
-                const int row = 32 * ks + 4 * g + (i >> 2);
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int col = 16 * (i & 3) + 4 * t;
-                    b8 vterms[P::RAW];
-#pragma unroll
-                    for (int p = 0; p < P::RAW; ++p) vterms[p] = join(read_transposed(&vl[p][row][col]), read_transposed(&vl[p][row + 16][col]));
-                    product<Terms<T>::ORDER>(o[t], vterms, pt);
+                if (t == w) {            // (a product that is not in the sum may be infinite)
+                    each<4>([&](auto e) { x[t / 2][4 * (t % 2) + e] = i >= 4 * g + e ? s[(int)e] * inside[(int)e] : 0.0f; });
+                } else {                 // keys t < w; else s is 0
+                    const f4 far = *reinterpret_cast<const f4 *>(&behind[(kChunk - 16 * (w - t) + 4 * g) & (kChunk - 1)]);
+                    each<4>([&](auto e) { x[t / 2][4 * (t % 2) + e] = s[(int)e] * from_first * far[(int)e]; });
                 }
+            });
+            __builtin_amdgcn_sched_barrier(0);
+            float up = 1.0f, back = 1.0f;
+            if constexpr (P::SCALED) {
+                const Scale scale(column_max(largest(x[1], largest(x[0]))));
+                up = scale.up, back = scale.down;
             }
-            if (add) {
-                if (h == 0 && live) {
-#pragma unroll
-                    for (int t = 0; t < P::TILES; ++t) state.s[t] *= carry;
-                }
-                state.update(kl, vl, weight);
-            }
+            auto values = [&](auto steps) {
+                Vec<E, 8> pt[steps][P::MADE];
+                each<steps>([&](auto ks) { split(x[ks], pt[ks], up); });
+                each<4>([&](auto t) {
+                    const int row = 4 * g + (i >> 2), col = half + 16 * (i & 3) + 4 * t;
+                    f4 sum = P::SCALED ? zeros() : o[t];
+                    each<steps>([&](auto ks) {
+                        Vec<E, 8> vterms[P::RAW];
+                        each<P::RAW>([&](auto p) {
+                            vterms[p] = join<E>(read_transposed(&vl[p][32 * ks + row][col]), read_transposed(&vl[p][32 * ks + row + 16][col]));
+                        });
+                        product<Terms<T>::ORDER>(sum, vterms, pt[ks]);
+                    });
+                    if constexpr (P::SCALED) {
+                        each<4>([&](auto e) { o[t][(int)e] = __builtin_fmaf(sum[(int)e], back, o[t][(int)e]); });
+                    } else {
+                        o[t] = sum;
+                    }
+                });
+            };
+            if (w < 2) values(std::integral_constant<int, 1>());
+            else values(std::integral_constant<int, 2>());
+            __builtin_amdgcn_sched_barrier(0);
+            if (more && h + 1 == sums) load_q(in_chunk(c + 1));
+            if (add) state.update(kl, vl, weight, h == 0 ? carry : 1.0f);
         }
         live = live || add;
         const __amdgpu_buffer_rsrc_t to = ot.at();
         ot.base += (uint64_t)ot.next;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        each<2>([&](auto p_) {
+            constexpr int p = p_;
             float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = o[2 * half + e / 4][e % 4];
-            store_eight<T>(to, query < n && c0 + 16 * g + 8 * half < vwidth ? oat + 8 * half * (uint32_t)sizeof(T) : kNowhere, x);
-        }
+            each<8>([&](auto e_) {
+                constexpr int e = e_;
+                x[e] = o[2 * p + e / 4][e % 4];
+            });
+            store_eight<T>(to, query < n && c0 + half + 16 * g + 8 * p < vwidth ? oat + 8 * p * (uint32_t)sizeof(T) : kNowhere, x);
+        });
     }
     if (last != nullptr) state.store(last, transposed, kwidth, vwidth, a.dv, c0);
 }
 
 // What each segment adds to the state, from a state of zeros.
-template <class T, int DK>
-__global__ __launch_bounds__(kThreads) void decay_states_kernel(const Args a) {
-    using P = Shape<T, DK>;
-    __shared__ __attribute__((aligned(16))) __bf16 kl[P::RAW][kChunk][P::KP];
-    __shared__ __attribute__((aligned(16))) __bf16 vl[P::RAW][kChunk][P::VP];
+template <class P>
+__global__ __launch_bounds__(P::THREADS) void decay_states_kernel(const Args a) {
+    typedef typename P::T T;
+    typedef typename P::E E;
+    __shared__ __attribute__((aligned(16))) E kl[P::RAW][kChunk][P::KP];
+    __shared__ __attribute__((aligned(16))) E vl[P::RAW][kChunk][P::VP];
     const uint32_t total = a.items[a.roles - 1];
     uint32_t item = xcd_place(total);
     if (item >= total) return;
@@ -425,8 +509,8 @@ __global__ __launch_bounds__(kThreads) void decay_states_kernel(const Args a) {
     const int kwidth = r.k.width, vwidth = r.v.width, sums = r.sums, shift = r.shift;
     const float update = r.update;
     const bool reverse = r.reverse;
-    const uint32_t slices = vwidth > kSlice ? 2 : 1;
-    const int c0 = (int)(item % slices) * kSlice;
+    const uint32_t slices = vwidth > P::COLS ? 2 : 1;
+    const int c0 = (int)(item % slices) * P::COLS;
     item /= slices;
     const int hk = (int)(item % (uint32_t)a.Hk);
     const Span sp = a.seq.of_unit(item / (uint32_t)a.Hk);
@@ -435,30 +519,26 @@ __global__ __launch_bounds__(kThreads) void decay_states_kernel(const Args a) {
     if (sp.seg < 0 || left <= 0 || (left <= a.seq.seg && r.last == nullptr)) return;
     const int tokens = left < a.seq.seg ? left : a.seq.seg, chunks = (tokens + kChunk - 1) / kChunk;
     const float rate = decay_rate(a.g[hk]);
-    State<T, DK> state;
+    State<P> state;
     state.clear();
     auto in_chunk = [&](int c) { return tokens - c * kChunk < kChunk ? tokens - c * kChunk : kChunk; };
     Tokens kt, vt;
     kt.set<T>(r.k, sp, p0, reverse, hk * sums, 0);
     vt.set<T>(r.v, sp, p0, reverse, hk * sums, c0);
     const uint32_t kmore = (uint32_t)kwidth * (uint32_t)sizeof(T), vmore = (uint32_t)vwidth * (uint32_t)sizeof(T);
-    Rows<T, DK> rows;
+    Rows<P> rows;
     rows.places(kt, kwidth, vt, vwidth - c0);
     rows.load(kt.at(), vt.at(), in_chunk(0));
-    float weight[2][8];
-    update_weights(weight, rate, kChunk, shift, update);
+    __shared__ __attribute__((aligned(16))) float weight[kChunk];
+    stage_weights(weight, rate, kChunk < tokens ? kChunk : tokens, shift, update);
     float carry = decay_pow(rate, kChunk);
     for (int c = 0; c < chunks; ++c) {
         const int n = in_chunk(c);
-        if (n < kChunk) {
-            update_weights(weight, rate, n, shift, update);
-            carry = decay_pow(rate, n);
-        }
-#pragma unroll
-        for (int t = 0; t < P::TILES; ++t) state.s[t] *= carry;
+        if (n < kChunk) carry = decay_pow(rate, n);
         for (int h = 0; h < sums; ++h) {
             if (c + h > 0) __syncthreads();
             rows.stage(kl, vl);
+            if (n < kChunk && c > 0 && h == 0) stage_weights(weight, rate, n, shift, update);
             if (h + 1 < sums) {
                 rows.load(kt.at((uint64_t)(h + 1) * kmore), vt.at((uint64_t)(h + 1) * vmore), n);
             } else if (c + 1 < chunks) {
@@ -466,17 +546,18 @@ __global__ __launch_bounds__(kThreads) void decay_states_kernel(const Args a) {
                 rows.load(kt.at(), vt.at(), in_chunk(c + 1));
             }
             __syncthreads();
-            state.update(kl, vl, weight);
+            state.update(kl, vl, weight, h == 0 ? carry : 1.0f);
         }
     }
     state.store(a.place(r.sums_out, sp.unit, hk), r.transposed, kwidth, vwidth, a.dv, c0);
 }
 
 // From the segments' sums to the states before them, in their place, and to the state behind the sequence.  A thread has 4 elements.
-__global__ __launch_bounds__(kThreads) void decay_scan_kernel(const Args a) {
+constexpr int kScanThreads = 256;
+__global__ __launch_bounds__(kScanThreads) void decay_scan_kernel(const Args a) {
     const Role &r = a.role[blockIdx.z];
     const int hk = (int)(blockIdx.y % (unsigned)a.Hk), b = (int)(blockIdx.y / (unsigned)a.Hk);
-    const int at = (int)(blockIdx.x * kThreads + threadIdx.x) * 4;
+    const int at = (int)(blockIdx.x * kScanThreads + threadIdx.x) * 4;
     if (at >= a.state) return;
     const Span sp = a.seq.of_sequence(b);
     const int place = r.first != nullptr || r.last != nullptr ? state_place(a, b) : -1;
@@ -548,45 +629,75 @@ size_t plan_bytes(const Plan &p, long T, int B, bool ragged, int Hk, int d, int 
     return (size_t)units * Hk * d * dv * sizeof(float);
 }
 
-constexpr int slices_of(int width) { return (width + kSlice - 1) / kSlice; }
+// The kernel of a role: by the widths of its keys and of its result.  128 columns are eight wavefronts of one workgroup, which read the keys
+// once, where the state's terms of both halves have room in LDS (of fp32 with keys of more than 64 they have not: two workgroups).
+struct Form {
+    int keys, halves;
+    bool operator==(const Form &o) const { return keys == o.keys && halves == o.halves; }
+};
+Form form_of(const Role &r, int type) {
+    Form f;
+    f.keys = r.k.width <= 32 ? 32 : r.k.width <= 64 ? 64 : 128;
+    f.halves = r.v.width > kHalf && !(type == SA_F32 && f.keys > 64) ? 2 : 1;
+    return f;
+}
+int slices_of(const Role &r, const Form &f) { return r.v.width > kHalf * f.halves ? 2 : 1; }
 
-template <class T, class F>
-int by_width(int width, F f) {
-    if (width <= 32) return f(std::integral_constant<int, 32>());
-    if (width <= 64) return f(std::integral_constant<int, 64>());
-    return f(std::integral_constant<int, 128>());
+template <class F>
+int by_form(int type, const Form &f, F run) {
+    return by_type(type, [&](auto t) {
+        typedef decltype(t) T;
+        if (f.halves == 2) {
+            if (f.keys == 32) return run(Shape<T, 32, 2>());
+            if (f.keys == 64) return run(Shape<T, 64, 2>());
+            if constexpr (sizeof(T) == 2) return run(Shape<T, 128, 2>());
+        }
+        if (f.keys == 32) return run(Shape<T, 32, 1>());
+        if (f.keys == 64) return run(Shape<T, 64, 1>());
+        return run(Shape<T, 128, 1>());
+    });
 }
 
-// The rows of all roles in one launch; the states' sums and their scan before it where there are segments.
+// Roles of one form are one launch.
+template <class F>
+int by_forms(const char *what, int type, const Args &a, int roles, bool rows, F run) {
+    bool done[3] = {false, false, false};
+    for (int r = 0; r < roles; ++r) {
+        if (done[r]) continue;
+        const Form f = form_of(a.role[r], type);
+        Args some = a;
+        some.roles = 0;
+        long total = 0;
+        for (int s = r; s < roles; ++s) {
+            if (done[s] || !(form_of(a.role[s], type) == f)) continue;
+            done[s] = true;
+            total += a.seq.units() * a.Hk * (rows ? a.role[s].outs : 1) * slices_of(a.role[s], f);
+            some.role[some.roles] = a.role[s];
+            some.items[some.roles++] = (uint32_t)total;
+        }
+        SA_REQUIRE(total < (1L << 31) - 8, SA_ERR_UNSUPPORTED, "%s: too many heads and tokens for one launch", what);
+        SA_TRY(by_form(type, f, [&](auto shape) {
+            run(shape, dim3((unsigned)xcd_blocks(total)), some);
+            return check_launch(what);
+        }));
+    }
+    return SA_OK;
+}
+
+// The rows of all roles; before them, where there are segments, the sums of the first `states` roles and their scan.
 int launch(const char *what, int type, Args a, const Plan &p, int states, hipStream_t st) {
-    const long units = a.seq.units();
-    if (units == 0) return SA_OK;
-    int widest = 0;
-    for (int r = 0; r < a.roles; ++r) widest = a.role[r].k.width > widest ? a.role[r].k.width : widest;
-    long total = 0;
-    for (int r = 0; r < a.roles; ++r) a.items[r] = (uint32_t)(total += units * a.Hk * a.role[r].outs * slices_of(a.role[r].out.width));
-    SA_REQUIRE(total < (1L << 31) - 8, SA_ERR_UNSUPPORTED, "%s: too many heads and tokens for one launch", what);
+    if (a.seq.units() == 0) return SA_OK;
     if (p.seg > 0) {
-        Args s = a;
-        s.roles = states;
-        long sums = 0;
-        for (int r = 0; r < states; ++r) s.items[r] = (uint32_t)(sums += units * a.Hk * slices_of(s.role[r].v.width));
-        const int rc = by_type(type, [&](auto t) {
-            return by_width<decltype(t)>(widest, [&](auto k) {
-                decay_states_kernel<decltype(t), decltype(k)::value><<<dim3((unsigned)xcd_blocks(sums)), dim3(kThreads), 0, st>>>(s);
-                return check_launch(what);
-            });
-        });
-        if (rc != SA_OK) return rc;
-        decay_scan_kernel<<<dim3((unsigned)((a.state / 4 + kThreads - 1) / kThreads), (unsigned)(a.Hk * a.seq.B), (unsigned)states), dim3(kThreads), 0, st>>>(s);
-        if (const int rc2 = check_launch(what); rc2 != SA_OK) return rc2;
+        SA_TRY(by_forms(what, type, a, states, false, [&](auto shape, dim3 grid, const Args &some) {
+            decay_states_kernel<decltype(shape)><<<grid, dim3(decltype(shape)::THREADS), 0, st>>>(some);
+        }));
+        const dim3 grid((unsigned)((a.state / 4 + kScanThreads - 1) / kScanThreads), (unsigned)(a.Hk * a.seq.B), (unsigned)states);
+        decay_scan_kernel<<<grid, dim3(kScanThreads), 0, st>>>(a);
+        SA_TRY(check_launch(what));
         for (int r = 0; r < a.roles; ++r) a.role[r].first = nullptr, a.role[r].last = nullptr;
     }
-    return by_type(type, [&](auto t) {
-        return by_width<decltype(t)>(widest, [&](auto k) {
-            decay_rows_kernel<decltype(t), decltype(k)::value><<<dim3((unsigned)xcd_blocks(total)), dim3(kThreads), 0, st>>>(a);
-            return check_launch(what);
-        });
+    return by_forms(what, type, a, a.roles, true, [&](auto shape, dim3 grid, const Args &some) {
+        decay_rows_kernel<decltype(shape)><<<grid, dim3(decltype(shape)::THREADS), 0, st>>>(some);
     });
 }
 
@@ -603,7 +714,7 @@ int check_sequences(const char *what, int type, long T, int B, bool ragged, int 
 
 extern "C" size_t sa_decay_attention_workspace_bytes(long T, int B, int H, int Hk, int d, int dv, int ragged) {
     if (check_sequences("", SA_F32, T, B, ragged != 0, H, Hk, d, dv) != SA_OK) return 0;
-    const long outs = (long)(H / Hk) * slices_of(dv);
+    const long outs = H / Hk;
     const size_t a = plan_bytes(make_plan(T, B, Hk, outs, ragged != 0, false), T, B, ragged != 0, Hk, d, dv);
     const size_t b = plan_bytes(make_plan(T, B, Hk, outs, ragged != 0, H != Hk), T, B, ragged != 0, Hk, d, dv);
     return a > b ? a : b;
@@ -630,7 +741,7 @@ extern "C" int sa_decay_attention(const void *q, long q_stride, const void *k, l
                    sa::aligned4(offsets_or_null) && sa::aligned4(slots_or_null),
                SA_ERR_ALIGN, "%s: pointers must be 16-byte aligned", what);
     if (B == 0 || (T == 0 && state_out_or_null == nullptr)) return SA_OK;
-    const Plan p = make_plan(T, B, Hk, (long)(H / Hk) * slices_of(dv), ragged, H != Hk && state_out_or_null != nullptr);
+    const Plan p = make_plan(T, B, Hk, (long)(H / Hk), ragged, H != Hk && state_out_or_null != nullptr);
     const size_t need = plan_bytes(p, T, B, ragged, Hk, d, dv);
     SA_REQUIRE(need == 0 || (workspace != nullptr && workspace_bytes >= need), SA_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", what,
                need, workspace_bytes);
@@ -649,7 +760,7 @@ extern "C" int sa_decay_attention(const void *q, long q_stride, const void *k, l
 
 extern "C" size_t sa_decay_attention_backward_workspace_bytes(long T, int B, int H, int Hk, int d, int dv, int ragged) {
     if (check_sequences("", SA_F32, T, B, ragged != 0, H, Hk, d, dv) != SA_OK) return 0;
-    return 2 * plan_bytes(make_plan(T, B, Hk, (long)(H / Hk + 1) * slices_of(d) + slices_of(dv), ragged != 0, false), T, B, ragged != 0, Hk, d, dv);
+    return 2 * plan_bytes(make_plan(T, B, Hk, (long)(H / Hk + 2), ragged != 0, false), T, B, ragged != 0, Hk, d, dv);
 }
 
 extern "C" int sa_decay_attention_backward(const void *dout, long dout_stride, const void *q, long q_stride, const void *k, long k_stride,
@@ -682,7 +793,7 @@ extern "C" int sa_decay_attention_backward(const void *dout, long dout_stride, c
                    sa::aligned16(workspace) && sa::aligned4(offsets_or_null),
                SA_ERR_ALIGN, "%s: pointers must be 16-byte aligned", what);
     if (B == 0 || (T == 0 && dstate_in_or_null == nullptr)) return SA_OK;
-    const Plan p = make_plan(T, B, Hk, (long)(H / Hk + 1) * slices_of(d) + slices_of(dv), ragged, false);
+    const Plan p = make_plan(T, B, Hk, (long)(H / Hk + 2), ragged, false);
     const size_t each = plan_bytes(p, T, B, ragged, Hk, d, dv);
     SA_REQUIRE(each == 0 || (workspace != nullptr && workspace_bytes >= 2 * each), SA_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given",
                what, 2 * each, workspace_bytes);

@@ -21,9 +21,11 @@ struct StepArgs {
     int places;
 };
 
+constexpr int kStepThreads = 256;
+
 // Lanes of COLS threads have 4 columns each; NR rows to a thread, one behind the other, so that its part of q and k is one load.
 template <class T, int COLS, int NR>
-__global__ __launch_bounds__(kThreads) void decay_step_kernel(const StepArgs a) {
+__global__ __launch_bounds__(kStepThreads) void decay_step_kernel(const StepArgs a) {
     constexpr int kHeads = 4;            // heads whose results wait in LDS at once
     __shared__ float red[4][kHeads][4 * COLS];
     const int tid = (int)threadIdx.x, lc = tid % COLS, row = tid / COLS * NR, lane = tid & 63, w = tid >> 6;
@@ -96,11 +98,11 @@ int launch_step(const StepArgs &a, long B, hipStream_t st) {
     const dim3 grid((unsigned)(B * a.Hk * a.blocks));
     const int d = a.k.width;
     if (a.v.width <= 32) {
-        decay_step_kernel<T, 8, 4><<<grid, dim3(kThreads), 0, st>>>(a);
+        decay_step_kernel<T, 8, 4><<<grid, dim3(kStepThreads), 0, st>>>(a);
     } else if (d <= 64) {
-        decay_step_kernel<T, 16, 4><<<grid, dim3(kThreads), 0, st>>>(a);
+        decay_step_kernel<T, 16, 4><<<grid, dim3(kStepThreads), 0, st>>>(a);
     } else {
-        decay_step_kernel<T, 16, 8><<<grid, dim3(kThreads), 0, st>>>(a);
+        decay_step_kernel<T, 16, 8><<<grid, dim3(kStepThreads), 0, st>>>(a);
     }
     return check_launch("sa_decay_attention_step");
 }
