@@ -53,10 +53,15 @@ struct Shape {
     static constexpr int DK = DK_, HALVES = HALVES_, RAW = Terms<T>::RAW, MADE = Terms<T>::MADE, ADDED = Terms<T>::ADDED;
     static constexpr bool SCALED = Terms<T>::SCALED;
     static constexpr int THREADS = 256 * HALVES, COLS = kHalf * HALVES;
-    static constexpr int KP = DK + 8, VP = COLS + 8;         // pitch: rows begin 4 banks apart
+    // Pitch of rows in LDS: 16 rows by 16 bytes (4.6 cycles of a CU a read; 8 with 16 bytes less, 16 without any) and transposed reads of 16 rows by
+    // 32 bytes (4.3) meet each bank evenly.
+    static constexpr int KP = DK + 16, VP = COLS + 16;
+    // Columns of the values, and of the state, are in LDS in the order in which the product with them takes them: tile t's row 4 a + b is column
+    // 16 a + 4 t + b of 64, so that a lane's results are 16 columns side by side while a tile's columns are side by side in LDS.
+    static __device__ inline int column(int at) { return (at & ~63) + 16 * ((at & 15) >> 2) + 4 * ((at & 63) >> 4) + (at & 3); }
     static constexpr int KPIECES = kChunk * DK / 8 / THREADS, VPIECES = kChunk * COLS / 8 / THREADS;
     static constexpr int TILES = DK / 16;
-    static_assert(kChunk * DK / 8 % THREADS == 0 || DK == 32, "a thread has whole pieces of the keys");
+    static_assert(kChunk * DK / 8 % THREADS == 0, "a thread has whole pieces of the keys");
 };
 
 // Where a workgroup's tokens are in one tensor: row i of chunk c is token first + c kChunk + i, or first - c kChunk - i.
@@ -82,7 +87,7 @@ template <class P>
 struct Rows {
     typedef typename P::T T;
     typedef typename P::E E;
-    static constexpr int KN = P::KPIECES > 0 ? P::KPIECES : 1, VN = P::VPIECES;      // (keys of 32 elements: half of 512 threads)
+    static constexpr int KN = P::KPIECES, VN = P::VPIECES;
     Eight<T> k[KN], v[VN];
     uint32_t kat[KN], vat[VN];
     __device__ inline static int krow(int j) { return ((int)threadIdx.x + P::THREADS * j) / (P::DK / 8); }
@@ -114,12 +119,7 @@ struct Rows {
             constexpr int j = j_;
             Vec<E, 8> t[P::RAW];
             k[j].terms(t);
-            if (P::KPIECES > 0 || krow(j) < kChunk) {
-                each<P::RAW>([&](auto p_) {
-                    constexpr int p = p_;
-                    *reinterpret_cast<Vec<E, 8> *>(&kl[p][krow(j)][kcol(j)]) = t[p];
-                });
-            }
+            each<P::RAW>([&](auto p) { *reinterpret_cast<Vec<E, 8> *>(&kl[p][krow(j)][kcol(j)]) = t[p]; });
         });
         each<VN>([&](auto j_) {
             constexpr int j = j_;
@@ -127,13 +127,16 @@ struct Rows {
             v[j].terms(t);
             each<P::RAW>([&](auto p_) {
                 constexpr int p = p_;
-                *reinterpret_cast<Vec<E, 8> *>(&vl[p][vrow(j)][vcol(j)]) = t[p];
+                // 8 columns are 4 of each of two tiles
+                E *to = &vl[p][vrow(j)][(vcol(j) & ~63) + 16 * ((vcol(j) & 8) >> 2) + 4 * ((vcol(j) & 63) >> 4)];
+                *reinterpret_cast<Vec<E, 4> *>(to) = __builtin_shufflevector(t[p], t[p], 0, 1, 2, 3);
+                *reinterpret_cast<Vec<E, 4> *>(to + 16) = __builtin_shufflevector(t[p], t[p], 4, 5, 6, 7);
             });
         });
     }
 };
 
-// The state of a slice, in registers: wavefront w has columns 16 w to 16 w + 15, lane l rows 16 t + 4 (l / 16) + r of column l % 16.
+// The state of a slice, in registers: wavefront w has the columns that LDS has at 16 w to 16 w + 15, lane l rows 16 t + 4 (l / 16) + r of the one at l % 16.
 template <class P>
 struct State {
     typedef typename P::E E;
@@ -146,7 +149,7 @@ struct State {
     }
     // Four rows of a lane are side by side in memory where the state lies there transposed.
     __device__ inline void load(const float *p, bool transposed, int rows, int cols, int dv, int c0) {
-        const int lane = (int)threadIdx.x & 63, g = lane >> 4, col = c0 + 16 * ((int)threadIdx.x >> 6) + (lane & 15);
+        const int lane = (int)threadIdx.x & 63, g = lane >> 4, col = c0 + P::column(16 * ((int)threadIdx.x >> 6) + (lane & 15));
         clear();
         if (col >= cols) return;
         each<P::TILES>([&](auto t_) {
@@ -164,7 +167,7 @@ struct State {
         });
     }
     __device__ inline void store(float *p, bool transposed, int rows, int cols, int dv, int c0) const {
-        const int lane = (int)threadIdx.x & 63, g = lane >> 4, col = c0 + 16 * ((int)threadIdx.x >> 6) + (lane & 15);
+        const int lane = (int)threadIdx.x & 63, g = lane >> 4, col = c0 + P::column(16 * ((int)threadIdx.x >> 6) + (lane & 15));
         if (col >= cols) return;
         each<P::TILES>([&](auto t_) {
             constexpr int t = t_;
@@ -180,14 +183,9 @@ struct State {
             }
         });
     }
-    // To LDS as terms, for the product with q: [column of the slice][row].  Columns are in the order in which the product's tiles take them: tile
-    // t, row 4 a + b is column 16 a + 4 t + b of a half, so that a lane's results are 16 columns side by side.  Blocks of 16 rows change
-    // places with the column's tile (swapped()): the 4 columns of a lane's neighbours would lie in the same banks otherwise.  `down`: the
-    // columns' scales.
-    __device__ inline static int swapped(int row, int tile) { return row ^ (16 * (tile & (P::TILES % 4 == 0 ? 3 : P::TILES % 2 == 0 ? 1 : 0))); }
+    // To LDS as terms, for the product with q: [column][row].  `down`: the columns' scales.
     __device__ inline void stage(E (*sl)[P::COLS][P::KP], float *down) const {
-        const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15, w = (int)threadIdx.x >> 6;
-        const int place = kHalf * (w >> 2) + 16 * (i >> 2) + 4 * (w & 3) + (i & 3);
+        const int lane = (int)threadIdx.x & 63, g = lane >> 4, at = 16 * ((int)threadIdx.x >> 6) + (lane & 15);
         float up = 1.0f;
         if constexpr (P::SCALED) {
             float m = 0.0f;
@@ -198,7 +196,7 @@ struct State {
             });
             const Scale scale(column_max(m));
             up = scale.up;
-            if (g == 0) down[place] = scale.down;
+            if (g == 0) down[at] = scale.down;
         }
         each<P::TILES>([&](auto t_) {
             constexpr int t = t_;
@@ -207,7 +205,7 @@ struct State {
             split(x, p, up);
             each<P::MADE>([&](auto n_) {
                 constexpr int n = n_;
-                *reinterpret_cast<Vec<E, 4> *>(&sl[n][place][swapped(16 * t + 4 * g, i >> 2)]) = p[n];
+                *reinterpret_cast<Vec<E, 4> *>(&sl[n][at][16 * t + 4 * g]) = p[n];
             });
         });
     }
@@ -286,14 +284,95 @@ __device__ inline const Role &role_of(const Args &a, uint32_t &item) {
     return a.role[r];
 }
 
-// Wavefronts on a SIMD: as many workgroups as have room for their rows in a CU's LDS, unless that would cost registers.
+// The queries of a wavefront, for the product with the keys (and with the state).
 template <class P>
-constexpr int rows_waves() {
-    return P::RAW == 3 ? (P::DK <= 32 ? 2 : P::HALVES) : P::DK <= 32 ? 4 : P::DK <= 64 ? (P::HALVES == 1 ? 3 : 4) : 2;
+struct Queries {
+    Eight<typename P::T> q[P::DK / 32];
+    __device__ inline void load(__amdgpu_buffer_rsrc_t from, uint32_t at, bool there, int width) {
+        const int g = ((int)threadIdx.x & 63) >> 4;
+        each<P::DK / 32>([&](auto s) {
+            q[s].load(from, there && 32 * s + 8 * g < width ? at + 32 * s * (uint32_t)sizeof(typename P::T) : kNowhere);
+        });
+    }
+    __device__ inline void terms(Vec<typename P::E, 8> (&t)[P::DK / 32][P::RAW]) const {
+        each<P::DK / 32>([&](auto s) { q[s].terms(t[s]); });
+    }
+};
+
+// o += sum_j exp(g (i - j)) (q_i k_j) v_j for the keys in LDS: those of the queries' own chunk, of which wavefront w has queries 16 w to 16 w + 15,
+// or all 64 of an earlier one (EARLIER).  (k_j q_i) comes out in the registers of the lanes that have it as the right operand of the
+// product with v.  Decays: `inside` within a tile of 16 x 16; of earlier tiles `from_first`, which counts from the tile's (the chunk's) first
+// query, and `behind`, which counts to it from the keys of 64 places before.
+template <class P, bool EARLIER, class F>
+__device__ inline void add_values(f4 (&o)[4], const Vec<typename P::E, 8> (&q)[P::DK / 32][P::RAW], const typename P::E (*kl)[kChunk][P::KP],
+                                  const typename P::E (*vl)[kChunk][P::VP], int w, int half, const f4 &inside, float from_first, const float *behind,
+                                  F keys_done) {
+    typedef typename P::E E;
+    typedef Terms<typename P::T> N;
+    const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15;
+    float x[2][8];
+    each<4>([&](auto tile) {
+        constexpr int t = tile;
+        f4 s = f4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (EARLIER || t <= w) {
+            each<P::DK / 32>([&](auto d) {
+                Vec<E, 8> kterms[P::RAW];
+                each<P::RAW>([&](auto p) { kterms[p] = *reinterpret_cast<const Vec<E, 8> *>(&kl[p][16 * t + i][32 * d + 8 * g]); });
+                product<N::ORDER_RAW>(s, kterms, q[d]);
+            });
+        }
+        if (!EARLIER && t == w) {        // (a product that is not in the sum may be infinite)
+            each<4>([&](auto e) { x[t / 2][4 * (t % 2) + e] = i >= 4 * g + e ? s[(int)e] * inside[(int)e] : 0.0f; });
+        } else {                         // (of later tiles s is 0)
+            const f4 far = *reinterpret_cast<const f4 *>(&behind[EARLIER ? 16 * t + 4 * g : (kChunk - 16 * (w - t) + 4 * g) & (kChunk - 1)]);
+            each<4>([&](auto e) { x[t / 2][4 * (t % 2) + e] = s[(int)e] * from_first * far[(int)e]; });
+        }
+    });
+    keys_done();
+    __builtin_amdgcn_sched_barrier(0);
+    float up = 1.0f, back = 1.0f;
+    if constexpr (P::SCALED) {
+        const Scale scale(column_max(largest(x[1], largest(x[0]))));
+        up = scale.up, back = scale.down;
+    }
+    auto values = [&](auto steps) {
+        Vec<E, 8> pt[steps][P::MADE];
+        each<steps>([&](auto ks) { split(x[ks], pt[ks], up); });
+        each<4>([&](auto t) {
+            const int row = 4 * g + (i >> 2), col = half + 16 * t + 4 * (i & 3);
+            f4 sum = P::SCALED ? zeros() : o[t];
+            each<steps>([&](auto ks) {
+                Vec<E, 8> vterms[P::RAW];
+                each<P::RAW>([&](auto p) {
+                    vterms[p] = join<E>(read_transposed(&vl[p][32 * ks + row][col]), read_transposed(&vl[p][32 * ks + row + 16][col]));
+                });
+                product<N::ORDER>(sum, vterms, pt[ks]);
+            });
+            if constexpr (P::SCALED) {
+                each<4>([&](auto e) { o[t][(int)e] = __builtin_fmaf(sum[(int)e], back, o[t][(int)e]); });
+            } else {
+                o[t] = sum;
+            }
+        });
+    };
+    if (EARLIER || w >= 2) values(std::integral_constant<int, 2>());
+    else values(std::integral_constant<int, 1>());
+    __builtin_amdgcn_sched_barrier(0);
 }
 
-// Rows of the result.  A workgroup has one segment, one head and a slice of the columns and goes through the chunks one after the other; of each half
-// of the slice, wavefront w has queries 16 w to 16 w + 15 of a chunk, and columns 16 w to 16 w + 15 of the state.
+// Wavefronts on a SIMD: as many workgroups as have room for their rows in a CU's LDS, unless registers would go to scratch memory, whose loads wait for
+// the rows that are under way (8 x 16384 tokens, 4 heads of 64, bf16: 65 us with 165 registers, 93 with 168 and 22 in memory).
+template <class P>
+constexpr int rows_waves() {
+    return P::RAW == 3 ? (P::DK <= 32 || P::HALVES == 2 ? 2 : 1) : P::DK <= 64 ? 3 : 2;
+}
+
+// Whether the next queries are asked for before the present ones have met the keys, which takes registers of their own.
+template <class P>
+constexpr bool early_queries() { return P::RAW == 3 || P::DK == 128; }
+
+// Rows of the result.  A workgroup has one segment, the heads of one state and a slice of the columns and goes through the chunks one after the other;
+// of each half of the slice, wavefront w has queries 16 w to 16 w + 15 of a chunk, and columns 16 w to 16 w + 15 of the state.
 template <class P>
 __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kernel(const Args a) {
     typedef typename P::T T;
@@ -308,20 +387,17 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
     uint32_t item = xcd_place(total);
     if (item >= total) return;
     const Role &r = role_of(a, item);
-    const int kwidth = r.k.width, vwidth = r.v.width, sums = r.sums, shift = r.shift;
+    const int kwidth = r.k.width, vwidth = r.v.width, sums = r.sums, outs = r.outs, shift = r.shift;
     const float update = r.update;
     const bool transposed = r.transposed, reverse = r.reverse;
     const uint32_t slices = vwidth > P::COLS ? 2 : 1;
     const int c0 = (int)(item % slices) * P::COLS;
     item /= slices;
-    int sub = 0;
-    if (r.outs > 1) sub = (int)(item % (uint32_t)r.outs), item /= (uint32_t)r.outs;
     const int hk = (int)(item % (uint32_t)a.Hk);
     const Span sp = a.seq.of_unit(item / (uint32_t)a.Hk);
     const int p0 = sp.seg * a.seq.seg, left = sp.length - p0;
     if (sp.seg < 0 || (left <= 0 && (sp.seg > 0 || r.last == nullptr))) return;
     const int tokens = left < a.seq.seg ? left : a.seq.seg;
-    const int out_head = hk * r.outs + sub;
 
     const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int w = wave & 3, half = kHalf * (wave >> 2), query = 16 * w + i;
@@ -330,25 +406,17 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
     auto in_chunk = [&](int c) { return tokens - c * kChunk < kChunk ? tokens - c * kChunk : kChunk; };
 
     Tokens qt, kt, vt, ot;
-    qt.set<T>(r.q, sp, p0, reverse, out_head, 0);
-    ot.set<T>(r.out, sp, p0, reverse, out_head, c0);
+    qt.set<T>(r.q, sp, p0, reverse, hk * outs, 0);
+    ot.set<T>(r.out, sp, p0, reverse, hk * outs, c0);
     kt.set<T>(r.k, sp, p0, reverse, hk * sums, 0);
     vt.set<T>(r.v, sp, p0, reverse, hk * sums, c0);
-    const uint32_t kmore = (uint32_t)kwidth * (uint32_t)sizeof(T), vmore = (uint32_t)vwidth * (uint32_t)sizeof(T);     // to the next head that is added up
+    const uint32_t kmore = (uint32_t)kwidth * (uint32_t)sizeof(T), vmore = (uint32_t)vwidth * (uint32_t)sizeof(T);     // to the next head
     const uint32_t qat = qt.row(query) + 8 * g * (uint32_t)sizeof(T), oat = ot.row(query) + (half + 16 * g) * (uint32_t)sizeof(T);
     Rows<P> rows;
     rows.places(kt, kwidth, vt, vwidth - c0);
-    Eight<T> q[DK / 32];
-    auto load_q = [&](int n) {
-        const __amdgpu_buffer_rsrc_t p = qt.at();
-        each<DK / 32>([&](auto s_) {
-            constexpr int s = s_;
-            q[s].load(p, query < n && 32 * s + 8 * g < kwidth ? qat + 32 * s * (uint32_t)sizeof(T) : kNowhere);
-        });
-        qt.base += (uint64_t)qt.next;
-    };
+    Queries<P> q;
     if (chunks > 0) {
-        load_q(in_chunk(0));
+        q.load(qt.at(), qat, query < in_chunk(0), kwidth);
         rows.load(kt.at(), vt.at(), in_chunk(0));
     }
 
@@ -365,7 +433,6 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
 
     stage_weights(weight, rate, kChunk < tokens ? kChunk : tokens, shift, update);
     stage_weights(behind, rate, kChunk, 0, 1.0f);
-    // of the pairs of a query and a key, exp(g (i - j)): within a tile of 16 x 16, and of earlier tiles by way of the tile's first query
     const float from_first = r.inside * decay_pow(rate, i);
     f4 inside;
     each<4>([&](auto e) { inside[(int)e] = i >= 4 * g + e ? r.inside * decay_pow(rate, i - 4 * g - e) : 0.0f; });
@@ -374,6 +441,7 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
 
     f4 o[4];
     Vec<E, 8> qterms[DK / 32][P::RAW];
+    // h: of several heads of keys and values that are added up; u: of several heads of queries.  One of the two has more than one.
     for (int c = 0; c < chunks; ++c) {
         const int n = in_chunk(c);
         const bool more = c + 1 < chunks, add = more || last != nullptr;
@@ -384,10 +452,6 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
             if (h == 0) {
                 if (n < kChunk && c > 0) stage_weights(weight, rate, n, shift, update);
                 if (live) state.stage(sl, down);
-                each<DK / 32>([&](auto s_) {
-                    constexpr int s = s_;
-                    q[s].terms(qterms[s]);
-                });
             }
             if (h + 1 < sums) {
                 rows.load(kt.at((uint64_t)(h + 1) * kmore), vt.at((uint64_t)(h + 1) * vmore), n);
@@ -396,103 +460,128 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
                 rows.load(kt.at(), vt.at(), in_chunk(c + 1));
             }
             __syncthreads();
-            if (h == 0) {
-                each<4>([&](auto t_) {
-                    constexpr int t = t_;
-                    o[t] = zeros();
-                });
-                if (live) {
-                    each<DK / 32>([&](auto s_) {
-                        constexpr int s = s_;
-                        each<4>([&](auto t_) {
-                            constexpr int t = t_;
-                            Vec<E, 8> st[P::MADE];
-#pragma unroll
-                            for (int p = 0; p < P::MADE; ++p)
-                                st[p] = *reinterpret_cast<const Vec<E, 8> *>(&sl[p][half + 16 * t + i][State<P>::swapped(32 * s + 8 * g, t)]);
-                            product<Terms<T>::ORDER>(o[t], st, qterms[s]);
-                        });
-                    });
-                    each<4>([&](auto t_) {
-                        constexpr int t = t_;
-                        if constexpr (P::SCALED) {
-                            o[t] *= *reinterpret_cast<const f4 *>(&down[half + 16 * t + 4 * g]) * into;
-                        } else {
-                            o[t] *= into;
-                        }
-                    });
-                }
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            // (k_j q_i), 32 keys at a time in the registers of the lanes that have them as the right operand of the product with v
-            float x[2][8];
-            each<4>([&](auto tile) {
-                constexpr int t = tile;
-                f4 s = f4{0.0f, 0.0f, 0.0f, 0.0f};
-                if (t <= w) {
-                    each<DK / 32>([&](auto d_) {
-                        constexpr int d = d_;
-                        Vec<E, 8> kterms[P::RAW];
-                        each<P::RAW>([&](auto p_) {
-                            constexpr int p = p_;
-                            kterms[p] = *reinterpret_cast<const Vec<E, 8> *>(&kl[p][16 * t + i][32 * d + 8 * g]);
-                        });
-                        product<Terms<T>::ORDER_RAW>(s, kterms, qterms[d]);
-                    });
-                }
-                if (t == w) {            // (a product that is not in the sum may be infinite)
-                    each<4>([&](auto e) { x[t / 2][4 * (t % 2) + e] = i >= 4 * g + e ? s[(int)e] * inside[(int)e] : 0.0f; });
-                } else {                 // keys t < w; else s is 0
-                    const f4 far = *reinterpret_cast<const f4 *>(&behind[(kChunk - 16 * (w - t) + 4 * g) & (kChunk - 1)]);
-                    each<4>([&](auto e) { x[t / 2][4 * (t % 2) + e] = s[(int)e] * from_first * far[(int)e]; });
-                }
-            });
-            __builtin_amdgcn_sched_barrier(0);
-            float up = 1.0f, back = 1.0f;
-            if constexpr (P::SCALED) {
-                const Scale scale(column_max(largest(x[1], largest(x[0]))));
-                up = scale.up, back = scale.down;
-            }
-            auto values = [&](auto steps) {
-                Vec<E, 8> pt[steps][P::MADE];
-                each<steps>([&](auto ks) { split(x[ks], pt[ks], up); });
-                each<4>([&](auto t) {
-                    const int row = 4 * g + (i >> 2), col = half + 16 * (i & 3) + 4 * t;
-                    f4 sum = P::SCALED ? zeros() : o[t];
-                    each<steps>([&](auto ks) {
-                        Vec<E, 8> vterms[P::RAW];
-                        each<P::RAW>([&](auto p) {
-                            vterms[p] = join<E>(read_transposed(&vl[p][32 * ks + row][col]), read_transposed(&vl[p][32 * ks + row + 16][col]));
-                        });
-                        product<Terms<T>::ORDER>(sum, vterms, pt[ks]);
-                    });
-                    if constexpr (P::SCALED) {
-                        each<4>([&](auto e) { o[t][(int)e] = __builtin_fmaf(sum[(int)e], back, o[t][(int)e]); });
-                    } else {
-                        o[t] = sum;
+            for (int u = 0; u < outs; ++u) {
+                auto next_q = [&] {
+                    if (u + 1 < outs) {
+                        q.load(qt.at((uint64_t)(u + 1) * kmore), qat, query < n, kwidth);
+                    } else if (more && (h + 1 == sums || early_queries<P>())) {
+                        qt.base += (uint64_t)qt.next;
+                        q.load(qt.at(), qat, query < in_chunk(c + 1), kwidth);
                     }
-                });
-            };
-            if (w < 2) values(std::integral_constant<int, 1>());
-            else values(std::integral_constant<int, 2>());
-            __builtin_amdgcn_sched_barrier(0);
-            if (more && h + 1 == sums) load_q(in_chunk(c + 1));
+                };
+                if (h == 0) {
+                    q.terms(qterms);
+                    if (early_queries<P>()) next_q();
+                    each<4>([&](auto t) { o[t] = zeros(); });
+                    if (live) {
+                        each<DK / 32>([&](auto s) {
+                            each<4>([&](auto t) {
+                                Vec<E, 8> st[P::MADE];
+                                each<P::MADE>([&](auto p) {
+                                    st[p] = *reinterpret_cast<const Vec<E, 8> *>(&sl[p][half + 16 * t + i][32 * s + 8 * g]);
+                                });
+                                product<Terms<T>::ORDER>(o[t], st, qterms[s]);
+                            });
+                        });
+                        each<4>([&](auto t) {
+                            if constexpr (P::SCALED) {
+                                o[t] *= *reinterpret_cast<const f4 *>(&down[half + 16 * t + 4 * g]) * into;
+                            } else {
+                                o[t] *= into;
+                            }
+                        });
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                add_values<P, false>(o, qterms, kl, vl, w, half, inside, from_first, behind, [&] { if (!early_queries<P>()) next_q(); });
+                if (h + 1 == sums) {
+                    const __amdgpu_buffer_rsrc_t to = ot.at((uint64_t)u * vmore);
+                    each<2>([&](auto p) {
+                        float x[8];
+                        each<8>([&](auto e) { x[e] = o[2 * p + e / 4][e % 4]; });
+                        store_eight<T>(to, query < n && c0 + half + 16 * g + 8 * p < vwidth ? oat + 8 * p * (uint32_t)sizeof(T) : kNowhere, x);
+                    });
+                }
+            }
             if (add) state.update(kl, vl, weight, h == 0 ? carry : 1.0f);
         }
-        live = live || add;
-        const __amdgpu_buffer_rsrc_t to = ot.at();
         ot.base += (uint64_t)ot.next;
-        each<2>([&](auto p_) {
-            constexpr int p = p_;
-            float x[8];
-            each<8>([&](auto e_) {
-                constexpr int e = e_;
-                x[e] = o[2 * p + e / 4][e % 4];
-            });
-            store_eight<T>(to, query < n && c0 + half + 16 * g + 8 * p < vwidth ? oat + 8 * p * (uint32_t)sizeof(T) : kNowhere, x);
-        });
+        live = live || add;
     }
     if (last != nullptr) state.store(last, transposed, kwidth, vwidth, a.dv, c0);
+}
+
+// Short sequences without a state before or behind them: a workgroup has 64 queries of one head and a slice of the columns, and adds the values of
+// all keys up to them, chunk by chunk, without a state: all queries at once instead of one chunk after the other.
+template <class P>
+__global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_short_kernel(const Args a) {
+    typedef typename P::T T;
+    typedef typename P::E E;
+    constexpr int DK = P::DK;
+    __shared__ __attribute__((aligned(16))) E kl[P::RAW][kChunk][P::KP];
+    __shared__ __attribute__((aligned(16))) E vl[P::RAW][kChunk][P::VP];
+    __shared__ __attribute__((aligned(16))) float behind[kChunk];
+    const uint32_t total = a.items[a.roles - 1];
+    uint32_t item = xcd_place(total);
+    if (item >= total) return;
+    const Role &r = role_of(a, item);
+    const int kwidth = r.k.width, vwidth = r.v.width, sums = r.sums;
+    const bool reverse = r.reverse;
+    const uint32_t slices = vwidth > P::COLS ? 2 : 1;
+    const int c0 = (int)(item % slices) * P::COLS;
+    item /= slices;
+    const int sub = (int)(item % (uint32_t)r.outs);
+    item /= (uint32_t)r.outs;
+    const int hk = (int)(item % (uint32_t)a.Hk);
+    const Span sp = a.seq.of_unit(item / (uint32_t)a.Hk);
+    const int left = sp.length - sp.seg * kChunk;
+    if (sp.seg < 0 || left <= 0) return;
+    const int mine = left < kChunk ? left : kChunk;
+
+    const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int w = wave & 3, half = kHalf * (wave >> 2), query = 16 * w + i;
+    const float rate = decay_rate(a.g[hk]);
+    Tokens qt, kt, vt, ot;
+    qt.set<T>(r.q, sp, sp.seg * kChunk, reverse, hk * r.outs + sub, 0);
+    ot.set<T>(r.out, sp, sp.seg * kChunk, reverse, hk * r.outs + sub, c0);
+    kt.set<T>(r.k, sp, 0, reverse, hk * sums, 0);
+    vt.set<T>(r.v, sp, 0, reverse, hk * sums, c0);
+    const uint32_t kmore = (uint32_t)kwidth * (uint32_t)sizeof(T), vmore = (uint32_t)vwidth * (uint32_t)sizeof(T);
+    const uint32_t qat = qt.row(query) + 8 * g * (uint32_t)sizeof(T), oat = ot.row(query) + (half + 16 * g) * (uint32_t)sizeof(T);
+    Rows<P> rows;
+    rows.places(kt, kwidth, vt, vwidth - c0);
+    Queries<P> q;
+    q.load(qt.at(), qat, query < mine, kwidth);
+    rows.load(kt.at(), vt.at(), sp.seg > 0 ? kChunk : mine);
+    stage_weights(behind, rate, kChunk, 0, 1.0f);
+    const float from_first = r.inside * decay_pow(rate, i);
+    f4 inside;
+    each<4>([&](auto e) { inside[(int)e] = i >= 4 * g + e ? r.inside * decay_pow(rate, i - 4 * g - e) : 0.0f; });
+    f4 o[4];
+    each<4>([&](auto t) { o[t] = zeros(); });
+    Vec<E, 8> qterms[DK / 32][P::RAW];
+    q.terms(qterms);
+    for (int c = 0; c <= sp.seg; ++c) {
+        for (int h = 0; h < sums; ++h) {
+            if (c + h > 0) __syncthreads();
+            rows.stage(kl, vl);
+            if (h + 1 < sums) {
+                rows.load(kt.at((uint64_t)(h + 1) * kmore), vt.at((uint64_t)(h + 1) * vmore), c < sp.seg ? kChunk : mine);
+            } else if (c < sp.seg) {
+                kt.base += (uint64_t)kt.next, vt.base += (uint64_t)vt.next;
+                rows.load(kt.at(), vt.at(), c + 1 < sp.seg ? kChunk : mine);
+            }
+            __syncthreads();
+            if (c < sp.seg) add_values<P, true>(o, qterms, kl, vl, w, half, inside, r.inside * decay_pow(rate, query + kChunk * (sp.seg - c - 1)), behind, [] {});
+            else add_values<P, false>(o, qterms, kl, vl, w, half, inside, from_first, behind, [] {});
+        }
+    }
+    const __amdgpu_buffer_rsrc_t to = ot.at();
+    each<2>([&](auto p) {
+        float x[8];
+        each<8>([&](auto e) { x[e] = o[2 * p + e / 4][e % 4]; });
+        store_eight<T>(to, query < mine && c0 + half + 16 * g + 8 * p < vwidth ? oat + 8 * p * (uint32_t)sizeof(T) : kNowhere, x);
+    });
 }
 
 // What each segment adds to the state, from a state of zeros.
@@ -568,12 +657,16 @@ __global__ __launch_bounds__(kScanThreads) void decay_scan_kernel(const Args a) 
     float *p = a.place(r.sums_out, sp.unit, hk) + at;
     const long next = (long)a.Hk * a.state;
     const float whole = decay_pow(rate, a.seq.seg);
-    for (int s = 0; s < segs; ++s, p += next) {
-        const bool end = s + 1 == segs;
-        f4 add = f4{0.0f, 0.0f, 0.0f, 0.0f};
-        if (!end || r.last != nullptr) add = *reinterpret_cast<const f4 *>(p);
-        *reinterpret_cast<f4 *>(p) = x;
-        x = x * (end ? decay_pow(rate, sp.length - s * a.seq.seg) : whole) + add;
+    const int sums = r.last != nullptr ? segs : segs - 1;    // (of the last segment only where the state behind it is asked for)
+    constexpr int kAhead = 8;
+    for (int s = 0; s < segs; s += kAhead) {
+        f4 add[kAhead];
+        each<kAhead>([&](auto k) { add[k] = s + k < sums ? *reinterpret_cast<const f4 *>(p + (s + k) * next) : f4{0.0f, 0.0f, 0.0f, 0.0f}; });
+        each<kAhead>([&](auto k) {
+            if (s + k >= segs) return;
+            *reinterpret_cast<f4 *>(p + (s + k) * next) = x;
+            x = x * (s + k + 1 == segs ? decay_pow(rate, sp.length - (s + k) * a.seq.seg) : whole) + add[k];
+        });
     }
     if (r.last != nullptr && place >= 0) *reinterpret_cast<f4 *>(a.place(r.last, place, hk) + at) = x;
 }
@@ -583,36 +676,37 @@ __global__ __launch_bounds__(kScanThreads) void decay_scan_kernel(const Args a) 
 struct Plan {
     int seg = 0;             // 0: one pass
     int per_sequence = 1;
+    bool shorts = false;     // decay_short_kernel, segments of 64 queries
 };
 
-// Segments where sequences and heads alone leave CUs without work, or where one long sequence among short ones would go on alone.
-// `shared_states`: heads that share a state would each make the one behind the sequence, and one might write it before another has read the
-// one before: then the states are made apart from the rows.
-Plan make_plan(long T, int B, int Hk, long outs, bool ragged, bool shared_states) {
+// Segments where sequences and states alone leave CUs without work, or where one long sequence among short ones would go on alone.
+Plan make_plan(long T, int B, int Hk, bool ragged, bool states) {
     Plan p;
     if (T == 0 || B == 0) return p;
-    const long mean = (T + B - 1) / B, groups = (long)B * Hk * outs;
-    constexpr long kWanted = 1024, kLeast = 256, kRagged = 2048;
+    const long mean = (T + B - 1) / B, groups = (long)B * Hk, longest = ragged ? T : T / B;
+    constexpr long kWanted = 512, kLeast = 256, kRagged = 2048, kShort = 512;
     long seg = 0;
-    if (groups < kWanted && mean > kLeast) {
+    if (!states && longest <= kShort && groups < kWanted) {
+        p.shorts = true;
+        seg = kChunk;
+    } else if (groups < kWanted && mean > kLeast) {
         const long parts = (kWanted + groups - 1) / groups;
-        seg = ((mean + parts - 1) / parts + kChunk - 1) / kChunk * kChunk;
+        seg = (mean + parts - 1) / parts;
         if (seg < kLeast) seg = kLeast;
     }
     if (ragged && T > kRagged && (seg == 0 || seg > kRagged)) seg = kRagged;
-    if (seg == 0 && shared_states) seg = T;
-    if (!ragged && !shared_states && seg >= T / B) seg = 0;
+    if (!ragged && !p.shorts && seg >= T / B) seg = 0;
     if (seg > 0) {
         if (ragged) {
             long power = kChunk;
-            while (power < seg && power < (1L << 30)) power *= 2;
+            while (power < seg) power *= 2;
             seg = power;
         } else {
             seg = (seg + kChunk - 1) / kChunk * kChunk;
             p.per_sequence = (int)((T / B + seg - 1) / seg);
         }
     }
-    p.seg = (int)(seg < (1L << 30) ? seg : 1L << 30);
+    p.seg = (int)seg;
     return p;
 }
 
@@ -624,21 +718,22 @@ Sequences sequences(const int32_t *offsets, long T, int B, const Plan &p) {
 }
 
 size_t plan_bytes(const Plan &p, long T, int B, bool ragged, int Hk, int d, int dv) {
-    if (p.seg == 0) return 0;
+    if (p.seg == 0 || p.shorts) return 0;
     const long units = ragged ? T / p.seg + B : (long)p.per_sequence * B;
     return (size_t)units * Hk * d * dv * sizeof(float);
 }
 
 // The kernel of a role: by the widths of its keys and of its result.  128 columns are eight wavefronts of one workgroup, which read the keys
-// once, where the state's terms of both halves have room in LDS (of fp32 with keys of more than 64 they have not: two workgroups).
+// once, where two workgroups of four would not have room in a CU together (keys of 65 to 128 in 16 bits, of 33 to 64 in fp32); of fp32 with more than 64
+// not even eight wavefronts' state has.
 struct Form {
     int keys, halves;
     bool operator==(const Form &o) const { return keys == o.keys && halves == o.halves; }
 };
 Form form_of(const Role &r, int type) {
     Form f;
-    f.keys = r.k.width <= 32 ? 32 : r.k.width <= 64 ? 64 : 128;
-    f.halves = r.v.width > kHalf && !(type == SA_F32 && f.keys > 64) ? 2 : 1;
+    f.keys = r.k.width <= 32 ? 32 : r.k.width <= 64 ? 64 : r.k.width <= 96 ? 96 : 128;
+    f.halves = r.v.width > kHalf && f.keys == (type == SA_F32 ? 64 : 128) ? 2 : 1;
     return f;
 }
 int slices_of(const Role &r, const Form &f) { return r.v.width > kHalf * f.halves ? 2 : 1; }
@@ -647,20 +742,17 @@ template <class F>
 int by_form(int type, const Form &f, F run) {
     return by_type(type, [&](auto t) {
         typedef decltype(t) T;
-        if (f.halves == 2) {
-            if (f.keys == 32) return run(Shape<T, 32, 2>());
-            if (f.keys == 64) return run(Shape<T, 64, 2>());
-            if constexpr (sizeof(T) == 2) return run(Shape<T, 128, 2>());
-        }
+        if (f.halves == 2) return run(Shape<T, sizeof(T) == 4 ? 64 : 128, 2>());
         if (f.keys == 32) return run(Shape<T, 32, 1>());
         if (f.keys == 64) return run(Shape<T, 64, 1>());
+        if (f.keys == 96) return run(Shape<T, 96, 1>());
         return run(Shape<T, 128, 1>());
     });
 }
 
 // Roles of one form are one launch.
 template <class F>
-int by_forms(const char *what, int type, const Args &a, int roles, bool rows, F run) {
+int by_forms(const char *what, int type, const Args &a, int roles, bool shorts, F run) {
     bool done[3] = {false, false, false};
     for (int r = 0; r < roles; ++r) {
         if (done[r]) continue;
@@ -671,7 +763,7 @@ int by_forms(const char *what, int type, const Args &a, int roles, bool rows, F 
         for (int s = r; s < roles; ++s) {
             if (done[s] || !(form_of(a.role[s], type) == f)) continue;
             done[s] = true;
-            total += a.seq.units() * a.Hk * (rows ? a.role[s].outs : 1) * slices_of(a.role[s], f);
+            total += a.seq.units() * a.Hk * (shorts ? a.role[s].outs : 1) * slices_of(a.role[s], f);
             some.role[some.roles] = a.role[s];
             some.items[some.roles++] = (uint32_t)total;
         }
@@ -687,6 +779,11 @@ int by_forms(const char *what, int type, const Args &a, int roles, bool rows, F 
 // The rows of all roles; before them, where there are segments, the sums of the first `states` roles and their scan.
 int launch(const char *what, int type, Args a, const Plan &p, int states, hipStream_t st) {
     if (a.seq.units() == 0) return SA_OK;
+    if (p.shorts) {
+        return by_forms(what, type, a, a.roles, true, [&](auto shape, dim3 grid, const Args &some) {
+            decay_short_kernel<decltype(shape)><<<grid, dim3(decltype(shape)::THREADS), 0, st>>>(some);
+        });
+    }
     if (p.seg > 0) {
         SA_TRY(by_forms(what, type, a, states, false, [&](auto shape, dim3 grid, const Args &some) {
             decay_states_kernel<decltype(shape)><<<grid, dim3(decltype(shape)::THREADS), 0, st>>>(some);
@@ -696,7 +793,7 @@ int launch(const char *what, int type, Args a, const Plan &p, int states, hipStr
         SA_TRY(check_launch(what));
         for (int r = 0; r < a.roles; ++r) a.role[r].first = nullptr, a.role[r].last = nullptr;
     }
-    return by_forms(what, type, a, a.roles, true, [&](auto shape, dim3 grid, const Args &some) {
+    return by_forms(what, type, a, a.roles, false, [&](auto shape, dim3 grid, const Args &some) {
         decay_rows_kernel<decltype(shape)><<<grid, dim3(decltype(shape)::THREADS), 0, st>>>(some);
     });
 }
@@ -714,10 +811,7 @@ int check_sequences(const char *what, int type, long T, int B, bool ragged, int 
 
 extern "C" size_t sa_decay_attention_workspace_bytes(long T, int B, int H, int Hk, int d, int dv, int ragged) {
     if (check_sequences("", SA_F32, T, B, ragged != 0, H, Hk, d, dv) != SA_OK) return 0;
-    const long outs = H / Hk;
-    const size_t a = plan_bytes(make_plan(T, B, Hk, outs, ragged != 0, false), T, B, ragged != 0, Hk, d, dv);
-    const size_t b = plan_bytes(make_plan(T, B, Hk, outs, ragged != 0, H != Hk), T, B, ragged != 0, Hk, d, dv);
-    return a > b ? a : b;
+    return plan_bytes(make_plan(T, B, Hk, ragged != 0, true), T, B, ragged != 0, Hk, d, dv);
 }
 
 extern "C" int sa_decay_attention(const void *q, long q_stride, const void *k, long k_stride, const void *v, long v_stride, int type,
@@ -741,7 +835,7 @@ extern "C" int sa_decay_attention(const void *q, long q_stride, const void *k, l
                    sa::aligned4(offsets_or_null) && sa::aligned4(slots_or_null),
                SA_ERR_ALIGN, "%s: pointers must be 16-byte aligned", what);
     if (B == 0 || (T == 0 && state_out_or_null == nullptr)) return SA_OK;
-    const Plan p = make_plan(T, B, Hk, (long)(H / Hk), ragged, H != Hk && state_out_or_null != nullptr);
+    const Plan p = make_plan(T, B, Hk, ragged, state_in_or_null != nullptr || state_out_or_null != nullptr);
     const size_t need = plan_bytes(p, T, B, ragged, Hk, d, dv);
     SA_REQUIRE(need == 0 || (workspace != nullptr && workspace_bytes >= need), SA_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", what,
                need, workspace_bytes);
@@ -754,13 +848,13 @@ extern "C" int sa_decay_attention(const void *q, long q_stride, const void *k, l
     r.outs = H / Hk, r.sums = 1, r.shift = 1;
     r.inside = scale, r.into = scale, r.update = 1.0f;
     r.first = state_in_or_null, r.last = state_out_or_null;
-    if (p.seg > 0) r.starts = r.sums_out = static_cast<float *>(workspace);
+    if (p.seg > 0 && !p.shorts) r.starts = r.sums_out = static_cast<float *>(workspace);
     return launch(what, type, a, p, 1, sa::as_stream(stream));
 }
 
 extern "C" size_t sa_decay_attention_backward_workspace_bytes(long T, int B, int H, int Hk, int d, int dv, int ragged) {
     if (check_sequences("", SA_F32, T, B, ragged != 0, H, Hk, d, dv) != SA_OK) return 0;
-    return 2 * plan_bytes(make_plan(T, B, Hk, (long)(H / Hk + 2), ragged != 0, false), T, B, ragged != 0, Hk, d, dv);
+    return 2 * plan_bytes(make_plan(T, B, 2 * Hk, ragged != 0, true), T, B, ragged != 0, Hk, d, dv);
 }
 
 extern "C" int sa_decay_attention_backward(const void *dout, long dout_stride, const void *q, long q_stride, const void *k, long k_stride,
@@ -793,7 +887,7 @@ extern "C" int sa_decay_attention_backward(const void *dout, long dout_stride, c
                    sa::aligned16(workspace) && sa::aligned4(offsets_or_null),
                SA_ERR_ALIGN, "%s: pointers must be 16-byte aligned", what);
     if (B == 0 || (T == 0 && dstate_in_or_null == nullptr)) return SA_OK;
-    const Plan p = make_plan(T, B, Hk, (long)(H / Hk + 2), ragged, false);
+    const Plan p = make_plan(T, B, 2 * Hk, ragged, state_in_or_null != nullptr || dstate_out_or_null != nullptr || dstate_in_or_null != nullptr);
     const size_t each = plan_bytes(p, T, B, ragged, Hk, d, dv);
     SA_REQUIRE(each == 0 || (workspace != nullptr && workspace_bytes >= 2 * each), SA_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given",
                what, 2 * each, workspace_bytes);
@@ -815,7 +909,7 @@ extern "C" int sa_decay_attention_backward(const void *dout, long dout_stride, c
     gq.inside = gq.into = scale, gq.update = 1.0f;
     gv.first = gk.first = dstate_out_or_null, gv.last = dstate_in_or_null;
     gq.first = state_in_or_null;
-    if (p.seg > 0) {
+    if (p.seg > 0 && !p.shorts) {
         float *ws = static_cast<float *>(workspace);
         gv.starts = gv.sums_out = ws;
         gk.starts = ws;
