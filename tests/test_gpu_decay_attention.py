@@ -1,0 +1,178 @@
+"""Linear attention with a decay for each head on the GPU: prompts against the definition in 64 bits, sequence by sequence."""
+import pytest
+import torch
+
+from decay_forms import check, reference, sequences
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+
+
+def run(sa, s, scale, state=True, **kw):
+    out = torch.full_like(s["dout"], 7.0)
+    o, last = sa.sa_decay_attention(s["q"], s["k"], s["v"], s["log_decay"], scale, offsets=s["offsets"], state_in=s["state_in"] if state else None,
+                                    want_state=state, out=out, **kw)
+    return o, last
+
+
+# one token, borders of a chunk and of a tile, several segments, nothing at all; widths of every kernel and odd ones
+LENGTHS = [[1], [16, 1, 17, 0, 15], [63, 64, 65], [127, 0, 129, 200], [700, 3, 90, 513]]
+HEADS = [(3, 3, 64, 64), (4, 2, 32, 24), (2, 1, 8, 128), (6, 2, 96, 72), (2, 2, 128, 128), (5, 5, 72, 40), (3, 1, 128, 8)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,Hk,d,dv", HEADS)
+@pytest.mark.parametrize("lengths", LENGTHS, ids=lambda l: "-".join(map(str, l)))
+@pytest.mark.parametrize("state", [False, True])
+def test_prompts_side_by_side(sa, lengths, H, Hk, d, dv, dtype, state):
+    s = sequences(lengths, H, Hk, d, dv, dtype, seed=sum(lengths) + H + d, device="cuda", offset=3, behind=2)
+    scale = d ** -0.5
+    o, last = run(sa, s, scale, state)
+    want = reference(s, scale, lengths, state=state)
+    check("out", o, want["out"], s, scale, dtype, lengths, state)
+    if state:
+        check("state_out", last, want["state_out"], s, scale, dtype, lengths)
+    assert bool((o[:3] == 7.0).all()) and bool((o[-2:] == 7.0).all())        # rows that no sequence has
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,N,H,Hk,d,dv", [
+    (2, 197, 3, 3, 64, 64), (70, 130, 8, 8, 64, 64), (1, 1500, 2, 2, 128, 72), (3, 1030, 4, 2, 40, 64), (2, 64, 2, 1, 96, 96), (600, 1, 1, 1, 8, 8),
+    (1, 2300, 1, 1, 64, 104)])
+@pytest.mark.parametrize("state", [False, True])
+def test_prompts_of_one_length(sa, B, N, H, Hk, d, dv, dtype, state):
+    """[B, N, heads, width], through short sequences, one pass and segments."""
+    s = sequences([N] * B, H, Hk, d, dv, dtype, seed=N, device="cuda")
+    scale = -0.75 * d ** -0.5
+    q, k, v = (s[n].view(B, N, *s[n].shape[1:]) for n in ("q", "k", "v"))
+    o, last = sa.sa_decay_attention(q, k, v, s["log_decay"], scale, state_in=s["state_in"] if state else None, want_state=state)
+    want = reference(s, scale, [N] * B, state=state)
+    check("out", o.view(B * N, H, dv), want["out"], s, scale, dtype, [N] * B, state)
+    if state:
+        check("state_out", last, want["state_out"], s, scale, dtype, [N] * B)
+    else:
+        assert last is None
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lengths", [[200, 1, 70], [3000, 5]])
+def test_decays_from_none_to_total(sa, lengths, dtype):
+    """Heads that forget nothing, almost nothing, nearly all at once, all but their own token."""
+    s = sequences(lengths, 6, 6, 32, 64, dtype, seed=5, device="cuda")
+    s["log_decay"] = torch.tensor([0.0, -1e-6, -0.02, -3.0, -90.0, -float("inf")], device="cuda")
+    # the definition needs no product of infinity and zero: a head without memory is one of exp(-800)
+    t = dict(s, log_decay=s["log_decay"].clamp(min=-800.0))
+    o, last = run(sa, s, 0.2)
+    want = reference(t, 0.2, lengths)
+    check("out", o, want["out"], t, 0.2, dtype, lengths)
+    check("state_out", last, want["state_out"], t, 0.2, dtype, lengths)
+    own = 0.2 * (s["q"][:, 5].double() * s["k"][:, 5].double()).sum(-1, keepdim=True) * s["v"][:, 5].double()
+    assert bool(((o[:, 5].double() - own).abs() <= 0.02 * own.abs() + 1e-5).all())
+
+
+@pytest.mark.parametrize("size", [2.0 ** -20, 2.0 ** -10, 1.0, 2.0 ** 8, 2.0 ** 14])
+def test_products_outside_of_fp16(sa, size):
+    """q k may be far outside of fp16 where out is not: v and scale bring it back."""
+    lengths = [150, 700]
+    s = sequences(lengths, 2, 2, 64, 64, torch.float16, seed=9, device="cuda")
+    s["q"], s["k"] = (s["q"] * size).clamp(-6e4, 6e4), (s["k"] * size).clamp(-6e4, 6e4)
+    s["state_in"] *= size
+    scale = float(min(1.0, size ** -2))
+    o, last = run(sa, s, scale)
+    want = reference(s, scale, lengths)
+    check("out", o, want["out"], s, scale, torch.float16, lengths)
+    check("state_out", last, want["state_out"], s, scale, torch.float16, lengths)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_columns_of_a_wider_matrix(sa, dtype):
+    """q, k and v as column blocks of a fused projection's rows, out as one of a wider matrix: the same bits."""
+    B, N, H, Hk, d, dv = 3, 300, 4, 2, 64, 72
+    s = sequences([N] * B, H, Hk, d, dv, dtype, seed=3, device="cuda")
+    parts = [H * d, Hk * d, Hk * dv]
+    fused = torch.cat([s[n].reshape(B * N, -1) for n in ("q", "k", "v")] + [torch.full((B * N, 8), float("nan"), dtype=dtype, device="cuda")], 1)
+    q, k, v = (x.view(B, N, h, w) for x, h, w in zip(fused.split(parts + [8], 1)[:3], (H, Hk, Hk), (d, d, dv)))
+    wide = torch.full((B * N, H * dv + 16), 5.0, dtype=dtype, device="cuda")
+    out = wide[:, 8:8 + H * dv].view(B, N, H, dv)
+    sa.sa_decay_attention(q, k, v, s["log_decay"], 0.1, out=out)
+    dense, _ = sa.sa_decay_attention(*(s[n].view(B, N, -1, s[n].shape[-1]) for n in ("q", "k", "v")), s["log_decay"], 0.1)
+    assert torch.equal(out, dense)
+    assert bool((wide[:, :8] == 5.0).all()) and bool((wide[:, -8:] == 5.0).all())
+
+
+def test_a_tensor_of_more_than_2_31_elements(sa):
+    """Tokens 2^16 bytes apart: the last ones begin behind 2^32 bytes."""
+    T, H, d = 70001, 1, 64
+    s = sequences([T], H, H, d, d, torch.bfloat16, seed=2, device="cuda")
+    wide = torch.empty(T, 32768, dtype=torch.bfloat16, device="cuda")
+    views = [wide[:, 64 * i:64 * i + 64].view(1, T, H, d) for i in (0, 200, 511)]
+    for view, n in zip(views, ("q", "k", "v")):
+        view.copy_(s[n].view(1, T, H, d))
+    out = wide[:, 6400:6464].view(1, T, H, d)
+    o, last = sa.sa_decay_attention(*views, s["log_decay"], 0.1, want_state=True, out=out)
+    dense, same = sa.sa_decay_attention(*(s[n].view(1, T, H, d) for n in ("q", "k", "v")), s["log_decay"], 0.1, want_state=True)
+    assert torch.equal(o, dense) and torch.equal(last, same)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,Hk", [(2, 2), (6, 2)])
+def test_slots_of_a_cache(sa, H, Hk, dtype):
+    """States in place in a cache; slots that are none begin with zeros and leave nothing; all other slots stay as they are."""
+    lengths, d, dv = [70, 1, 0, 900, 64, 5], 64, 96
+    s = sequences(lengths, H, Hk, d, dv, dtype, seed=8, device="cuda")
+    slots = torch.tensor([7, 2, 4, 0, -1, 9], dtype=torch.int32, device="cuda")          # of 9: -1 and 9 are none
+    cache = torch.randn(9, Hk, d, dv, device="cuda")
+    before = cache.clone()
+    s["state_in"] = torch.stack([before[p] if 0 <= p < 9 else torch.zeros_like(before[0]) for p in slots.tolist()])
+    o, last = sa.sa_decay_attention(s["q"], s["k"], s["v"], s["log_decay"], 0.1, offsets=s["offsets"], state_in=cache, state_out=cache, slots=slots)
+    assert last is cache
+    want = reference(s, 0.1, lengths)
+    check("out", o, want["out"], s, 0.1, dtype, lengths)
+    kept = [b for b, p in enumerate(slots.tolist()) if 0 <= p < 9]
+    left = torch.stack([cache[p] if b in kept else want["state_out"][b].float() for b, p in enumerate(slots.tolist())])
+    check("state_out", left, want["state_out"], s, 0.1, dtype, lengths)
+    others = [p for p in range(9) if p not in slots.tolist()]
+    assert torch.equal(cache[others], before[others])
+    assert torch.equal(cache[4], before[4])                  # the empty sequence's
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N", [130, 1400])
+def test_what_is_not_finite_stays_behind_its_chunk(sa, N, dtype):
+    """A NaN or infinity reaches rows of its own sequence from 63 tokens before it on, and no others."""
+    s = sequences([N, N], 2, 2, 64, 64, dtype, seed=4, device="cuda")
+    clean, _ = run(sa, s, 0.1)
+    at = N - 20
+    for name, value in (("q", float("nan")), ("k", float("inf")), ("v", float("nan"))):
+        bad = dict(s, **{name: s[name].clone()})
+        bad[name][at, 0, 5] = value
+        o, last = run(sa, bad, 0.1)
+        assert torch.equal(o[:at - 63], clean[:at - 63]) and torch.equal(o[N:], clean[N:]) and torch.equal(o[:, 1], clean[:, 1])
+        assert not o[at, 0].isfinite().all()
+        assert last[1].isfinite().all() and last[0, 1].isfinite().all()
+
+
+def test_offsets_that_are_none(sa):
+    """Offsets outside of the tokens, or descending, read and write nothing outside."""
+    s = sequences([100, 100], 2, 2, 64, 64, torch.float32, seed=1, device="cuda")
+    for off in ([-50, 90, 1000], [150, 20, 120], [2 ** 31 - 1, -2 ** 31, 7]):
+        s["offsets"] = torch.tensor(off, dtype=torch.int32, device="cuda")
+        guard = torch.full((400, 2, 64), 3.0, device="cuda")
+        sa.sa_decay_attention(s["q"], s["k"], s["v"], s["log_decay"], 0.1, offsets=s["offsets"], state_in=s["state_in"], want_state=True, out=guard[100:300])
+        assert bool((guard[:100] == 3.0).all()) and bool((guard[300:] == 3.0).all())
+
+
+def test_no_tokens(sa):
+    e = torch.empty(0, 2, 64, device="cuda")
+    g = torch.zeros(2, device="cuda")
+    state = torch.randn(3, 2, 64, 64, device="cuda")
+    off = torch.zeros(4, dtype=torch.int32, device="cuda")
+    o, last = sa.sa_decay_attention(e, e, e, g, 1.0, offsets=off, state_in=state, want_state=True)
+    assert o.shape == (0, 2, 64) and torch.equal(last, state)
+    _, last = sa.sa_decay_attention(e, e, e, g, 1.0, offsets=off, want_state=True)
+    assert bool((last == 0).all())
+    none = torch.zeros(1, dtype=torch.int32, device="cuda")
+    assert sa.sa_decay_attention(e, e, e, g, 1.0, offsets=none)[0].shape == (0, 2, 64)
+    four = torch.empty(2, 0, 2, 64, device="cuda")
+    o, last = sa.sa_decay_attention(four, four, four, g, 1.0, state_in=state[:2].clone(), want_state=True)
+    assert o.shape == four.shape and torch.equal(last, state[:2])
