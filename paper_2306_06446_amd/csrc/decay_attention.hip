@@ -33,8 +33,9 @@ struct Role {
 
 struct Args {
     Role role[3];
-    uint32_t items[3];       // of the roles before and with this one
+    uint32_t shares[3];      // of a segment and key/value head: workgroups of the roles up to this one
     int roles;
+    uint32_t total;          // workgroups
     Sequences seq;
     const float *g;
     int Hk, dv;              // (dv: columns of a state in memory)
@@ -211,6 +212,8 @@ struct State {
     }
     // S = carry S + sum_j weight[j] k_j v_j^T over the chunk in LDS.  Both operands have tokens for the places of the sum: transposed
     // reads, in the order 32 s + 16 (e / 4) + 4 (l / 16) + e % 4 for element e.
+    // TERMS: of what is added to the state.
+    template <int TERMS>
     __device__ inline void update(const E (*kl)[kChunk][P::KP], const E (*vl)[kChunk][P::VP], const float *weight, float carry) {
         const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15, w = (int)threadIdx.x >> 6, row = 4 * g + (i >> 2), col = 4 * (i & 3);
         auto decayed = [&](auto ks, float (&x)[8]) {
@@ -235,7 +238,7 @@ struct State {
             decayed(std::integral_constant<int, 0>(), x0);
             decayed(std::integral_constant<int, 1>(), x1);
             const Scale scale(column_max(largest(x1, largest(x0))));
-            Vec<E, 8> b[2][P::ADDED];
+            Vec<E, 8> b[2][TERMS];
             split(x0, b[0], scale.up);
             split(x1, b[1], scale.up);
             each<P::TILES>([&](auto t) {
@@ -252,7 +255,7 @@ struct State {
             each<2>([&](auto ks) {
                 float x[8];
                 decayed(ks, x);
-                Vec<E, 8> b[P::ADDED];
+                Vec<E, 8> b[TERMS];
                 split(x, b);
                 each<P::TILES>([&](auto t) {
                     Vec<E, 8> a[P::RAW];
@@ -277,10 +280,14 @@ __device__ inline int state_place(const Args &a, int seq) {
     return p >= 0 && p < a.places ? p : -1;
 }
 
-__device__ inline const Role &role_of(const Args &a, uint32_t &item) {
+// A workgroup's role and its place in it.  All workgroups of one segment and head follow each other, on one XCD: a gradient's three roles read the same rows.
+__device__ inline const Role &role_of(const Args &a, uint32_t &item, uint32_t &rest) {
+    const uint32_t per = a.shares[a.roles - 1];
+    rest = per == 1 ? item : item / per;
+    item -= rest * per;
     int r = 0;
-    while (r + 1 < a.roles && item >= a.items[r]) ++r;
-    if (r > 0) item -= a.items[r - 1];
+    while (r + 1 < a.roles && item >= a.shares[r]) ++r;
+    if (r > 0) item -= a.shares[r - 1];
     return a.role[r];
 }
 
@@ -329,7 +336,6 @@ __device__ inline void add_values(f4 (&o)[4], const Vec<typename P::E, 8> (&q)[P
         }
     });
     keys_done();
-    __builtin_amdgcn_sched_barrier(0);
     float up = 1.0f, back = 1.0f;
     if constexpr (P::SCALED) {
         const Scale scale(column_max(largest(x[1], largest(x[0]))));
@@ -357,7 +363,6 @@ __device__ inline void add_values(f4 (&o)[4], const Vec<typename P::E, 8> (&q)[P
     };
     if (EARLIER || w >= 2) values(std::integral_constant<int, 2>());
     else values(std::integral_constant<int, 1>());
-    __builtin_amdgcn_sched_barrier(0);
 }
 
 // Wavefronts on a SIMD: as many workgroups as have room for their rows in a CU's LDS, unless registers would go to scratch memory, whose loads wait for
@@ -383,18 +388,16 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
     __shared__ __attribute__((aligned(16))) E sl[P::MADE][P::COLS][P::KP];
     __shared__ __attribute__((aligned(16))) float down[P::SCALED ? P::COLS : 4];
     __shared__ __attribute__((aligned(16))) float weight[kChunk], behind[kChunk];      // exp(g (64 - j)) in the latter
-    const uint32_t total = a.items[a.roles - 1];
-    uint32_t item = xcd_place(total);
-    if (item >= total) return;
-    const Role &r = role_of(a, item);
+    uint32_t item = xcd_place(a.total), rest;
+    if (item >= a.total) return;
+    const Role &r = role_of(a, item, rest);
     const int kwidth = r.k.width, vwidth = r.v.width, sums = r.sums, outs = r.outs, shift = r.shift;
     const float update = r.update;
     const bool transposed = r.transposed, reverse = r.reverse;
-    const uint32_t slices = vwidth > P::COLS ? 2 : 1;
-    const int c0 = (int)(item % slices) * P::COLS;
-    item /= slices;
-    const int hk = (int)(item % (uint32_t)a.Hk);
-    const Span sp = a.seq.of_unit(item / (uint32_t)a.Hk);
+    const int c0 = (int)item * P::COLS;
+    const uint32_t unit = rest / (uint32_t)a.Hk;
+    const int hk = (int)(rest - unit * (uint32_t)a.Hk);
+    const Span sp = a.seq.of_unit(unit);
     const int p0 = sp.seg * a.seq.seg, left = sp.length - p0;
     if (sp.seg < 0 || (left <= 0 && (sp.seg > 0 || r.last == nullptr))) return;
     const int tokens = left < a.seq.seg ? left : a.seq.seg;
@@ -491,7 +494,6 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
                             }
                         });
                     }
-                    __builtin_amdgcn_sched_barrier(0);
                 }
                 add_values<P, false>(o, qterms, kl, vl, w, half, inside, from_first, behind, [&] { if (!early_queries<P>()) next_q(); });
                 if (h + 1 == sums) {
@@ -503,7 +505,11 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
                     });
                 }
             }
-            if (add) state.update(kl, vl, weight, h == 0 ? carry : 1.0f);
+            // (a state that only rows in 16 bits are made of takes the terms that these do)
+            if (add) {
+                if (P::MADE == P::ADDED || last != nullptr) state.template update<P::ADDED>(kl, vl, weight, h == 0 ? carry : 1.0f);
+                else state.template update<P::MADE>(kl, vl, weight, h == 0 ? carry : 1.0f);
+            }
         }
         ot.base += (uint64_t)ot.next;
         live = live || add;
@@ -521,19 +527,16 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_short_ker
     __shared__ __attribute__((aligned(16))) E kl[P::RAW][kChunk][P::KP];
     __shared__ __attribute__((aligned(16))) E vl[P::RAW][kChunk][P::VP];
     __shared__ __attribute__((aligned(16))) float behind[kChunk];
-    const uint32_t total = a.items[a.roles - 1];
-    uint32_t item = xcd_place(total);
-    if (item >= total) return;
-    const Role &r = role_of(a, item);
+    uint32_t item = xcd_place(a.total), rest;
+    if (item >= a.total) return;
+    const Role &r = role_of(a, item, rest);
     const int kwidth = r.k.width, vwidth = r.v.width, sums = r.sums;
     const bool reverse = r.reverse;
     const uint32_t slices = vwidth > P::COLS ? 2 : 1;
-    const int c0 = (int)(item % slices) * P::COLS;
-    item /= slices;
-    const int sub = (int)(item % (uint32_t)r.outs);
-    item /= (uint32_t)r.outs;
-    const int hk = (int)(item % (uint32_t)a.Hk);
-    const Span sp = a.seq.of_unit(item / (uint32_t)a.Hk);
+    const int sub = (int)(slices == 2 ? item >> 1 : item), c0 = (int)(slices == 2 ? item & 1 : 0) * P::COLS;
+    const uint32_t unit = rest / (uint32_t)a.Hk;
+    const int hk = (int)(rest - unit * (uint32_t)a.Hk);
+    const Span sp = a.seq.of_unit(unit);
     const int left = sp.length - sp.seg * kChunk;
     if (sp.seg < 0 || left <= 0) return;
     const int mine = left < kChunk ? left : kChunk;
@@ -591,18 +594,16 @@ __global__ __launch_bounds__(P::THREADS) void decay_states_kernel(const Args a) 
     typedef typename P::E E;
     __shared__ __attribute__((aligned(16))) E kl[P::RAW][kChunk][P::KP];
     __shared__ __attribute__((aligned(16))) E vl[P::RAW][kChunk][P::VP];
-    const uint32_t total = a.items[a.roles - 1];
-    uint32_t item = xcd_place(total);
-    if (item >= total) return;
-    const Role &r = role_of(a, item);
+    uint32_t item = xcd_place(a.total), rest;
+    if (item >= a.total) return;
+    const Role &r = role_of(a, item, rest);
     const int kwidth = r.k.width, vwidth = r.v.width, sums = r.sums, shift = r.shift;
     const float update = r.update;
     const bool reverse = r.reverse;
-    const uint32_t slices = vwidth > P::COLS ? 2 : 1;
-    const int c0 = (int)(item % slices) * P::COLS;
-    item /= slices;
-    const int hk = (int)(item % (uint32_t)a.Hk);
-    const Span sp = a.seq.of_unit(item / (uint32_t)a.Hk);
+    const int c0 = (int)item * P::COLS;
+    const uint32_t unit = rest / (uint32_t)a.Hk;
+    const int hk = (int)(rest - unit * (uint32_t)a.Hk);
+    const Span sp = a.seq.of_unit(unit);
     const int p0 = sp.seg * a.seq.seg, left = sp.length - p0;
     // the last segment's sum is for the state behind the sequence only
     if (sp.seg < 0 || left <= 0 || (left <= a.seq.seg && r.last == nullptr)) return;
@@ -635,7 +636,7 @@ __global__ __launch_bounds__(P::THREADS) void decay_states_kernel(const Args a) 
                 rows.load(kt.at(), vt.at(), in_chunk(c + 1));
             }
             __syncthreads();
-            state.update(kl, vl, weight, h == 0 ? carry : 1.0f);
+            state.template update<P::ADDED>(kl, vl, weight, h == 0 ? carry : 1.0f);
         }
     }
     state.store(a.place(r.sums_out, sp.unit, hk), r.transposed, kwidth, vwidth, a.dv, c0);
@@ -759,14 +760,16 @@ int by_forms(const char *what, int type, const Args &a, int roles, bool shorts, 
         const Form f = form_of(a.role[r], type);
         Args some = a;
         some.roles = 0;
-        long total = 0;
+        uint32_t shares = 0;
         for (int s = r; s < roles; ++s) {
             if (done[s] || !(form_of(a.role[s], type) == f)) continue;
             done[s] = true;
-            total += a.seq.units() * a.Hk * (shorts ? a.role[s].outs : 1) * slices_of(a.role[s], f);
+            shares += (uint32_t)((shorts ? a.role[s].outs : 1) * slices_of(a.role[s], f));
             some.role[some.roles] = a.role[s];
-            some.items[some.roles++] = (uint32_t)total;
+            some.shares[some.roles++] = shares;
         }
+        const long total = a.seq.units() * a.Hk * shares;
+        some.total = (uint32_t)total;
         SA_REQUIRE(total < (1L << 31) - 8, SA_ERR_UNSUPPORTED, "%s: too many heads and tokens for one launch", what);
         SA_TRY(by_form(type, f, [&](auto shape) {
             run(shape, dim3((unsigned)xcd_blocks(total)), some);
