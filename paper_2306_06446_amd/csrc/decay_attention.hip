@@ -7,7 +7,10 @@
 //   dq = (do, v, k) on S^T;  dv = (k, q, do) reversed, dk = (v, do, q) reversed, on R_t = l R_{t+1} + scale q_t do_t^T (dk: R^T)
 // R begins with the gradient of the last state, which meets the last token undecayed, so in reversed time a state is read as it is and decays on
 // its way on: l^i instead of l^(i + 1), l^(n - j) instead of l^(n - 1 - j) (`shift`).
+#include <algorithm>
+#include <initializer_list>
 #include <type_traits>
+#include <utility>
 
 #include "common.h"
 #include "decay_attention.h"
@@ -378,7 +381,7 @@ constexpr bool early_queries() { return P::RAW == 3 || P::DK == 128; }
 
 // Rows of the result.  A workgroup has one segment, the heads of one state and a slice of the columns and goes through the chunks one after the other;
 // of each half of the slice, wavefront w has queries 16 w to 16 w + 15 of a chunk, and columns 16 w to 16 w + 15 of the state.
-template <class P>
+template <class P, bool STREAM>
 __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kernel(const Args a) {
     typedef typename P::T T;
     typedef typename P::E E;
@@ -418,10 +421,8 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
     Rows<P> rows;
     rows.places(kt, kwidth, vt, vwidth - c0);
     Queries<P> q;
-    if (chunks > 0) {
-        q.load(qt.at(), qat, query < in_chunk(0), kwidth);
-        rows.load(kt.at(), vt.at(), in_chunk(0));
-    }
+    q.load(qt.at(), qat, query < in_chunk(0), kwidth);       // (of an empty sequence nothing)
+    rows.load(kt.at(), vt.at(), in_chunk(0));
 
     State<P> state;
     bool live = false;                   // a state that is not zero
@@ -501,7 +502,7 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
                     each<2>([&](auto p) {
                         float x[8];
                         each<8>([&](auto e) { x[e] = o[2 * p + e / 4][e % 4]; });
-                        store_eight<T>(to, query < n && c0 + half + 16 * g + 8 * p < vwidth ? oat + 8 * p * (uint32_t)sizeof(T) : kNowhere, x);
+                        store_eight<T, STREAM>(to, query < n && c0 + half + 16 * g + 8 * p < vwidth ? oat + 8 * p * (uint32_t)sizeof(T) : kNowhere, x);
                     });
                 }
             }
@@ -583,7 +584,7 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_short_ker
     each<2>([&](auto p) {
         float x[8];
         each<8>([&](auto e) { x[e] = o[2 * p + e / 4][e % 4]; });
-        store_eight<T>(to, query < mine && c0 + half + 16 * g + 8 * p < vwidth ? oat + 8 * p * (uint32_t)sizeof(T) : kNowhere, x);
+        store_eight<T, false>(to, query < mine && c0 + half + 16 * g + 8 * p < vwidth ? oat + 8 * p * (uint32_t)sizeof(T) : kNowhere, x);
     });
 }
 
@@ -636,7 +637,8 @@ __global__ __launch_bounds__(P::THREADS) void decay_states_kernel(const Args a) 
                 rows.load(kt.at(), vt.at(), in_chunk(c + 1));
             }
             __syncthreads();
-            state.template update<P::ADDED>(kl, vl, weight, h == 0 ? carry : 1.0f);
+            if (P::MADE == P::ADDED || r.last != nullptr) state.template update<P::ADDED>(kl, vl, weight, h == 0 ? carry : 1.0f);
+            else state.template update<P::MADE>(kl, vl, weight, h == 0 ? carry : 1.0f);
         }
     }
     state.store(a.place(r.sums_out, sp.unit, hk), r.transposed, kwidth, vwidth, a.dv, c0);
@@ -674,33 +676,67 @@ __global__ __launch_bounds__(kScanThreads) void decay_scan_kernel(const Args a) 
 
 // ------------------------------------------------------------------------------------------- plan --
 
+// The kernel of a role: by the widths of its keys and of its result.  128 columns are eight wavefronts of one workgroup, which read the keys
+// once, where two workgroups of four would not have room in a CU together (keys of 65 to 128 in 16 bits, of 33 to 64 in fp32); of fp32 with more than 64
+// not even eight wavefronts' state has.
+struct Form {
+    int keys, halves;
+    bool operator==(const Form &o) const { return keys == o.keys && halves == o.halves; }
+};
+Form form_of(int keys, int columns, int type) {
+    Form f;
+    f.keys = keys <= 32 ? 32 : keys <= 64 ? 64 : keys <= 96 ? 96 : 128;
+    f.halves = columns > kHalf && f.keys == (type == SA_F32 ? 64 : 128) ? 2 : 1;
+    return f;
+}
+Form form_of(const Role &r, int type) { return form_of(r.k.width, r.v.width, type); }
+int slices_of(int columns, const Form &f) { return columns > kHalf * f.halves ? 2 : 1; }
+// Workgroups of decay_rows_kernel that a CU has at once, by registers and LDS.
+int resident(const Form &f, int type) { return type == SA_F32 ? (f.keys == 32 ? 2 : 1) : f.keys <= 64 ? 3 : f.halves == 2 ? 1 : 2; }
+
 struct Plan {
     int seg = 0;             // 0: one pass
     int per_sequence = 1;
     bool shorts = false;     // decay_short_kernel, segments of 64 queries
 };
 
-// Segments where sequences and states alone leave CUs without work, or where one long sequence among short ones would go on alone.
-Plan make_plan(long T, int B, int Hk, bool ragged, bool states) {
+// What a call's rows take: workgroups of a segment and key/value head, and how many of them fill the GPU.
+struct Load {
+    int workgroups, fill;
+};
+Load load_of(int type, std::initializer_list<std::pair<int, int>> roles) {       // keys' and results' widths
+    Load l{0, 1 << 30};
+    for (const auto &r : roles) {
+        const Form f = form_of(r.first, r.second, type);
+        l.workgroups += slices_of(r.second, f);
+        l.fill = std::min(l.fill, 256 * resident(f, type));
+    }
+    return l;
+}
+
+// Segments where sequences and states alone leave CUs without work, as many as fill them once, or where one long sequence among short ones would go on
+// alone.
+Plan make_plan(long T, int B, int Hk, const Load &l, bool ragged, bool states) {
     Plan p;
     if (T == 0 || B == 0) return p;
-    const long mean = (T + B - 1) / B, groups = (long)B * Hk, longest = ragged ? T : T / B;
-    constexpr long kWanted = 512, kLeast = 256, kRagged = 2048, kShort = 512;
+    const long mean = (T + B - 1) / B, groups = (long)B * Hk * l.workgroups, longest = ragged ? T : T / B;
+    const long kLeast = ragged ? 256 : 128;
+    constexpr long kRagged = 4, kShort = 512;
     long seg = 0;
-    if (!states && longest <= kShort && groups < kWanted) {
+    if (!states && longest <= kShort && groups < l.fill) {
         p.shorts = true;
         seg = kChunk;
-    } else if (groups < kWanted && mean > kLeast) {
-        const long parts = (kWanted + groups - 1) / groups;
+    } else if ((2 * groups <= l.fill || ragged) && longest > kLeast) {
+        // (of a ragged batch four times as many: the GPU is busy as long as there are segments left, and its longest sequence may be many times the mean)
+        const long parts = std::max(1L, (ragged ? kRagged : 1) * l.fill / groups);
         seg = (mean + parts - 1) / parts;
         if (seg < kLeast) seg = kLeast;
     }
-    if (ragged && T > kRagged && (seg == 0 || seg > kRagged)) seg = kRagged;
     if (!ragged && !p.shorts && seg >= T / B) seg = 0;
     if (seg > 0) {
         if (ragged) {
             long power = kChunk;
-            while (power < seg) power *= 2;
+            while (2 * power <= seg) power *= 2;
             seg = power;
         } else {
             seg = (seg + kChunk - 1) / kChunk * kChunk;
@@ -723,21 +759,6 @@ size_t plan_bytes(const Plan &p, long T, int B, bool ragged, int Hk, int d, int 
     const long units = ragged ? T / p.seg + B : (long)p.per_sequence * B;
     return (size_t)units * Hk * d * dv * sizeof(float);
 }
-
-// The kernel of a role: by the widths of its keys and of its result.  128 columns are eight wavefronts of one workgroup, which read the keys
-// once, where two workgroups of four would not have room in a CU together (keys of 65 to 128 in 16 bits, of 33 to 64 in fp32); of fp32 with more than 64
-// not even eight wavefronts' state has.
-struct Form {
-    int keys, halves;
-    bool operator==(const Form &o) const { return keys == o.keys && halves == o.halves; }
-};
-Form form_of(const Role &r, int type) {
-    Form f;
-    f.keys = r.k.width <= 32 ? 32 : r.k.width <= 64 ? 64 : r.k.width <= 96 ? 96 : 128;
-    f.halves = r.v.width > kHalf && f.keys == (type == SA_F32 ? 64 : 128) ? 2 : 1;
-    return f;
-}
-int slices_of(const Role &r, const Form &f) { return r.v.width > kHalf * f.halves ? 2 : 1; }
 
 template <class F>
 int by_form(int type, const Form &f, F run) {
@@ -764,7 +785,7 @@ int by_forms(const char *what, int type, const Args &a, int roles, bool shorts, 
         for (int s = r; s < roles; ++s) {
             if (done[s] || !(form_of(a.role[s], type) == f)) continue;
             done[s] = true;
-            shares += (uint32_t)((shorts ? a.role[s].outs : 1) * slices_of(a.role[s], f));
+            shares += (uint32_t)((shorts ? a.role[s].outs : 1) * slices_of(a.role[s].v.width, f));
             some.role[some.roles] = a.role[s];
             some.shares[some.roles++] = shares;
         }
@@ -797,7 +818,11 @@ int launch(const char *what, int type, Args a, const Plan &p, int states, hipStr
         for (int r = 0; r < a.roles; ++r) a.role[r].first = nullptr, a.role[r].last = nullptr;
     }
     return by_forms(what, type, a, a.roles, false, [&](auto shape, dim3 grid, const Args &some) {
-        decay_rows_kernel<decltype(shape)><<<grid, dim3(decltype(shape)::THREADS), 0, st>>>(some);
+        typedef decltype(shape) S;
+        bool lines = true;
+        for (int r = 0; r < some.roles; ++r) lines = lines && some.role[r].out.width * sizeof(typename S::T) % 128 == 0;
+        if (lines) decay_rows_kernel<S, true><<<grid, dim3(S::THREADS), 0, st>>>(some);
+        else decay_rows_kernel<S, false><<<grid, dim3(S::THREADS), 0, st>>>(some);
     });
 }
 
@@ -814,7 +839,10 @@ int check_sequences(const char *what, int type, long T, int B, bool ragged, int 
 
 extern "C" size_t sa_decay_attention_workspace_bytes(long T, int B, int H, int Hk, int d, int dv, int ragged) {
     if (check_sequences("", SA_F32, T, B, ragged != 0, H, Hk, d, dv) != SA_OK) return 0;
-    return plan_bytes(make_plan(T, B, Hk, ragged != 0, true), T, B, ragged != 0, Hk, d, dv);
+    size_t most = 0;
+    for (const int type : {SA_F32, SA_F16, SA_BF16})
+        most = std::max(most, plan_bytes(make_plan(T, B, Hk, load_of(type, {{d, dv}}), ragged != 0, true), T, B, ragged != 0, Hk, d, dv));
+    return most;
 }
 
 extern "C" int sa_decay_attention(const void *q, long q_stride, const void *k, long k_stride, const void *v, long v_stride, int type,
@@ -838,7 +866,7 @@ extern "C" int sa_decay_attention(const void *q, long q_stride, const void *k, l
                    sa::aligned4(offsets_or_null) && sa::aligned4(slots_or_null),
                SA_ERR_ALIGN, "%s: pointers must be 16-byte aligned", what);
     if (B == 0 || (T == 0 && state_out_or_null == nullptr)) return SA_OK;
-    const Plan p = make_plan(T, B, Hk, ragged, state_in_or_null != nullptr || state_out_or_null != nullptr);
+    const Plan p = make_plan(T, B, Hk, load_of(type, {{d, dv}}), ragged, state_in_or_null != nullptr || state_out_or_null != nullptr);
     const size_t need = plan_bytes(p, T, B, ragged, Hk, d, dv);
     SA_REQUIRE(need == 0 || (workspace != nullptr && workspace_bytes >= need), SA_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", what,
                need, workspace_bytes);
@@ -857,7 +885,10 @@ extern "C" int sa_decay_attention(const void *q, long q_stride, const void *k, l
 
 extern "C" size_t sa_decay_attention_backward_workspace_bytes(long T, int B, int H, int Hk, int d, int dv, int ragged) {
     if (check_sequences("", SA_F32, T, B, ragged != 0, H, Hk, d, dv) != SA_OK) return 0;
-    return 2 * plan_bytes(make_plan(T, B, 2 * Hk, ragged != 0, true), T, B, ragged != 0, Hk, d, dv);
+    size_t most = 0;
+    for (const int type : {SA_F32, SA_F16, SA_BF16})
+        most = std::max(most, plan_bytes(make_plan(T, B, Hk, load_of(type, {{d, dv}, {dv, d}, {dv, d}}), ragged != 0, true), T, B, ragged != 0, Hk, d, dv));
+    return 2 * most;
 }
 
 extern "C" int sa_decay_attention_backward(const void *dout, long dout_stride, const void *q, long q_stride, const void *k, long k_stride,
@@ -890,7 +921,7 @@ extern "C" int sa_decay_attention_backward(const void *dout, long dout_stride, c
                    sa::aligned16(workspace) && sa::aligned4(offsets_or_null),
                SA_ERR_ALIGN, "%s: pointers must be 16-byte aligned", what);
     if (B == 0 || (T == 0 && dstate_in_or_null == nullptr)) return SA_OK;
-    const Plan p = make_plan(T, B, 2 * Hk, ragged, state_in_or_null != nullptr || dstate_out_or_null != nullptr || dstate_in_or_null != nullptr);
+    const Plan p = make_plan(T, B, Hk, load_of(type, {{d, dv}, {dv, d}, {dv, d}}), ragged, state_in_or_null != nullptr || dstate_out_or_null != nullptr || dstate_in_or_null != nullptr);
     const size_t each = plan_bytes(p, T, B, ragged, Hk, d, dv);
     SA_REQUIRE(each == 0 || (workspace != nullptr && workspace_bytes >= 2 * each), SA_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given",
                what, 2 * each, workspace_bytes);
