@@ -111,11 +111,11 @@ struct Rows {
     __device__ inline void load(__amdgpu_buffer_rsrc_t kp, __amdgpu_buffer_rsrc_t vp, int n) {
         each<KN>([&](auto j_) {
             constexpr int j = j_;
-            k[j].load(kp, krow(j) < n ? kat[j] : kNowhere);
+            k[j].load(kp, kat[j] | (krow(j) < n ? 0u : kNowhere));
         });
         each<VN>([&](auto j_) {
             constexpr int j = j_;
-            v[j].load(vp, vrow(j) < n ? vat[j] : kNowhere);
+            v[j].load(vp, vat[j] | (vrow(j) < n ? 0u : kNowhere));
         });
     }
     __device__ inline void stage(E (*kl)[kChunk][P::KP], E (*vl)[kChunk][P::VP]) const {
@@ -301,7 +301,7 @@ struct Queries {
     __device__ inline void load(__amdgpu_buffer_rsrc_t from, uint32_t at, bool there, int width) {
         const int g = ((int)threadIdx.x & 63) >> 4;
         each<P::DK / 32>([&](auto s) {
-            q[s].load(from, there && 32 * s + 8 * g < width ? at + 32 * s * (uint32_t)sizeof(typename P::T) : kNowhere);
+            q[s].load(from, (at + 32 * s * (uint32_t)sizeof(typename P::T)) | (there && 32 * s + 8 * g < width ? 0u : kNowhere));
         });
     }
     __device__ inline void terms(Vec<typename P::E, 8> (&t)[P::DK / 32][P::RAW]) const {
@@ -421,8 +421,6 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
     Rows<P> rows;
     rows.places(kt, kwidth, vt, vwidth - c0);
     Queries<P> q;
-    q.load(qt.at(), qat, query < in_chunk(0), kwidth);       // (of an empty sequence nothing)
-    rows.load(kt.at(), vt.at(), in_chunk(0));
 
     State<P> state;
     bool live = false;                   // a state that is not zero
@@ -435,6 +433,19 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
         state.clear();
     }
 
+    // Loads and stores come back in the order in which they left, and the compiler counts those behind the one it waits for, the fewest that may be there
+    // on any way to that place.  So every turn of the loop asks for as many rows and queries and stores as many, and what is
+    // not needed goes nowhere; and the loop is entered as it is entered again, keys and values before queries before stores.  (With branches around
+    // them each chunk waited for the rows of the next one and for the stores of the last.)
+    rows.load(kt.at(), vt.at(), in_chunk(0));                // (of an empty sequence nothing)
+    q.load(qt.at(), qat, query < in_chunk(0), kwidth);
+    auto store = [&](__amdgpu_buffer_rsrc_t to, bool there, const f4 (&o)[4]) {
+        each<2>([&](auto p) {
+            float x[8];
+            each<8>([&](auto e) { x[e] = o[2 * p + e / 4][e % 4]; });
+            store_eight<T, STREAM>(to, (oat + 8 * p * (uint32_t)sizeof(T)) | (there && c0 + half + 16 * g + 8 * p < vwidth ? 0u : kNowhere), x);
+        });
+    };
     stage_weights(weight, rate, kChunk < tokens ? kChunk : tokens, shift, update);
     stage_weights(behind, rate, kChunk, 0, 1.0f);
     const float from_first = r.inside * decay_pow(rate, i);
@@ -444,74 +455,63 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
     float carry = decay_pow(rate, kChunk);
 
     f4 o[4];
+    each<4>([&](auto t) { o[t] = zeros(); });
+    store(ot.at(), false, o);
     Vec<E, 8> qterms[DK / 32][P::RAW];
     // h: of several heads of keys and values that are added up; u: of several heads of queries.  One of the two has more than one.
     for (int c = 0; c < chunks; ++c) {
-        const int n = in_chunk(c);
-        const bool more = c + 1 < chunks, add = more || last != nullptr;
+        const int n = in_chunk(c), next = c + 1 < chunks ? in_chunk(c + 1) : 0;
+        const bool add = next > 0 || last != nullptr;
         if (n < kChunk) carry = decay_pow(rate, n);
-        for (int h = 0; h < sums; ++h) {
+        int h = 0;
+        do {
             if (c + h > 0) __syncthreads();
             rows.stage(kl, vl);
             if (h == 0) {
                 if (n < kChunk && c > 0) stage_weights(weight, rate, n, shift, update);
                 if (live) state.stage(sl, down);
+                q.terms(qterms);             // (ahead of the next rows, which they would be waited for with)
             }
-            if (h + 1 < sums) {
-                rows.load(kt.at((uint64_t)(h + 1) * kmore), vt.at((uint64_t)(h + 1) * vmore), n);
-            } else if (more) {
-                kt.base += (uint64_t)kt.next, vt.base += (uint64_t)vt.next;
-                rows.load(kt.at(), vt.at(), in_chunk(c + 1));
-            }
+            const bool end = h + 1 == sums;
+            kt.base += end ? (uint64_t)kt.next - (uint64_t)(sums - 1) * kmore : kmore;
+            vt.base += end ? (uint64_t)vt.next - (uint64_t)(sums - 1) * vmore : vmore;
+            rows.load(kt.at(), vt.at(), end ? next : n);
             __syncthreads();
-            for (int u = 0; u < outs; ++u) {
+            int u = 0;
+            do {
                 auto next_q = [&] {
-                    if (u + 1 < outs) {
-                        q.load(qt.at((uint64_t)(u + 1) * kmore), qat, query < n, kwidth);
-                    } else if (more && (h + 1 == sums || early_queries<P>())) {
-                        qt.base += (uint64_t)qt.next;
-                        q.load(qt.at(), qat, query < in_chunk(c + 1), kwidth);
-                    }
+                    const bool turn = u + 1 == outs;
+                    if (end) qt.base += turn ? (uint64_t)qt.next - (uint64_t)(outs - 1) * kmore : kmore;
+                    q.load(qt.at(), qat, query < (turn ? (end ? next : 0) : n), kwidth);
                 };
-                if (h == 0) {
-                    q.terms(qterms);
-                    if (early_queries<P>()) next_q();
-                    each<4>([&](auto t) { o[t] = zeros(); });
-                    if (live) {
-                        each<DK / 32>([&](auto s) {
-                            each<4>([&](auto t) {
-                                Vec<E, 8> st[P::MADE];
-                                each<P::MADE>([&](auto p) {
-                                    st[p] = *reinterpret_cast<const Vec<E, 8> *>(&sl[p][half + 16 * t + i][32 * s + 8 * g]);
-                                });
-                                product<Terms<T>::ORDER>(o[t], st, qterms[s]);
-                            });
-                        });
+                if (u > 0) q.terms(qterms);
+                if (h == 0) each<4>([&](auto t) { o[t] = zeros(); });
+                if (early_queries<P>()) next_q();
+                if (h == 0 && live) {
+                    each<DK / 32>([&](auto s) {
                         each<4>([&](auto t) {
-                            if constexpr (P::SCALED) {
-                                o[t] *= *reinterpret_cast<const f4 *>(&down[half + 16 * t + 4 * g]) * into;
-                            } else {
-                                o[t] *= into;
-                            }
+                            Vec<E, 8> st[P::MADE];
+                            each<P::MADE>([&](auto p) { st[p] = *reinterpret_cast<const Vec<E, 8> *>(&sl[p][half + 16 * t + i][32 * s + 8 * g]); });
+                            product<Terms<T>::ORDER>(o[t], st, qterms[s]);
                         });
-                    }
-                }
-                add_values<P, false>(o, qterms, kl, vl, w, half, inside, from_first, behind, [&] { if (!early_queries<P>()) next_q(); });
-                if (h + 1 == sums) {
-                    const __amdgpu_buffer_rsrc_t to = ot.at((uint64_t)u * vmore);
-                    each<2>([&](auto p) {
-                        float x[8];
-                        each<8>([&](auto e) { x[e] = o[2 * p + e / 4][e % 4]; });
-                        store_eight<T, STREAM>(to, query < n && c0 + half + 16 * g + 8 * p < vwidth ? oat + 8 * p * (uint32_t)sizeof(T) : kNowhere, x);
+                    });
+                    each<4>([&](auto t) {
+                        if constexpr (P::SCALED) {
+                            o[t] *= *reinterpret_cast<const f4 *>(&down[half + 16 * t + 4 * g]) * into;
+                        } else {
+                            o[t] *= into;
+                        }
                     });
                 }
-            }
+                add_values<P, false>(o, qterms, kl, vl, w, half, inside, from_first, behind, [&] { if (!early_queries<P>()) next_q(); });
+                store(ot.at((uint64_t)u * vmore), end && query < n, o);
+            } while (++u < outs);
             // (a state that only rows in 16 bits are made of takes the terms that these do)
             if (add) {
                 if (P::MADE == P::ADDED || last != nullptr) state.template update<P::ADDED>(kl, vl, weight, h == 0 ? carry : 1.0f);
                 else state.template update<P::MADE>(kl, vl, weight, h == 0 ? carry : 1.0f);
             }
-        }
+        } while (++h < sums);
         ot.base += (uint64_t)ot.next;
         live = live || add;
     }
