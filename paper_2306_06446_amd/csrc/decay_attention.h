@@ -111,15 +111,14 @@ __device__ inline Vec<E, 4> read_transposed(const E *p) {
 template <class E>
 __device__ inline Vec<E, 8> join(const Vec<E, 4> &a, const Vec<E, 4> &b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
-// Rows of one head, from memory: a base that all lanes share and a 32-bit offset each.  What lies beyond kReach (an offset made kNowhere)
-// reads as zeros and is not written, without a branch.
-constexpr uint32_t kReach = 0x7fffffffu, kNowhere = 0x80000000u;
-__device__ inline __amdgpu_buffer_rsrc_t buffer(const void *p) {
-    const uint64_t u = reinterpret_cast<uint64_t>(p);
+// Rows of one head, from memory: a base and a size in bytes that all lanes share and a 32-bit offset each.  What begins behind the size, as kNowhere
+// and up to 2^30 less do, reads as zeros and is not written, without a branch.
+constexpr uint32_t kNowhere = 0xc0000000u;
+__device__ inline __amdgpu_buffer_rsrc_t buffer(uint64_t p, uint32_t bytes) {
     // (the builtin's result is signed: a low half of 2^31 or more would set all of the high one)
-    const uint32_t high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32)), low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)u);
+    const uint32_t high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)), low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p);
     const uint64_t at = (uint64_t)high << 32 | low;
-    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(at), 0, (int)kReach, 0x00027000);
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(at), 0, __builtin_amdgcn_readfirstlane((int)bytes), 0x00027000);
 }
 
 // 8 elements on their way from memory to LDS.
@@ -228,6 +227,7 @@ struct Sequences {
 
 // exp(n g), n >= 0, as 2^(n g / ln 2): the exponent is rounded twice, relative to itself, so a result of 2^-20 is off by some 30 units and one near 1 by
 // one or two.  A head without memory (g = -infinity) has 1 for n = 0 and 0 for all others: so has one of -2000.
+__device__ inline float uniform(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
 __device__ inline float decay_rate(float g) { return (g < -2000.0f ? -2000.0f : g) * 1.44269504f; }
 __device__ inline float decay_pow(float rate, int n) { return __builtin_amdgcn_exp2f(rate * (float)n); }
 

@@ -72,7 +72,7 @@ struct Shape {
 struct Tokens {
     uint64_t base;           // of row 0 of the current chunk, or of row 63 where time is reversed
     int64_t next;            // bytes to the next chunk
-    uint32_t pitch;          // bytes from token to token
+    uint32_t pitch;          // bytes from token to token (of 64 tokens: 2^30 at most)
     bool reverse;
     template <class T>
     __device__ inline void set(const HeadRows &r, const Span &sp, int p0, bool reverse_, int head, int col) {
@@ -82,8 +82,10 @@ struct Tokens {
         base = reinterpret_cast<uint64_t>(r.p) + (uint64_t)(first * (long)pitch) + (uint64_t)(head * r.width + col) * sizeof(T);
         next = (reverse ? -(int64_t)kChunk : (int64_t)kChunk) * (int64_t)pitch;
     }
+    // The first n rows of the chunk: their memory alone is in the buffer, at row(i) - skipped(n) for row i.  All others' offsets are beyond it.
     __device__ inline uint32_t row(int i) const { return (uint32_t)(reverse ? kChunk - 1 - i : i) * pitch; }
-    __device__ inline __amdgpu_buffer_rsrc_t at(uint64_t more = 0) const { return buffer(reinterpret_cast<const void *>(base + more)); }
+    __device__ inline uint32_t skipped(int n) const { return reverse ? (uint32_t)(kChunk - n) * pitch : 0u; }
+    __device__ inline __amdgpu_buffer_rsrc_t rows(int n, uint64_t more = 0) const { return buffer(base + more + skipped(n), (uint32_t)n * pitch); }
 };
 
 // The keys and values of one chunk: from memory to registers, from there to LDS.
@@ -108,15 +110,10 @@ struct Rows {
             vat[j] = vcol(j) < vwidth ? vt.row(vrow(j)) + vcol(j) * (uint32_t)sizeof(T) : kNowhere;
         });
     }
-    __device__ inline void load(__amdgpu_buffer_rsrc_t kp, __amdgpu_buffer_rsrc_t vp, int n) {
-        each<KN>([&](auto j_) {
-            constexpr int j = j_;
-            k[j].load(kp, kat[j] | (krow(j) < n ? 0u : kNowhere));
-        });
-        each<VN>([&](auto j_) {
-            constexpr int j = j_;
-            v[j].load(vp, vat[j] | (vrow(j) < n ? 0u : kNowhere));
-        });
+    __device__ inline void load(const Tokens &kt, const Tokens &vt, int n) {
+        const __amdgpu_buffer_rsrc_t kp = kt.rows(n), vp = vt.rows(n);
+        each<KN>([&](auto j) { k[j].load(kp, kat[j] - kt.skipped(n)); });
+        each<VN>([&](auto j) { v[j].load(vp, vat[j] - vt.skipped(n)); });
     }
     __device__ inline void stage(E (*kl)[kChunk][P::KP], E (*vl)[kChunk][P::VP]) const {
         each<KN>([&](auto j_) {
@@ -294,90 +291,118 @@ __device__ inline const Role &role_of(const Args &a, uint32_t &item, uint32_t &r
     return a.role[r];
 }
 
-// The queries of a wavefront, for the product with the keys (and with the state).
+// The queries of a wavefront, as operands of the products with the keys and with the state.  Those in memory as one term are loaded into the operand's place.
 template <class P>
 struct Queries {
-    Eight<typename P::T> q[P::DK / 32];
-    __device__ inline void load(__amdgpu_buffer_rsrc_t from, uint32_t at, bool there, int width) {
+    typedef typename P::T T;
+    typedef typename P::E E;
+    Vec<E, 8> t[P::DK / 32][P::RAW];
+    Eight<T> raw[P::RAW > 1 ? P::DK / 32 : 1];
+    __device__ inline void load(const Tokens &qt, uint32_t at, int n, int width) {
+        const __amdgpu_buffer_rsrc_t from = qt.rows(n);
         const int g = ((int)threadIdx.x & 63) >> 4;
+        at -= qt.skipped(n);
         each<P::DK / 32>([&](auto s) {
-            q[s].load(from, (at + 32 * s * (uint32_t)sizeof(typename P::T)) | (there && 32 * s + 8 * g < width ? 0u : kNowhere));
+            const uint32_t place = 32 * s + 8 * g < width ? at + 32 * s * (uint32_t)sizeof(T) : kNowhere;
+            if constexpr (P::RAW > 1) {
+                raw[s].load(from, place);
+            } else {
+                Eight<T> x;
+                x.load(from, place);
+                t[s][0] = x.v;
+            }
         });
     }
-    __device__ inline void terms(Vec<typename P::E, 8> (&t)[P::DK / 32][P::RAW]) const {
-        each<P::DK / 32>([&](auto s) { q[s].terms(t[s]); });
+    // Has them there: what is asked for behind this is not waited for with them.
+    __device__ inline void arrived() {
+        each<P::DK / 32>([&](auto s) {
+            if constexpr (P::RAW > 1) {
+                raw[s].terms(t[s]);
+            } else {
+                u4 words = __builtin_bit_cast(u4, t[s][0]);
+                asm volatile("" : "+v"(words));
+                t[s][0] = __builtin_bit_cast(Vec<E, 8>, words);
+            }
+        });
     }
 };
 
-// o += sum_j exp(g (i - j)) (q_i k_j) v_j for the keys in LDS: those of the queries' own chunk, of which wavefront w has queries 16 w to 16 w + 15,
-// or all 64 of an earlier one (EARLIER).  (k_j q_i) comes out in the registers of the lanes that have it as the right operand of the
-// product with v.  Decays: `inside` within a tile of 16 x 16; of earlier tiles `from_first`, which counts from the tile's (the chunk's) first
+// o += sum_j exp(g (i - j)) (q_i k_j) v_j for the keys in LDS: those of the queries' own chunk, of which wavefront W has queries 16 W to 16 W + 15, or
+// all 64 of an earlier one (W = 4).  (k_j q_i) comes out in the registers of the lanes that have it as the right operand of the product
+// with v.  Decays: `inside` within a tile of 16 x 16; of earlier tiles `from_first`, which counts from the tile's (the chunk's) first
 // query, and `behind`, which counts to it from the keys of 64 places before.
-template <class P, bool EARLIER, class F>
+template <class P, int W, class F>
 __device__ inline void add_values(f4 (&o)[4], const Vec<typename P::E, 8> (&q)[P::DK / 32][P::RAW], const typename P::E (*kl)[kChunk][P::KP],
-                                  const typename P::E (*vl)[kChunk][P::VP], int w, int half, const f4 &inside, float from_first, const float *behind,
-                                  F keys_done) {
+                                  const typename P::E (*vl)[kChunk][P::VP], int half, const f4 &inside, float from_first, const float *behind, F keys_done) {
     typedef typename P::E E;
     typedef Terms<typename P::T> N;
+    constexpr int TILES = W < 4 ? W + 1 : 4, STEPS = (TILES + 1) / 2;        // of 16 keys; of 32
     const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15;
-    float x[2][8];
-    each<4>([&](auto tile) {
+    float x[STEPS][8];
+    each<2 * STEPS>([&](auto tile) {
         constexpr int t = tile;
-        f4 s = f4{0.0f, 0.0f, 0.0f, 0.0f};
-        if (EARLIER || t <= w) {
+        if constexpr (t < TILES) {
+            f4 s = f4{0.0f, 0.0f, 0.0f, 0.0f};
             each<P::DK / 32>([&](auto d) {
                 Vec<E, 8> kterms[P::RAW];
                 each<P::RAW>([&](auto p) { kterms[p] = *reinterpret_cast<const Vec<E, 8> *>(&kl[p][16 * t + i][32 * d + 8 * g]); });
                 product<N::ORDER_RAW>(s, kterms, q[d]);
             });
-        }
-        if (!EARLIER && t == w) {        // (a product that is not in the sum may be infinite)
-            each<4>([&](auto e) { x[t / 2][4 * (t % 2) + e] = i >= 4 * g + e ? s[(int)e] * inside[(int)e] : 0.0f; });
-        } else {                         // (of later tiles s is 0)
-            const f4 far = *reinterpret_cast<const f4 *>(&behind[EARLIER ? 16 * t + 4 * g : (kChunk - 16 * (w - t) + 4 * g) & (kChunk - 1)]);
-            each<4>([&](auto e) { x[t / 2][4 * (t % 2) + e] = s[(int)e] * from_first * far[(int)e]; });
+            if constexpr (t == W) {      // (a product that is not in the sum may be infinite)
+                each<4>([&](auto e) { x[t / 2][4 * (t % 2) + e] = i >= 4 * g + e ? s[(int)e] * inside[(int)e] : 0.0f; });
+            } else {
+                const f4 far = *reinterpret_cast<const f4 *>(&behind[kChunk - 16 * (W - t) + 4 * g]);
+                each<4>([&](auto e) { x[t / 2][4 * (t % 2) + e] = s[(int)e] * from_first * far[(int)e]; });
+            }
+        } else {
+            each<4>([&](auto e) { x[t / 2][4 * (t % 2) + e] = 0.0f; });
         }
     });
     keys_done();
     float up = 1.0f, back = 1.0f;
     if constexpr (P::SCALED) {
-        const Scale scale(column_max(largest(x[1], largest(x[0]))));
+        float m = 0.0f;
+        each<STEPS>([&](auto ks) { m = largest(x[ks], m); });
+        const Scale scale(column_max(m));
         up = scale.up, back = scale.down;
     }
-    auto values = [&](auto steps) {
-        Vec<E, 8> pt[steps][P::MADE];
-        each<steps>([&](auto ks) { split(x[ks], pt[ks], up); });
-        each<4>([&](auto t) {
-            const int row = 4 * g + (i >> 2), col = half + 16 * t + 4 * (i & 3);
-            f4 sum = P::SCALED ? zeros() : o[t];
-            each<steps>([&](auto ks) {
-                Vec<E, 8> vterms[P::RAW];
-                each<P::RAW>([&](auto p) {
-                    vterms[p] = join<E>(read_transposed(&vl[p][32 * ks + row][col]), read_transposed(&vl[p][32 * ks + row + 16][col]));
-                });
-                product<N::ORDER>(sum, vterms, pt[ks]);
+    Vec<E, 8> pt[STEPS][P::MADE];
+    each<STEPS>([&](auto ks) { split(x[ks], pt[ks], up); });
+    each<4>([&](auto t) {
+        const int row = 4 * g + (i >> 2), col = half + 16 * t + 4 * (i & 3);
+        f4 sum = P::SCALED ? zeros() : o[t];
+        each<STEPS>([&](auto ks) {
+            Vec<E, 8> vterms[P::RAW];
+            each<P::RAW>([&](auto p) {
+                vterms[p] = join<E>(read_transposed(&vl[p][32 * ks + row][col]), read_transposed(&vl[p][32 * ks + row + 16][col]));
             });
-            if constexpr (P::SCALED) {
-                each<4>([&](auto e) { o[t][(int)e] = __builtin_fmaf(sum[(int)e], back, o[t][(int)e]); });
-            } else {
-                o[t] = sum;
-            }
+            product<N::ORDER>(sum, vterms, pt[ks]);
         });
-    };
-    if (EARLIER || w >= 2) values(std::integral_constant<int, 2>());
-    else values(std::integral_constant<int, 1>());
+        if constexpr (P::SCALED) {
+            each<4>([&](auto e) { o[t][(int)e] = __builtin_fmaf(sum[(int)e], back, o[t][(int)e]); });
+        } else {
+            o[t] = sum;
+        }
+    });
+}
+
+// The same for a wavefront's own chunk: each wavefront has code of its own, without a branch in it, so that loads and products of its tiles overlap.
+template <class P, class F>
+__device__ inline void add_own_values(f4 (&o)[4], const Vec<typename P::E, 8> (&q)[P::DK / 32][P::RAW], const typename P::E (*kl)[kChunk][P::KP],
+                                      const typename P::E (*vl)[kChunk][P::VP], int w, int half, const f4 &inside, float from_first, const float *behind,
+                                      F keys_done) {
+    if (w == 0) add_values<P, 0>(o, q, kl, vl, half, inside, from_first, behind, keys_done);
+    else if (w == 1) add_values<P, 1>(o, q, kl, vl, half, inside, from_first, behind, keys_done);
+    else if (w == 2) add_values<P, 2>(o, q, kl, vl, half, inside, from_first, behind, keys_done);
+    else add_values<P, 3>(o, q, kl, vl, half, inside, from_first, behind, keys_done);
 }
 
 // Wavefronts on a SIMD: as many workgroups as have room for their rows in a CU's LDS, unless registers would go to scratch memory, whose loads wait for
 // the rows that are under way (8 x 16384 tokens, 4 heads of 64, bf16: 65 us with 165 registers, 93 with 168 and 22 in memory).
 template <class P>
 constexpr int rows_waves() {
-    return P::RAW == 3 ? (P::DK <= 32 || P::HALVES == 2 ? 2 : 1) : P::DK <= 64 ? 3 : 2;
+    return P::RAW == 3 ? (P::DK <= 32 || P::HALVES == 2 ? 2 : 1) : P::DK <= 96 ? 3 : 2;
 }
-
-// Whether the next queries are asked for before the present ones have met the keys, which takes registers of their own.
-template <class P>
-constexpr bool early_queries() { return P::RAW == 3 || P::DK == 128; }
 
 // Rows of the result.  A workgroup has one segment, the heads of one state and a slice of the columns and goes through the chunks one after the other;
 // of each half of the slice, wavefront w has queries 16 w to 16 w + 15 of a chunk, and columns 16 w to 16 w + 15 of the state.
@@ -407,7 +432,7 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
 
     const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int w = wave & 3, half = kHalf * (wave >> 2), query = 16 * w + i;
-    const float rate = decay_rate(a.g[hk]);
+    const float rate = uniform(decay_rate(a.g[hk]));
     const int chunks = (tokens + kChunk - 1) / kChunk;
     auto in_chunk = [&](int c) { return tokens - c * kChunk < kChunk ? tokens - c * kChunk : kChunk; };
 
@@ -437,32 +462,31 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
     // on any way to that place.  So every turn of the loop asks for as many rows and queries and stores as many, and what is
     // not needed goes nowhere; and the loop is entered as it is entered again, keys and values before queries before stores.  (With branches around
     // them each chunk waited for the rows of the next one and for the stores of the last.)
-    rows.load(kt.at(), vt.at(), in_chunk(0));                // (of an empty sequence nothing)
-    q.load(qt.at(), qat, query < in_chunk(0), kwidth);
-    auto store = [&](__amdgpu_buffer_rsrc_t to, bool there, const f4 (&o)[4]) {
+    rows.load(kt, vt, chunks > 0 ? in_chunk(0) : 0);
+    q.load(qt, qat, chunks > 0 ? in_chunk(0) : 0, kwidth);
+    auto store = [&](int n, uint64_t more, const f4 (&o)[4]) {
+        const __amdgpu_buffer_rsrc_t to = ot.rows(n, more);
         each<2>([&](auto p) {
             float x[8];
             each<8>([&](auto e) { x[e] = o[2 * p + e / 4][e % 4]; });
-            store_eight<T, STREAM>(to, (oat + 8 * p * (uint32_t)sizeof(T)) | (there && c0 + half + 16 * g + 8 * p < vwidth ? 0u : kNowhere), x);
+            store_eight<T, STREAM>(to, c0 + half + 16 * g + 8 * p < vwidth ? oat - ot.skipped(n) + 8 * p * (uint32_t)sizeof(T) : kNowhere, x);
         });
     };
     stage_weights(weight, rate, kChunk < tokens ? kChunk : tokens, shift, update);
     stage_weights(behind, rate, kChunk, 0, 1.0f);
-    const float from_first = r.inside * decay_pow(rate, i);
+    const float from_first = decay_pow(rate, i), scale = r.inside, into = uniform(r.into * decay_pow(rate, 16 * w + shift));
     f4 inside;
-    each<4>([&](auto e) { inside[(int)e] = i >= 4 * g + e ? r.inside * decay_pow(rate, i - 4 * g - e) : 0.0f; });
-    const float into = r.into * decay_pow(rate, query + shift);
-    float carry = decay_pow(rate, kChunk);
+    each<4>([&](auto e) { inside[(int)e] = i >= 4 * g + e ? scale * decay_pow(rate, i - 4 * g - e) : 0.0f; });
+    float carry = uniform(decay_pow(rate, kChunk));
 
     f4 o[4];
     each<4>([&](auto t) { o[t] = zeros(); });
-    store(ot.at(), false, o);
-    Vec<E, 8> qterms[DK / 32][P::RAW];
+    store(0, 0, o);
     // h: of several heads of keys and values that are added up; u: of several heads of queries.  One of the two has more than one.
     for (int c = 0; c < chunks; ++c) {
         const int n = in_chunk(c), next = c + 1 < chunks ? in_chunk(c + 1) : 0;
         const bool add = next > 0 || last != nullptr;
-        if (n < kChunk) carry = decay_pow(rate, n);
+        if (n < kChunk) carry = uniform(decay_pow(rate, n));
         int h = 0;
         do {
             if (c + h > 0) __syncthreads();
@@ -470,41 +494,40 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
             if (h == 0) {
                 if (n < kChunk && c > 0) stage_weights(weight, rate, n, shift, update);
                 if (live) state.stage(sl, down);
-                q.terms(qterms);             // (ahead of the next rows, which they would be waited for with)
             }
+            if (h == 0 || P::RAW == 1) q.arrived();          // (ahead of the next rows, which they would be waited for with)
             const bool end = h + 1 == sums;
             kt.base += end ? (uint64_t)kt.next - (uint64_t)(sums - 1) * kmore : kmore;
             vt.base += end ? (uint64_t)vt.next - (uint64_t)(sums - 1) * vmore : vmore;
-            rows.load(kt.at(), vt.at(), end ? next : n);
+            rows.load(kt, vt, end ? next : n);
             __syncthreads();
             int u = 0;
             do {
                 auto next_q = [&] {
                     const bool turn = u + 1 == outs;
                     if (end) qt.base += turn ? (uint64_t)qt.next - (uint64_t)(outs - 1) * kmore : kmore;
-                    q.load(qt.at(), qat, query < (turn ? (end ? next : 0) : n), kwidth);
+                    q.load(qt, qat, turn && end ? next : n, kwidth);     // (the same again for the next head of the keys)
                 };
-                if (u > 0) q.terms(qterms);
+                if (u > 0) q.arrived();
                 if (h == 0) each<4>([&](auto t) { o[t] = zeros(); });
-                if (early_queries<P>()) next_q();
                 if (h == 0 && live) {
                     each<DK / 32>([&](auto s) {
                         each<4>([&](auto t) {
                             Vec<E, 8> st[P::MADE];
                             each<P::MADE>([&](auto p) { st[p] = *reinterpret_cast<const Vec<E, 8> *>(&sl[p][half + 16 * t + i][32 * s + 8 * g]); });
-                            product<Terms<T>::ORDER>(o[t], st, qterms[s]);
+                            product<Terms<T>::ORDER>(o[t], st, q.t[s]);
                         });
                     });
                     each<4>([&](auto t) {
                         if constexpr (P::SCALED) {
-                            o[t] *= *reinterpret_cast<const f4 *>(&down[half + 16 * t + 4 * g]) * into;
+                            o[t] *= *reinterpret_cast<const f4 *>(&down[half + 16 * t + 4 * g]) * (from_first * into);
                         } else {
-                            o[t] *= into;
+                            o[t] *= from_first * into;
                         }
                     });
                 }
-                add_values<P, false>(o, qterms, kl, vl, w, half, inside, from_first, behind, [&] { if (!early_queries<P>()) next_q(); });
-                store(ot.at((uint64_t)u * vmore), end && query < n, o);
+                add_own_values<P>(o, q.t, kl, vl, w, half, inside, scale * from_first, behind, next_q);
+                store(end ? n : 0, (uint64_t)u * vmore, o);
             } while (++u < outs);
             // (a state that only rows in 16 bits are made of takes the terms that these do)
             if (add) {
@@ -524,7 +547,6 @@ template <class P>
 __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_short_kernel(const Args a) {
     typedef typename P::T T;
     typedef typename P::E E;
-    constexpr int DK = P::DK;
     __shared__ __attribute__((aligned(16))) E kl[P::RAW][kChunk][P::KP];
     __shared__ __attribute__((aligned(16))) E vl[P::RAW][kChunk][P::VP];
     __shared__ __attribute__((aligned(16))) float behind[kChunk];
@@ -544,7 +566,7 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_short_ker
 
     const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int w = wave & 3, half = kHalf * (wave >> 2), query = 16 * w + i;
-    const float rate = decay_rate(a.g[hk]);
+    const float rate = uniform(decay_rate(a.g[hk]));
     Tokens qt, kt, vt, ot;
     qt.set<T>(r.q, sp, sp.seg * kChunk, reverse, hk * r.outs + sub, 0);
     ot.set<T>(r.out, sp, sp.seg * kChunk, reverse, hk * r.outs + sub, c0);
@@ -555,36 +577,33 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_short_ker
     Rows<P> rows;
     rows.places(kt, kwidth, vt, vwidth - c0);
     Queries<P> q;
-    q.load(qt.at(), qat, query < mine, kwidth);
-    rows.load(kt.at(), vt.at(), sp.seg > 0 ? kChunk : mine);
+    q.load(qt, qat, mine, kwidth);
+    rows.load(kt, vt, sp.seg > 0 ? kChunk : mine);
     stage_weights(behind, rate, kChunk, 0, 1.0f);
     const float from_first = r.inside * decay_pow(rate, i);
     f4 inside;
     each<4>([&](auto e) { inside[(int)e] = i >= 4 * g + e ? r.inside * decay_pow(rate, i - 4 * g - e) : 0.0f; });
     f4 o[4];
     each<4>([&](auto t) { o[t] = zeros(); });
-    Vec<E, 8> qterms[DK / 32][P::RAW];
-    q.terms(qterms);
+    q.arrived();
     for (int c = 0; c <= sp.seg; ++c) {
         for (int h = 0; h < sums; ++h) {
             if (c + h > 0) __syncthreads();
             rows.stage(kl, vl);
-            if (h + 1 < sums) {
-                rows.load(kt.at((uint64_t)(h + 1) * kmore), vt.at((uint64_t)(h + 1) * vmore), c < sp.seg ? kChunk : mine);
-            } else if (c < sp.seg) {
-                kt.base += (uint64_t)kt.next, vt.base += (uint64_t)vt.next;
-                rows.load(kt.at(), vt.at(), c + 1 < sp.seg ? kChunk : mine);
-            }
+            const bool end = h + 1 == sums;
+            kt.base += end ? (uint64_t)kt.next - (uint64_t)(sums - 1) * kmore : kmore;
+            vt.base += end ? (uint64_t)vt.next - (uint64_t)(sums - 1) * vmore : vmore;
+            rows.load(kt, vt, c + end < sp.seg ? kChunk : c + end == sp.seg ? mine : 0);
             __syncthreads();
-            if (c < sp.seg) add_values<P, true>(o, qterms, kl, vl, w, half, inside, r.inside * decay_pow(rate, query + kChunk * (sp.seg - c - 1)), behind, [] {});
-            else add_values<P, false>(o, qterms, kl, vl, w, half, inside, from_first, behind, [] {});
+            if (c < sp.seg) add_values<P, 4>(o, q.t, kl, vl, half, inside, r.inside * decay_pow(rate, query + kChunk * (sp.seg - c - 1)), behind, [] {});
+            else add_own_values<P>(o, q.t, kl, vl, w, half, inside, from_first, behind, [] {});
         }
     }
-    const __amdgpu_buffer_rsrc_t to = ot.at();
+    const __amdgpu_buffer_rsrc_t to = ot.rows(mine);
     each<2>([&](auto p) {
         float x[8];
         each<8>([&](auto e) { x[e] = o[2 * p + e / 4][e % 4]; });
-        store_eight<T, false>(to, query < mine && c0 + half + 16 * g + 8 * p < vwidth ? oat + 8 * p * (uint32_t)sizeof(T) : kNowhere, x);
+        store_eight<T, false>(to, c0 + half + 16 * g + 8 * p < vwidth ? oat - ot.skipped(mine) + 8 * p * (uint32_t)sizeof(T) : kNowhere, x);
     });
 }
 
@@ -609,7 +628,7 @@ __global__ __launch_bounds__(P::THREADS) void decay_states_kernel(const Args a) 
     // the last segment's sum is for the state behind the sequence only
     if (sp.seg < 0 || left <= 0 || (left <= a.seq.seg && r.last == nullptr)) return;
     const int tokens = left < a.seq.seg ? left : a.seq.seg, chunks = (tokens + kChunk - 1) / kChunk;
-    const float rate = decay_rate(a.g[hk]);
+    const float rate = uniform(decay_rate(a.g[hk]));
     State<P> state;
     state.clear();
     auto in_chunk = [&](int c) { return tokens - c * kChunk < kChunk ? tokens - c * kChunk : kChunk; };
@@ -619,23 +638,21 @@ __global__ __launch_bounds__(P::THREADS) void decay_states_kernel(const Args a) 
     const uint32_t kmore = (uint32_t)kwidth * (uint32_t)sizeof(T), vmore = (uint32_t)vwidth * (uint32_t)sizeof(T);
     Rows<P> rows;
     rows.places(kt, kwidth, vt, vwidth - c0);
-    rows.load(kt.at(), vt.at(), in_chunk(0));
+    rows.load(kt, vt, in_chunk(0));
     __shared__ __attribute__((aligned(16))) float weight[kChunk];
     stage_weights(weight, rate, kChunk < tokens ? kChunk : tokens, shift, update);
     float carry = decay_pow(rate, kChunk);
     for (int c = 0; c < chunks; ++c) {
         const int n = in_chunk(c);
-        if (n < kChunk) carry = decay_pow(rate, n);
+        if (n < kChunk) carry = uniform(decay_pow(rate, n));
         for (int h = 0; h < sums; ++h) {
             if (c + h > 0) __syncthreads();
             rows.stage(kl, vl);
             if (n < kChunk && c > 0 && h == 0) stage_weights(weight, rate, n, shift, update);
-            if (h + 1 < sums) {
-                rows.load(kt.at((uint64_t)(h + 1) * kmore), vt.at((uint64_t)(h + 1) * vmore), n);
-            } else if (c + 1 < chunks) {
-                kt.base += (uint64_t)kt.next, vt.base += (uint64_t)vt.next;
-                rows.load(kt.at(), vt.at(), in_chunk(c + 1));
-            }
+            const bool end = h + 1 == sums;
+            kt.base += end ? (uint64_t)kt.next - (uint64_t)(sums - 1) * kmore : kmore;
+            vt.base += end ? (uint64_t)vt.next - (uint64_t)(sums - 1) * vmore : vmore;
+            rows.load(kt, vt, !end ? n : c + 1 < chunks ? in_chunk(c + 1) : 0);
             __syncthreads();
             if (P::MADE == P::ADDED || r.last != nullptr) state.template update<P::ADDED>(kl, vl, weight, h == 0 ? carry : 1.0f);
             else state.template update<P::MADE>(kl, vl, weight, h == 0 ? carry : 1.0f);
@@ -654,7 +671,7 @@ __global__ __launch_bounds__(kScanThreads) void decay_scan_kernel(const Args a) 
     const Span sp = a.seq.of_sequence(b);
     const int place = r.first != nullptr || r.last != nullptr ? state_place(a, b) : -1;
     const int segs = (sp.length + a.seq.seg - 1) / a.seq.seg;
-    const float rate = decay_rate(a.g[hk]);
+    const float rate = uniform(decay_rate(a.g[hk]));
     f4 x = f4{0.0f, 0.0f, 0.0f, 0.0f};
     if (r.first != nullptr && place >= 0) x = *reinterpret_cast<const f4 *>(a.place(r.first, place, hk) + at);
     float *p = a.place(r.sums_out, sp.unit, hk) + at;
