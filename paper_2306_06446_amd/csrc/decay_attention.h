@@ -111,14 +111,17 @@ __device__ inline Vec<E, 4> read_transposed(const E *p) {
 template <class E>
 __device__ inline Vec<E, 8> join(const Vec<E, 4> &a, const Vec<E, 4> &b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
+// What all lanes have the same, in a scalar register.
+// (The builtin's result is signed: as the low half of an address it would set all of the high one.)
+__device__ inline uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+__device__ inline float uniform(float x) { return __builtin_bit_cast(float, uniform(__builtin_bit_cast(uint32_t, x))); }
+
 // Rows of one head, from memory: a base and a size in bytes that all lanes share and a 32-bit offset each.  What begins behind the size, as kNowhere
 // and up to 2^30 less do, reads as zeros and is not written, without a branch.
 constexpr uint32_t kNowhere = 0xc0000000u;
 __device__ inline __amdgpu_buffer_rsrc_t buffer(uint64_t p, uint32_t bytes) {
-    // (the builtin's result is signed: a low half of 2^31 or more would set all of the high one)
-    const uint32_t high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)), low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p);
-    const uint64_t at = (uint64_t)high << 32 | low;
-    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(at), 0, __builtin_amdgcn_readfirstlane((int)bytes), 0x00027000);
+    const uint64_t at = (uint64_t)uniform((uint32_t)(p >> 32)) << 32 | uniform((uint32_t)p);
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(at), 0, (int)uniform(bytes), 0x00027000);
 }
 
 // 8 elements on their way from memory to LDS.
@@ -203,23 +206,28 @@ struct Sequences {
     }
     // The sequence that has unit u: the last one whose first unit is not behind u, 64 sequences at a time.
     __device__ inline Span of_unit(uint32_t u) const {
-        int b = 0;
         if (offsets == nullptr) {
-            b = per_sequence == 1 ? (int)u : (int)(u / (uint32_t)per_sequence);
-        } else {
-            int n = B;
-            while (n > 1) {
-                const int step = (n + 63) >> 6, lane = (int)(threadIdx.x & 63), at = lane * step;
-                const int place = b + (at < n ? at : 0);
-                const uint64_t there = __ballot(at < n && (uint32_t)((offset(place) >> log_seg) + place) <= u);
-                const int last = there == 0 ? 0 : 63 - __builtin_clzll(there);
-                b += last * step;
-                n = n - last * step < step ? n - last * step : step;
-            }
-            b = __builtin_amdgcn_readfirstlane(b);
+            Span s = of_sequence(per_sequence == 1 ? (int)u : (int)(u / (uint32_t)per_sequence));
+            s.seg = (int)u - s.unit;
+            s.unit = (int)u;
+            return s;
         }
-        Span s = of_sequence(b);
-        s.seg = (int)u - s.unit;
+        int b = 0, n = B, at, last;
+        do {
+            const int step = (n + 63) >> 6, lane = (int)(threadIdx.x & 63) * step, place = b + (lane < n ? lane : n);
+            at = offset(place);          // (there are B + 1 of them)
+            const uint64_t there = __ballot(lane < n && (uint32_t)((at >> log_seg) + place) <= u);
+            last = there == 0 ? 0 : 63 - __builtin_clzll(there);
+            b += last * step;
+            n = n - last * step < step ? n - last * step : step;
+        } while (n > 1);
+        // the last round's lanes have the sequence's first token and, but for the last lane, the one behind its last
+        Span s;
+        s.seq = __builtin_amdgcn_readfirstlane(b);
+        s.begin = __builtin_amdgcn_readlane(at, last);
+        const int end = last < 63 ? __builtin_amdgcn_readlane(at, last + 1) : __builtin_amdgcn_readfirstlane(offset(s.seq + 1));
+        s.length = end > s.begin ? end - s.begin : 0;
+        s.seg = (int)u - ((s.begin >> log_seg) + s.seq);
         s.unit = (int)u;
         return s;
     }
@@ -227,17 +235,18 @@ struct Sequences {
 
 // exp(n g), n >= 0, as 2^(n g / ln 2): the exponent is rounded twice, relative to itself, so a result of 2^-20 is off by some 30 units and one near 1 by
 // one or two.  A head without memory (g = -infinity) has 1 for n = 0 and 0 for all others: so has one of -2000.
-__device__ inline float uniform(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
 __device__ inline float decay_rate(float g) { return (g < -2000.0f ? -2000.0f : g) * 1.44269504f; }
 __device__ inline float decay_pow(float rate, int n) { return __builtin_amdgcn_exp2f(rate * (float)n); }
 
-// A workgroup's share of the launch: workgroups go to the 8 XCDs in turn, neighbours of one list of work belong on one XCD (they read the
-// same keys and values).
-__device__ inline uint32_t xcd_place(uint32_t total) {
-    const uint32_t each = (total + 7) / 8, i = blockIdx.x;
-    return (i & 7) * each + (i >> 3);
+// Workgroups go to the 8 XCDs in turn.  Those of one segment (`per` of them, which read the same rows) belong on one XCD.  Equal segments that follow each
+// other do, too (8 x 16384 tokens, 4 heads of 64: 98 -> 94 us); those of a ragged batch are dealt one at a time, so that no XCD has the long
+// sequences (50021 tokens in 37 sequences, 12 heads of 96 over 4 of 72, fp16: 180 -> 162).  The segment, and the workgroup's place in it.
+__device__ inline uint32_t xcd_unit(uint32_t units, uint32_t per, bool equal, uint32_t &place) {
+    const uint32_t i = blockIdx.x, k = i >> 3, round = per == 1 ? k : k / per;
+    place = k - round * per;
+    return equal ? (i & 7) * ((units + 7) / 8) + round : round * 8 + (i & 7);
 }
-inline long xcd_blocks(long total) { return (total + 7) / 8 * 8; }
+inline long xcd_blocks(long groups, long per) { return (groups + 7) / 8 * 8 * per; }
 
 template <class F>
 int by_type(int type, F f) {

@@ -38,7 +38,7 @@ struct Args {
     Role role[3];
     uint32_t shares[3];      // of a segment and key/value head: workgroups of the roles up to this one
     int roles;
-    uint32_t total;          // workgroups
+    uint32_t units;          // segments
     Sequences seq;
     const float *g;
     int Hk, dv;              // (dv: columns of a state in memory)
@@ -62,6 +62,8 @@ struct Shape {
     static constexpr int KP = DK + 16, VP = COLS + 16;
     // Columns of the values, and of the state, are in LDS in the order in which the product with them takes them: tile t's row 4 a + b is column
     // 16 a + 4 t + b of 64, so that a lane's results are 16 columns side by side while a tile's columns are side by side in LDS.
+    // (fp16) The columns' scales are behind the values' rows, 8 to a row: 256 bytes more would be a workgroup less of keys of 96 on a CU.
+    static __device__ inline float *down(E (*vl)[kChunk][VP], int at) { return reinterpret_cast<float *>(&vl[0][at >> 3][COLS]) + (at & 7); }
     static __device__ inline int column(int at) { return (at & ~63) + 16 * ((at & 15) >> 2) + 4 * ((at & 63) >> 4) + (at & 3); }
     static constexpr int KPIECES = kChunk * DK / 8 / THREADS, VPIECES = kChunk * COLS / 8 / THREADS;
     static constexpr int TILES = DK / 16;
@@ -184,8 +186,8 @@ struct State {
             }
         });
     }
-    // To LDS as terms, for the product with q: [column][row].  `down`: the columns' scales.
-    __device__ inline void stage(E (*sl)[P::COLS][P::KP], float *down) const {
+    // To LDS as terms, for the product with q: [column][row].
+    __device__ inline void stage(E (*sl)[P::COLS][P::KP], E (*vl)[kChunk][P::VP]) const {
         const int lane = (int)threadIdx.x & 63, g = lane >> 4, at = 16 * ((int)threadIdx.x >> 6) + (lane & 15);
         float up = 1.0f;
         if constexpr (P::SCALED) {
@@ -197,7 +199,7 @@ struct State {
             });
             const Scale scale(column_max(m));
             up = scale.up;
-            if (g == 0) down[at] = scale.down;
+            if (g == 0) *P::down(vl, at) = scale.down;
         }
         each<P::TILES>([&](auto t_) {
             constexpr int t = t_;
@@ -280,11 +282,12 @@ __device__ inline int state_place(const Args &a, int seq) {
     return p >= 0 && p < a.places ? p : -1;
 }
 
-// A workgroup's role and its place in it.  All workgroups of one segment and head follow each other, on one XCD: a gradient's three roles read the same rows.
-__device__ inline const Role &role_of(const Args &a, uint32_t &item, uint32_t &rest) {
+// A workgroup's role, segment and key/value head and, of the role, its slice of columns (and head).
+__device__ inline const Role &role_of(const Args &a, uint32_t &unit, int &hk, uint32_t &item) {
     const uint32_t per = a.shares[a.roles - 1];
-    rest = per == 1 ? item : item / per;
-    item -= rest * per;
+    unit = uniform(xcd_unit(a.units, per * (uint32_t)a.Hk, a.seq.offsets == nullptr, item));
+    hk = (int)uniform(per == 1 ? item : item / per);
+    item = uniform(item - (uint32_t)hk * per);
     int r = 0;
     while (r + 1 < a.roles && item >= a.shares[r]) ++r;
     if (r > 0) item -= a.shares[r - 1];
@@ -414,17 +417,19 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
     __shared__ __attribute__((aligned(16))) E kl[P::RAW][kChunk][P::KP];
     __shared__ __attribute__((aligned(16))) E vl[P::RAW][kChunk][P::VP];
     __shared__ __attribute__((aligned(16))) E sl[P::MADE][P::COLS][P::KP];
-    __shared__ __attribute__((aligned(16))) float down[P::SCALED ? P::COLS : 4];
     __shared__ __attribute__((aligned(16))) float weight[kChunk], behind[kChunk];      // exp(g (64 - j)) in the latter
-    uint32_t item = xcd_place(a.total), rest;
-    if (item >= a.total) return;
-    const Role &r = role_of(a, item, rest);
+    uint32_t unit, item;
+    int hk;
+    const Role &r = role_of(a, unit, hk, item);
+    if (unit >= a.units) return;
     const int kwidth = r.k.width, vwidth = r.v.width, sums = r.sums, outs = r.outs, shift = r.shift;
     const float update = r.update;
     const bool transposed = r.transposed, reverse = r.reverse;
     const int c0 = (int)item * P::COLS;
-    const uint32_t unit = rest / (uint32_t)a.Hk;
-    const int hk = (int)(rest - unit * (uint32_t)a.Hk);
+    State<P> state;
+    const bool segments = r.starts != nullptr;       // (asked for first: it takes nothing but the segment's number to find it)
+    if (segments) state.load(a.place(r.starts, (int)unit, hk), transposed, kwidth, vwidth, a.dv, c0);
+    else state.clear();
     const Span sp = a.seq.of_unit(unit);
     const int p0 = sp.seg * a.seq.seg, left = sp.length - p0;
     if (sp.seg < 0 || (left <= 0 && (sp.seg > 0 || r.last == nullptr))) return;
@@ -447,16 +452,10 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
     rows.places(kt, kwidth, vt, vwidth - c0);
     Queries<P> q;
 
-    State<P> state;
-    bool live = false;                   // a state that is not zero
     const int place = r.first != nullptr || r.last != nullptr ? state_place(a, sp.seq) : -1;
     float *const last = r.last != nullptr && place >= 0 ? a.place(r.last, place, hk) : nullptr;
-    if (r.starts != nullptr || (r.first != nullptr && place >= 0)) {
-        state.load(r.starts != nullptr ? a.place(r.starts, sp.unit, hk) : a.place(r.first, place, hk), transposed, kwidth, vwidth, a.dv, c0);
-        live = true;
-    } else {
-        state.clear();
-    }
+    bool live = segments || (r.first != nullptr && place >= 0);      // a state that is not zero
+    if (live && !segments) state.load(a.place(r.first, place, hk), transposed, kwidth, vwidth, a.dv, c0);
 
     // Loads and stores come back in the order in which they left, and the compiler counts those behind the one it waits for, the fewest that may be there
     // on any way to that place.  So every turn of the loop asks for as many rows and queries and stores as many, and what is
@@ -493,7 +492,7 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
             rows.stage(kl, vl);
             if (h == 0) {
                 if (n < kChunk && c > 0) stage_weights(weight, rate, n, shift, update);
-                if (live) state.stage(sl, down);
+                if (live) state.stage(sl, vl);
             }
             if (h == 0 || P::RAW == 1) q.arrived();          // (ahead of the next rows, which they would be waited for with)
             const bool end = h + 1 == sums;
@@ -520,7 +519,7 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
                     });
                     each<4>([&](auto t) {
                         if constexpr (P::SCALED) {
-                            o[t] *= *reinterpret_cast<const f4 *>(&down[half + 16 * t + 4 * g]) * (from_first * into);
+                            o[t] *= *reinterpret_cast<const f4 *>(P::down(vl, half + 16 * t + 4 * g)) * (from_first * into);
                         } else {
                             o[t] *= from_first * into;
                         }
@@ -550,15 +549,14 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_short_ker
     __shared__ __attribute__((aligned(16))) E kl[P::RAW][kChunk][P::KP];
     __shared__ __attribute__((aligned(16))) E vl[P::RAW][kChunk][P::VP];
     __shared__ __attribute__((aligned(16))) float behind[kChunk];
-    uint32_t item = xcd_place(a.total), rest;
-    if (item >= a.total) return;
-    const Role &r = role_of(a, item, rest);
+    uint32_t unit, item;
+    int hk;
+    const Role &r = role_of(a, unit, hk, item);
+    if (unit >= a.units) return;
     const int kwidth = r.k.width, vwidth = r.v.width, sums = r.sums;
     const bool reverse = r.reverse;
     const uint32_t slices = vwidth > P::COLS ? 2 : 1;
     const int sub = (int)(slices == 2 ? item >> 1 : item), c0 = (int)(slices == 2 ? item & 1 : 0) * P::COLS;
-    const uint32_t unit = rest / (uint32_t)a.Hk;
-    const int hk = (int)(rest - unit * (uint32_t)a.Hk);
     const Span sp = a.seq.of_unit(unit);
     const int left = sp.length - sp.seg * kChunk;
     if (sp.seg < 0 || left <= 0) return;
@@ -614,15 +612,14 @@ __global__ __launch_bounds__(P::THREADS) void decay_states_kernel(const Args a) 
     typedef typename P::E E;
     __shared__ __attribute__((aligned(16))) E kl[P::RAW][kChunk][P::KP];
     __shared__ __attribute__((aligned(16))) E vl[P::RAW][kChunk][P::VP];
-    uint32_t item = xcd_place(a.total), rest;
-    if (item >= a.total) return;
-    const Role &r = role_of(a, item, rest);
+    uint32_t unit, item;
+    int hk;
+    const Role &r = role_of(a, unit, hk, item);
+    if (unit >= a.units) return;
     const int kwidth = r.k.width, vwidth = r.v.width, sums = r.sums, shift = r.shift;
     const float update = r.update;
     const bool reverse = r.reverse;
     const int c0 = (int)item * P::COLS;
-    const uint32_t unit = rest / (uint32_t)a.Hk;
-    const int hk = (int)(rest - unit * (uint32_t)a.Hk);
     const Span sp = a.seq.of_unit(unit);
     const int p0 = sp.seg * a.seq.seg, left = sp.length - p0;
     // the last segment's sum is for the state behind the sequence only
@@ -806,11 +803,11 @@ int by_forms(const char *what, int type, const Args &a, int roles, bool shorts, 
             some.role[some.roles] = a.role[s];
             some.shares[some.roles++] = shares;
         }
-        const long total = a.seq.units() * a.Hk * shares;
-        some.total = (uint32_t)total;
-        SA_REQUIRE(total < (1L << 31) - 8, SA_ERR_UNSUPPORTED, "%s: too many heads and tokens for one launch", what);
+        const long total = xcd_blocks(a.seq.units(), (long)shares * a.Hk);
+        some.units = (uint32_t)a.seq.units();
+        SA_REQUIRE(total < (1L << 31), SA_ERR_UNSUPPORTED, "%s: too many heads and tokens for one launch", what);
         SA_TRY(by_form(type, f, [&](auto shape) {
-            run(shape, dim3((unsigned)xcd_blocks(total)), some);
+            run(shape, dim3((unsigned)total), some);
             return check_launch(what);
         }));
     }
