@@ -675,7 +675,7 @@ __global__ __launch_bounds__(kScanThreads) void decay_scan_kernel(const Args a) 
     const long next = (long)a.Hk * a.state;
     const float whole = decay_pow(rate, a.seq.seg);
     const int sums = r.last != nullptr ? segs : segs - 1;    // (of the last segment only where the state behind it is asked for)
-    constexpr int kAhead = 8;
+    constexpr int kAhead = 16;
     for (int s = 0; s < segs; s += kAhead) {
         f4 add[kAhead];
         each<kAhead>([&](auto k) { add[k] = s + k < sums ? *reinterpret_cast<const f4 *>(p + (s + k) * next) : f4{0.0f, 0.0f, 0.0f, 0.0f}; });
@@ -706,7 +706,7 @@ Form form_of(int keys, int columns, int type) {
 Form form_of(const Role &r, int type) { return form_of(r.k.width, r.v.width, type); }
 int slices_of(int columns, const Form &f) { return columns > kHalf * f.halves ? 2 : 1; }
 // Workgroups of decay_rows_kernel that a CU has at once, by registers and LDS.
-int resident(const Form &f, int type) { return type == SA_F32 ? (f.keys == 32 ? 2 : 1) : f.keys <= 64 ? 3 : f.halves == 2 ? 1 : 2; }
+int resident(const Form &f, int type) { return type == SA_F32 ? (f.keys == 32 ? 2 : 1) : f.keys <= 96 ? 3 : f.halves == 2 ? 1 : 2; }
 
 struct Plan {
     int seg = 0;             // 0: one pass

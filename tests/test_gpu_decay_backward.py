@@ -138,3 +138,21 @@ def test_a_training_step_in_a_graph(sa, dtype):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip([o, last] + list(grads.values()), eager[i])), i
         torch.randn(1000, 1000, device="cuda").sum()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N", [130, 1400])
+def test_what_is_not_finite_stays_in_its_head(sa, N, dtype):
+    """A NaN in dout reaches gradients of its own sequence and head, of k and v up to 63 tokens behind it, of q from 63 before it on."""
+    s = sequences([N, N], 2, 2, 64, 64, dtype, seed=4, device="cuda")
+    call = lambda s: sa.sa_decay_attention_backward(s["dout"], s["q"], s["k"], s["v"], s["log_decay"], 0.1, offsets=s["offsets"])      # noqa: E731
+    clean = call(s)
+    at = N // 2
+    s["dout"][at, 0, 5] = float("nan")
+    for name, a, b in zip("qkv", call(s), clean):
+        assert torch.equal(a[N:], b[N:]) and torch.equal(a[:, 1], b[:, 1]), name
+        if name == "q":
+            assert torch.equal(a[:at - 63], b[:at - 63])
+        else:
+            assert torch.equal(a[at + 64:], b[at + 64:])
+        assert not a[at, 0].isfinite().all()
