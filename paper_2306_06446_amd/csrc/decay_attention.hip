@@ -7,6 +7,18 @@
 //   dq = (do, v, k) on S^T;  dv = (k, q, do) reversed, dk = (v, do, q) reversed, on R_t = l R_{t+1} + scale q_t do_t^T (dk: R^T)
 // R begins with the gradient of the last state, which meets the last token undecayed, so in reversed time a state is read as it is and decays on
 // its way on: l^i instead of l^(i + 1), l^(n - j) instead of l^(n - 1 - j) (`shift`).
+//
+// A chunk of 64 tokens: 32 have twice the state's ways to LDS, 128 twice the pairs of tokens.  Four wavefronts have 16 queries each, and 16 columns of the
+// state each, which stays in their registers; what a chunk adds to it and what the next one reads of it go through LDS.
+// Where sequences and states are too few to fill the GPU, sequences are cut into segments: what each adds to the state (decay_states_kernel), the states
+// before them (decay_scan_kernel), the rows from there (decay_rows_kernel).  Keys and values are then read twice.  Few short sequences need
+// no state (decay_short_kernel).
+//
+// What bounds it, with keys of up to 64 in 16 bits: memory.  8 x 16384 tokens, 4 heads of 64, bf16: rows 53 us (268 MB, 5 TB/s), sums of the segments 33
+// (134 MB), their scan 6; 64 x 197 tokens, 12 heads of 64, one pass: 20 us (77 MB, 15 at a copy's rate).  Its gradient at 8 x 16384: rows 135 us,
+// 805 MB through the memory-side cache of which 430 come from memory.  With keys of 128, latency: 16384 tokens, 16 heads of 128, bf16: rows
+// 81 us (268 MB; vector ALU 31 %, LDS 37 %, matrix cores 21 % of the time), as the terms of the state take 70 KB of LDS and 200 registers leave two
+// wavefronts to a SIMD.  The same of fp32, whose operands are three terms: 8 x 16384 tokens, 4 heads of 64: 234 us in all (537 MB, 107 us).
 #include <algorithm>
 #include <initializer_list>
 #include <type_traits>
@@ -103,14 +115,8 @@ struct Rows {
     __device__ inline static int vrow(int j) { return ((int)threadIdx.x + P::THREADS * j) / (P::COLS / 8); }
     __device__ inline static int vcol(int j) { return ((int)threadIdx.x + P::THREADS * j) % (P::COLS / 8) * 8; }
     __device__ inline void places(const Tokens &kt, int kwidth, const Tokens &vt, int vwidth) {
-        each<KN>([&](auto j_) {
-            constexpr int j = j_;
-            kat[j] = kcol(j) < kwidth ? kt.row(krow(j)) + kcol(j) * (uint32_t)sizeof(T) : kNowhere;
-        });
-        each<VN>([&](auto j_) {
-            constexpr int j = j_;
-            vat[j] = vcol(j) < vwidth ? vt.row(vrow(j)) + vcol(j) * (uint32_t)sizeof(T) : kNowhere;
-        });
+        each<KN>([&](auto j) { kat[j] = kcol(j) < kwidth ? kt.row(krow(j)) + kcol(j) * (uint32_t)sizeof(T) : kNowhere; });
+        each<VN>([&](auto j) { vat[j] = vcol(j) < vwidth ? vt.row(vrow(j)) + vcol(j) * (uint32_t)sizeof(T) : kNowhere; });
     }
     __device__ inline void load(const Tokens &kt, const Tokens &vt, int n) {
         const __amdgpu_buffer_rsrc_t kp = kt.rows(n), vp = vt.rows(n);
@@ -145,10 +151,7 @@ struct State {
     typedef typename P::E E;
     f4 s[P::TILES];
     __device__ inline void clear() {
-        each<P::TILES>([&](auto t_) {
-            constexpr int t = t_;
-            s[t] = zeros();
-        });
+        each<P::TILES>([&](auto t) { s[t] = zeros(); });
     }
     // Four rows of a lane are side by side in memory where the state lies there transposed.
     __device__ inline void load(const float *p, bool transposed, int rows, int cols, int dv, int c0) {
@@ -407,7 +410,8 @@ constexpr int rows_waves() {
     return P::RAW == 3 ? (P::DK <= 32 || P::HALVES == 2 ? 2 : 1) : P::DK <= 96 ? 3 : 2;
 }
 
-// Rows of the result.  A workgroup has one segment, the heads of one state and a slice of the columns and goes through the chunks one after the other;
+// Rows of the result.  A workgroup has one segment, the heads of one state (their keys, values and state are in LDS once for all of them: 12 heads of 96
+// over 4 of 72 250 -> 203 us) and a slice of the columns and goes through the chunks one after the other;
 // of each half of the slice, wavefront w has queries 16 w to 16 w + 15 of a chunk, and columns 16 w to 16 w + 15 of the state.
 template <class P, bool STREAM>
 __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kernel(const Args a) {
@@ -509,6 +513,8 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
                 };
                 if (u > 0) q.arrived();
                 if (h == 0) each<4>([&](auto t) { o[t] = zeros(); });
+                float decayed = from_first;
+                if constexpr (P::SCALED) asm("" : "+v"(decayed));        // (its products are made here again: with them kept, keys of 64 are a register short)
                 if (h == 0 && live) {
                     each<DK / 32>([&](auto s) {
                         each<4>([&](auto t) {
@@ -519,13 +525,13 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
                     });
                     each<4>([&](auto t) {
                         if constexpr (P::SCALED) {
-                            o[t] *= *reinterpret_cast<const f4 *>(P::down(vl, half + 16 * t + 4 * g)) * (from_first * into);
+                            o[t] *= *reinterpret_cast<const f4 *>(P::down(vl, half + 16 * t + 4 * g)) * (decayed * into);
                         } else {
-                            o[t] *= from_first * into;
+                            o[t] *= decayed * into;
                         }
                     });
                 }
-                add_own_values<P>(o, q.t, kl, vl, w, half, inside, scale * from_first, behind, next_q);
+                add_own_values<P>(o, q.t, kl, vl, w, half, inside, scale * decayed, behind, next_q);
                 store(end ? n : 0, (uint64_t)u * vmore, o);
             } while (++u < outs);
             // (a state that only rows in 16 bits are made of takes the terms that these do)
@@ -540,7 +546,8 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
     if (last != nullptr) state.store(last, transposed, kwidth, vwidth, a.dv, c0);
 }
 
-// Short sequences without a state before or behind them: a workgroup has 64 queries of one head and a slice of the columns, and adds the values of
+// Few short sequences without a state before or behind them (197 tokens, 3 heads of 64, fp32: 21 -> 12 us on the device; with 768 sequences and heads of 197
+// tokens one pass is faster, 20.5 us to 24.6): a workgroup has 64 queries of one head and a slice of the columns, and adds the values of
 // all keys up to them, chunk by chunk, without a state: all queries at once instead of one chunk after the other.
 template <class P>
 __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_short_kernel(const Args a) {
@@ -605,7 +612,7 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_short_ker
     });
 }
 
-// What each segment adds to the state, from a state of zeros.
+// What each segment adds to the state, from a state of zeros.  The chunks' keys and values pass through LDS for the transposed reads alone.
 template <class P>
 __global__ __launch_bounds__(P::THREADS) void decay_states_kernel(const Args a) {
     typedef typename P::T T;
@@ -658,7 +665,8 @@ __global__ __launch_bounds__(P::THREADS) void decay_states_kernel(const Args a) 
     state.store(a.place(r.sums_out, sp.unit, hk), r.transposed, kwidth, vwidth, a.dv, c0);
 }
 
-// From the segments' sums to the states before them, in their place, and to the state behind the sequence.  A thread has 4 elements.
+// From the segments' sums to the states before them, in their place, and to the state behind the sequence.  A thread has 4 elements, 16 segments of them
+// under way at a time (one at a time: 16384 tokens, 16 states of 128 x 128, 16 segments 13 -> 9 us).
 constexpr int kScanThreads = 256;
 __global__ __launch_bounds__(kScanThreads) void decay_scan_kernel(const Args a) {
     const Role &r = a.role[blockIdx.z];
