@@ -884,7 +884,7 @@ extern "C" int sa_decay_attention(const void *q, long q_stride, const void *k, l
         SA_TRY(check_rows(what, "out", out, out_stride, H, dv, type));
         SA_REQUIRE(out != q && out != k && out != v, SA_ERR_INVALID, "%s: out must not be an input", what);
     }
-    SA_REQUIRE(sa::aligned16(log_decay) && sa::aligned16(state_in_or_null) && sa::aligned16(state_out_or_null) && sa::aligned16(workspace) &&
+    SA_REQUIRE(sa::aligned4(log_decay) && sa::aligned16(state_in_or_null) && sa::aligned16(state_out_or_null) && sa::aligned16(workspace) &&
                    sa::aligned4(offsets_or_null) && sa::aligned4(slots_or_null),
                SA_ERR_ALIGN, "%s: pointers must be 16-byte aligned", what);
     if (B == 0 || (T == 0 && state_out_or_null == nullptr)) return SA_OK;
@@ -939,7 +939,7 @@ extern "C" int sa_decay_attention_backward(const void *dout, long dout_stride, c
     }
     SA_REQUIRE(dstate_in_or_null == nullptr || (dstate_in_or_null != dstate_out_or_null && dstate_in_or_null != state_in_or_null), SA_ERR_INVALID,
                "%s: dstate_in must not be an input", what);
-    SA_REQUIRE(sa::aligned16(log_decay) && sa::aligned16(state_in_or_null) && sa::aligned16(dstate_out_or_null) && sa::aligned16(dstate_in_or_null) &&
+    SA_REQUIRE(sa::aligned4(log_decay) && sa::aligned16(state_in_or_null) && sa::aligned16(dstate_out_or_null) && sa::aligned16(dstate_in_or_null) &&
                    sa::aligned16(workspace) && sa::aligned4(offsets_or_null),
                SA_ERR_ALIGN, "%s: pointers must be 16-byte aligned", what);
     if (B == 0 || (T == 0 && dstate_in_or_null == nullptr)) return SA_OK;

@@ -44,8 +44,9 @@ def test_prompts(lib):      # noqa: F811
     for name in ("q", "k", "v"):
         assert call(out={"q": A, "k": B_, "v": C}[name]) == INVALID
     assert call(g=None) == INVALID
-    for name in ("g", "first", "last", "ws"):
+    for name in ("first", "last", "ws"):
         assert call(**{name: ODD}) == ALIGN, name
+    assert call(g=ODD) == HIP and call(g=0x1002) == ALIGN
     assert call(off=0x1002) == ALIGN and call(slots=0x1002, places=3) == ALIGN and call(off=ODD) == HIP
     need = lib.sa_decay_attention_workspace_bytes(4000, 1, 4, 2, 64, 72, 0)
     assert need > 0 and call(T=4000, B=1, bytes=need) == HIP and call(T=4000, B=1, bytes=need - 1) == WORKSPACE and call(T=4000, B=1, ws=None) == WORKSPACE
@@ -65,8 +66,9 @@ def test_steps(lib):      # noqa: F811
     refuses_heads(call, "B")
     refuses_rows(call, ("q", "k", "v", "out"))
     assert call(slots=FAKE, places=-1) == INVALID and call(out=A) == INVALID and call(out=B_) == INVALID and call(out=C) == INVALID
-    for name in ("g", "first", "last"):
+    for name in ("first", "last"):
         assert call(**{name: None}) == INVALID and call(**{name: ODD}) == ALIGN, name
+    assert call(g=None) == INVALID and call(g=ODD) == HIP and call(g=0x1002) == ALIGN
     assert call(slots=0x1002, places=3) == ALIGN and call(B=(1 << 31) - 1, Hk=4, H=4) == UNSUPPORTED
 
 
@@ -82,8 +84,9 @@ def test_backward(lib):      # noqa: F811
             assert call(**{name: other}) == INVALID, name
     assert call(dq=F) == INVALID and call(dk=G) == INVALID and call(dv_rows=E) == INVALID
     assert call(dfirst=0x100000) == INVALID and call(dfirst=0x200000) == INVALID and call(g=None) == INVALID
-    for name in ("g", "first", "dlast", "dfirst", "ws"):
+    for name in ("first", "dlast", "dfirst", "ws"):
         assert call(**{name: ODD}) == ALIGN, name
+    assert call(g=ODD) == HIP and call(g=0x1002) == ALIGN
     need = lib.sa_decay_attention_backward_workspace_bytes(4000, 1, 4, 2, 64, 72, 0)
     assert need > 0 and call(T=4000, B=1, bytes=need) == HIP and call(T=4000, B=1, bytes=need - 1) == WORKSPACE and call(T=4000, B=1, ws=None) == WORKSPACE
     none = dict(T=0, dout=None, q=None, k=None, v=None, dq=None, dk=None, dv_rows=None)

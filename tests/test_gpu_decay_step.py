@@ -109,3 +109,17 @@ def test_token_by_token_is_the_definition(sa):
         o, _ = sa.sa_decay_attention_step(s["q"][t:t + 1], s["k"][t:t + 1], s["v"][t:t + 1], s["log_decay"], 0.25, state)
         assert (o[0].double() - out[t]).abs().max().item() <= 64 * HALF_STEP[torch.float32] * 40      # sums of 16 products below 40
     assert (state[0].double() - last).abs().max().item() <= 32 * HALF_STEP[torch.float32] * 16
+
+
+def test_decays_of_one_layer(sa):
+    """A row of a table of decays, layer by layer, begins where it begins."""
+    H, d, n = 3, 64, 150
+    s = sequences([n, n], H, H, d, d, torch.bfloat16, seed=5, device="cuda")
+    table = s["log_decay"].repeat(4, 1)
+    q, k, v, do = (s[name].view(2, n, H, d) for name in ("q", "k", "v", "dout"))
+    for row in (1, 2, 3):
+        g, own = table[row], s["log_decay"]
+        for call in (lambda g: sa.sa_decay_attention(q, k, v, g, 0.1, want_state=True),
+                     lambda g: sa.sa_decay_attention_step(q[:, 0], k[:, 0], v[:, 0], g, 0.1, s["state_in"], state_out=torch.zeros_like(s["state_in"])),
+                     lambda g: sa.sa_decay_attention_backward(do, q, k, v, g, 0.1, want_dstate=True)):
+            assert all(torch.equal(a, b) for a, b in zip(call(g), call(own)))
