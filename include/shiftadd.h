@@ -146,10 +146,12 @@ int sa_linear_attention_01(const uint64_t *q_codes, const uint64_t *k_codes, con
  *   state_in_or_null, state_out_or_null fp32 [places, Hk, d, dv]: sequence b has place b, or, with slots_or_null int32 [B], place slots[b] of
  *   n_slots; a sequence whose slot is none of them begins with zeros and leaves no state.  The two may be the same memory; a slot may be
  *   named once only.  An empty sequence leaves the state it began with.
- * d and dv are multiples of 8, up to 128; B * Hk <= 65535.  Rows begin at multiples of 16 bytes.  Sums and states are fp32 in a fixed order (the
- * same call gives the same bits), q, k and v enter them exactly and out is rounded once.  An infinity or NaN in a token makes results
- * of its sequence NaN from 63 tokens before it on.  out may not overlap an input.
- * The workspace is as long as sequences and heads are too few to fill the GPU (the query returns 0 otherwise); offsets count as ragged.
+ * d and dv are multiples of 8, up to 128; H <= 4096, B * Hk <= 65535, T < 2^30, strides below 2^22 elements.  Rows and states begin at multiples of 16 bytes.
+ * Sums and states are fp32 in a fixed order (the same call gives the same bits), q, k and v enter them exactly and out is rounded once.  An infinity or NaN in a
+ * token (fp32: 3.39e38 and more, in the state too) may make results of its sequence and head NaN from 63 tokens before it on, and the state; no others.
+ * out may not overlap an input.
+ * Workspace: states of segments, where sequences and heads are too few to fill the GPU (else the query returns 0; it asks for what any of the types may need;
+ * ragged: whether there are offsets).  Its contents do not matter; it belongs to one call from its first launch to its last.
  */
 size_t sa_decay_attention_workspace_bytes(long T, int B, int H, int Hk, int d, int dv, int ragged);
 int sa_decay_attention(const void *q, long q_stride, const void *k, long k_stride, const void *v, long v_stride, int type,
@@ -168,7 +170,8 @@ int sa_decay_attention_step(const void *q, long q_stride, const void *k, long k_
  *   R_t = exp(log_decay) * R_{t+1} + scale * q_t dout_t^T   (summed over the heads that share a state; behind the last token: dstate_out or zeros)
  *   dq_t = scale * S_t dout_t,   dk_t = R_t v_t,   dv_t = R_t^T k_t,   dstate_in = exp(log_decay) * R_0
  * dq, dk, dv as q, k and v, of the same type; state_in_or_null as in the forward call (S is computed again), dstate_out_or_null and
- * dstate_in_or_null fp32 [B, Hk, d, dv].  No output may overlap an input or another output.  Sequences, types and sizes as above.
+ * dstate_in_or_null fp32 [B, Hk, d, dv].  No output may overlap an input or another output.  Sequences, types, sizes and workspace as above; an infinity or
+ * NaN in a token may make the gradients of q of its sequence and head NaN from 63 tokens before it on, those of k and v up to 63 tokens behind it.
  */
 size_t sa_decay_attention_backward_workspace_bytes(long T, int B, int H, int Hk, int d, int dv, int ragged);
 int sa_decay_attention_backward(const void *dout, long dout_stride, const void *q, long q_stride, const void *k, long k_stride,
