@@ -167,8 +167,9 @@ int sa_decay_attention_step(const void *q, long q_stride, const void *k, long k_
                             float *state_out, const int32_t *slots_or_null, int n_slots, void *out, long out_stride, void *stream);
 /*
  * The gradient of sa_decay_attention for constant decays, from dout (as out) and that of state_out:
- *   R_t = exp(log_decay) * R_{t+1} + scale * q_t dout_t^T   (summed over the heads that share a state; behind the last token: dstate_out or zeros)
- *   dq_t = scale * S_t dout_t,   dk_t = R_t v_t,   dv_t = R_t^T k_t,   dstate_in = exp(log_decay) * R_0
+ *   R_t = scale * q_t dout_t^T + exp(log_decay) * R_{t+1}   (summed over the heads that share a state), of the last token scale * q_t dout_t^T + dstate_out:
+ *   dstate_out (or zeros) meets the last token as it is, without a decay
+ *   dq_t = scale * S_t dout_t,   dk_t = R_t v_t,   dv_t = R_t^T k_t,   dstate_in = exp(log_decay) * R_0 (of an empty sequence dstate_out)
  * dq, dk, dv as q, k and v, of the same type; state_in_or_null as in the forward call (S is computed again), dstate_out_or_null and
  * dstate_in_or_null fp32 [B, Hk, d, dv].  No output may overlap an input or another output.  Sequences, types, sizes and workspace as above; an infinity or
  * NaN in a token may make the gradients of q of its sequence and head NaN from 63 tokens before it on, those of k and v up to 63 tokens behind it.

@@ -156,3 +156,30 @@ def test_what_is_not_finite_stays_in_its_head(sa, N, dtype):
         else:
             assert torch.equal(a[at + 64:], b[at + 64:])
         assert not a[at, 0].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,Hk", [(2, 2), (4, 2)])
+def test_the_recurrence_token_by_token(sa, H, Hk, dtype):
+    """R_t = scale q_t dout_t^T + e^g R_{t+1}, of the last token scale q_t dout_t^T + dstate_out: read literally, from the last token to the first, through
+    one pass of a chunk and a half; an empty sequence hands dstate_out on."""
+    lengths, d, dv, scale = [70, 0, 1], 32, 40, 0.3
+    s = sequences(lengths, H, Hk, d, dv, dtype, seed=21, device="cuda")
+    s["log_decay"] = torch.tensor([-0.7, -0.05], device="cuda")
+    got = sa.sa_decay_attention_backward(s["dout"], s["q"], s["k"], s["v"], s["log_decay"], scale, offsets=s["offsets"], state_in=s["state_in"],
+                                         dstate_out=s["dstate_out"], want_dstate=True)
+    fade = s["log_decay"].double().exp()[:, None, None]
+    q, do = (s[n].double().view(-1, Hk, H // Hk, s[n].shape[-1]) for n in ("q", "dout"))
+    k, v = s["k"].double(), s["v"].double()
+    dk, dv_rows, dstate = torch.empty_like(k), torch.empty_like(v), s["dstate_out"].double().clone()
+    first = s["offsets"].tolist()
+    for b, n in enumerate(lengths):
+        for t in reversed(range(first[b], first[b] + n)):
+            behind = dstate[b] if t == first[b] + n - 1 else fade * dstate[b]
+            dstate[b] = behind + scale * (q[t].unsqueeze(-1) * do[t].unsqueeze(-2)).sum(1)
+            dk[t] = (dstate[b] * v[t].unsqueeze(-2)).sum(-1)
+            dv_rows[t] = (dstate[b] * k[t].unsqueeze(-1)).sum(-2)
+        if n:
+            dstate[b] *= fade
+    for name, g, want in zip(("dk", "dv", "dstate_in"), got[1:], (dk, dv_rows, dstate)):
+        check(name, g, want, s, scale, dtype, lengths)
