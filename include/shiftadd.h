@@ -161,6 +161,7 @@ int sa_decay_attention(const void *q, long q_stride, const void *k, long k_strid
 /*
  * The same for one token of each of B sequences: the step of a decoder.  q [B, H, d], k [B, Hk, d], v [B, Hk, dv], out [B, H, dv] with a row's
  * stride each, states and slots as above, both states needed (in place where they are the same memory).  Other slots' states are not touched.
+ * B * Hk < 2^24, with dv > 64 below 2^23.
  */
 int sa_decay_attention_step(const void *q, long q_stride, const void *k, long k_stride, const void *v, long v_stride, int type,
                             const float *log_decay, long B, int H, int Hk, int d, int dv, float scale, const float *state_in,

@@ -128,6 +128,7 @@ extern "C" int sa_decay_attention_step(const void *q, long q_stride, const void 
                "%s: pointers must be 16-byte aligned", what);
     StepArgs a{{q, q_stride, d}, {k, k_stride, d}, {v, v_stride, dv}, {out, out_stride, dv}, log_decay, Hk, H / Hk, dv > 64 ? 2 : 1, scale,
                state_in, state_out, slots_or_null, n_slots};
-    SA_REQUIRE(B * Hk * a.blocks < (1L << 31), SA_ERR_UNSUPPORTED, "%s: too many states for one launch", what);
+    // (a launch has less than 2^32 threads)
+    SA_REQUIRE(B * Hk * a.blocks * kStepThreads < (1L << 32), SA_ERR_UNSUPPORTED, "%s: too many states for one launch", what);
     return by_type(type, [&](auto t) { return launch_step<decltype(t)>(a, B, sa::as_stream(stream)); });
 }

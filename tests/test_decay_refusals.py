@@ -72,6 +72,15 @@ def test_steps(lib):      # noqa: F811
     assert call(slots=0x1002, places=3) == ALIGN and call(B=(1 << 31) - 1, Hk=4, H=4) == UNSUPPORTED
 
 
+@pytest.mark.parametrize("dv,states", [(64, 1 << 24), (72, 1 << 23)])
+def test_steps_of_more_threads_than_a_launch_has(lib, dv, states):      # noqa: F811
+    """256 threads to 64 columns of a state, and less than 2^32 of them: more states are refused before the launch."""
+    call = caller(lib.sa_decay_attention_step, dict(
+        q=A, qs=1024, k=B_, ks=1024, v=C, vs=1024, type=1, g=FAKE, B=6, H=4, Hk=4, d=8, dv=dv, scale=0.1, first=D, last=E, slots=None, places=0, out=F, os=1024,
+        stream=None))
+    assert call(B=states // 4 - 1) == HIP and call(B=states // 4) == UNSUPPORTED
+
+
 def test_backward(lib):      # noqa: F811
     call = caller(lib.sa_decay_attention_backward, dict(
         dout=A, os=1024, q=B_, qs=1024, k=C, ks=1024, v=D, vs=1024, type=1, g=FAKE, T=96, B=2, off=None, H=4, Hk=2, d=64, dv=72, scale=0.1, first=0x100000,
