@@ -736,16 +736,18 @@ Load load_of(int type, std::initializer_list<std::pair<int, int>> roles) {      
     return l;
 }
 
+constexpr long kThreads = 1L << 32;      // a launch has less
+
 // Segments where sequences and states alone leave CUs without work, as many as fill them once, or where one long sequence among short ones would go on
 // alone.
-Plan make_plan(long T, int B, int Hk, const Load &l, bool ragged, bool states) {
+Plan make_plan(long T, int B, int H, int Hk, const Load &l, bool ragged, bool states) {
     Plan p;
     if (T == 0 || B == 0) return p;
     const long mean = (T + B - 1) / B, groups = (long)B * Hk * l.workgroups, longest = ragged ? T : T / B;
     const long kLeast = ragged ? 256 : 128;
     constexpr long kRagged = 4, kShort = 512;
     long seg = 0;
-    if (!states && longest <= kShort && groups < l.fill) {
+    if (!states && longest <= kShort && groups < l.fill && (T / kChunk + B + 8) * H * l.workgroups * 512 < kThreads) {
         p.shorts = true;
         seg = kChunk;
     } else if ((2 * groups <= l.fill || ragged) && longest > kLeast) {
@@ -813,7 +815,7 @@ int by_forms(const char *what, int type, const Args &a, int roles, bool shorts, 
         }
         const long total = xcd_blocks(a.seq.units(), (long)shares * a.Hk);
         some.units = (uint32_t)a.seq.units();
-        SA_REQUIRE(total < (1L << 31), SA_ERR_UNSUPPORTED, "%s: too many heads and tokens for one launch", what);
+        SA_REQUIRE(total * 256 * f.halves < kThreads, SA_ERR_UNSUPPORTED, "%s: too many heads and tokens for one launch", what);
         SA_TRY(by_form(type, f, [&](auto shape) {
             run(shape, dim3((unsigned)total), some);
             return check_launch(what);
@@ -863,7 +865,7 @@ extern "C" size_t sa_decay_attention_workspace_bytes(long T, int B, int H, int H
     if (check_sequences("", SA_F32, T, B, ragged != 0, H, Hk, d, dv) != SA_OK) return 0;
     size_t most = 0;
     for (const int type : {SA_F32, SA_F16, SA_BF16})
-        most = std::max(most, plan_bytes(make_plan(T, B, Hk, load_of(type, {{d, dv}}), ragged != 0, true), T, B, ragged != 0, Hk, d, dv));
+        most = std::max(most, plan_bytes(make_plan(T, B, H, Hk, load_of(type, {{d, dv}}), ragged != 0, true), T, B, ragged != 0, Hk, d, dv));
     return most;
 }
 
@@ -888,7 +890,7 @@ extern "C" int sa_decay_attention(const void *q, long q_stride, const void *k, l
                    sa::aligned4(offsets_or_null) && sa::aligned4(slots_or_null),
                SA_ERR_ALIGN, "%s: pointers must be 16-byte aligned", what);
     if (B == 0 || (T == 0 && state_out_or_null == nullptr)) return SA_OK;
-    const Plan p = make_plan(T, B, Hk, load_of(type, {{d, dv}}), ragged, state_in_or_null != nullptr || state_out_or_null != nullptr);
+    const Plan p = make_plan(T, B, H, Hk, load_of(type, {{d, dv}}), ragged, state_in_or_null != nullptr || state_out_or_null != nullptr);
     const size_t need = plan_bytes(p, T, B, ragged, Hk, d, dv);
     SA_REQUIRE(need == 0 || (workspace != nullptr && workspace_bytes >= need), SA_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", what,
                need, workspace_bytes);
@@ -909,7 +911,7 @@ extern "C" size_t sa_decay_attention_backward_workspace_bytes(long T, int B, int
     if (check_sequences("", SA_F32, T, B, ragged != 0, H, Hk, d, dv) != SA_OK) return 0;
     size_t most = 0;
     for (const int type : {SA_F32, SA_F16, SA_BF16})
-        most = std::max(most, plan_bytes(make_plan(T, B, Hk, load_of(type, {{d, dv}, {dv, d}, {dv, d}}), ragged != 0, true), T, B, ragged != 0, Hk, d, dv));
+        most = std::max(most, plan_bytes(make_plan(T, B, H, Hk, load_of(type, {{d, dv}, {dv, d}, {dv, d}}), ragged != 0, true), T, B, ragged != 0, Hk, d, dv));
     return 2 * most;
 }
 
@@ -943,7 +945,7 @@ extern "C" int sa_decay_attention_backward(const void *dout, long dout_stride, c
                    sa::aligned16(workspace) && sa::aligned4(offsets_or_null),
                SA_ERR_ALIGN, "%s: pointers must be 16-byte aligned", what);
     if (B == 0 || (T == 0 && dstate_in_or_null == nullptr)) return SA_OK;
-    const Plan p = make_plan(T, B, Hk, load_of(type, {{d, dv}, {dv, d}, {dv, d}}), ragged, state_in_or_null != nullptr || dstate_out_or_null != nullptr || dstate_in_or_null != nullptr);
+    const Plan p = make_plan(T, B, H, Hk, load_of(type, {{d, dv}, {dv, d}, {dv, d}}), ragged, state_in_or_null != nullptr || dstate_out_or_null != nullptr || dstate_in_or_null != nullptr);
     const size_t each = plan_bytes(p, T, B, ragged, Hk, d, dv);
     SA_REQUIRE(each == 0 || (workspace != nullptr && workspace_bytes >= 2 * each), SA_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given",
                what, 2 * each, workspace_bytes);

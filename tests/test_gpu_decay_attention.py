@@ -176,3 +176,20 @@ def test_no_tokens(sa):
     four = torch.empty(2, 0, 2, 64, device="cuda")
     o, last = sa.sa_decay_attention(four, four, four, g, 1.0, state_in=state[:2].clone(), want_state=True)
     assert o.shape == four.shape and torch.equal(last, state[:2])
+
+
+def test_more_heads_and_short_sequences_than_a_launch_has_threads_for(sa):
+    """4096 heads of a single key/value head over 512 sequences of 512 tokens: 64 queries to a workgroup would be 2^24 workgroups of 256 threads."""
+    B, N, H, d = 512, 512, 4096, 8
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("40 GB are needed")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q = torch.empty(B, N, H, d, dtype=torch.float16, device="cuda").normal_(generator=g)
+    k, v = (torch.randn(B, N, 1, d, generator=g, device="cuda").half() for _ in range(2))
+    log_decay = torch.tensor([-0.1], device="cuda")
+    out, _ = sa.sa_decay_attention(q, k, v, log_decay, 0.3)
+    for b in (0, B - 1):
+        for heads in (slice(0, 2), slice(H - 2, H)):
+            s = dict(q=q[b, :, heads], k=k[b], v=v[b], dout=out[b, :, heads], log_decay=log_decay, state_in=torch.zeros(1, 1, d, d, device="cuda"),
+                     offsets=torch.tensor([0, N], dtype=torch.int32))
+            check("out", out[b, :, heads], reference(s, 0.3, [N], state=False)["out"], s, 0.3, torch.float16, [N], False)
