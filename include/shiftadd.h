@@ -147,7 +147,9 @@ int sa_linear_attention_01(const uint64_t *q_codes, const uint64_t *k_codes, con
  *   n_slots; a sequence whose slot is none of them begins with zeros and leaves no state.  The two may be the same memory; a slot may be
  *   named once only.  An empty sequence leaves the state it began with.
  * d and dv are multiples of 8, up to 128; H <= 4096, B * Hk <= 65535, T < 2^30, strides below 2^22 elements.  Rows and states begin at multiples of 16 bytes.
- * Sums and states are fp32 in a fixed order (the same call gives the same bits), q, k and v enter them exactly and out is rounded once.  An infinity or NaN in a
+ * Sums and states are fp32 in a fixed order (the same call gives the same bits), q, k and v enter them exactly (fp16 below 2^-14, its subnormal numbers:
+ * to 2^-38) and out is rounded once.  What rows of 16 bits are made of on the way, the products q k of a token and the state that it meets, enters them in more bits than
+ * they have: bf16 to 2^-17 of each value; fp16 to 2^-22 of it, but no finer than 2^-39 of the largest of the token's products in its 64 tokens or of the state's column.  An infinity or NaN in a
  * token (fp32: 3.39e38 and more, in the state too) may make results of its sequence and head NaN from 63 tokens before it on, and the state; no others.
  * out may not overlap an input.
  * Workspace: states of segments, where sequences and heads are too few to fill the GPU (else the query returns 0; it asks for what any of the types may need;

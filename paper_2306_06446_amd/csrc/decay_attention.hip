@@ -217,8 +217,10 @@ struct State {
     }
     // S = carry S + sum_j weight[j] k_j v_j^T over the chunk in LDS.  Both operands have tokens for the places of the sum: transposed
     // reads, in the order 32 s + 16 (e / 4) + 4 (l / 16) + e % 4 for element e.
-    // TERMS: of what is added to the state.
-    template <int TERMS>
+    // TERMS: of what is added to the state.  WHOLE (fp16): for a state in memory, whose elements have fp32's precision of what they are made of, small values
+    // alone where the large ones' keys are zero.  Two terms behind one power of two hold 22 bits of what is above 2^-18 of the column's largest; what is
+    // below is looked at, and has turns of its own if it matters (50021 tokens in 37 sequences, 4 of 96 x 72: sums 33 -> 38 us; heads of fast decay look).
+    template <int TERMS, bool WHOLE>
     __device__ inline void update(const E (*kl)[kChunk][P::KP], const E (*vl)[kChunk][P::VP], const float *weight, float carry) {
         const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15, w = (int)threadIdx.x >> 6, row = 4 * g + (i >> 2), col = 4 * (i & 3);
         auto decayed = [&](auto ks, float (&x)[8]) {
@@ -239,22 +241,58 @@ struct State {
             });
         };
         if constexpr (P::SCALED) {
-            float x0[8], x1[8];
-            decayed(std::integral_constant<int, 0>(), x0);
-            decayed(std::integral_constant<int, 1>(), x1);
-            const Scale scale(column_max(largest(x1, largest(x0))));
-            Vec<E, 8> b[2][TERMS];
-            split(x0, b[0], scale.up);
-            split(x1, b[1], scale.up);
-            each<P::TILES>([&](auto t) {
-                f4 add = zeros();
-                each<2>([&](auto ks) {
-                    Vec<E, 8> a[P::RAW];
-                    keys(ks, t, a);
-                    product<Terms<typename P::T>::ORDER_ADDED>(add, a, b[ks]);
+            float below = __builtin_inff();
+            bool more = false;       // turns, each of the values that hold their bits behind its power of two
+            do {
+                float x0[8], x1[8];
+                decayed(std::integral_constant<int, 0>(), x0);
+                decayed(std::integral_constant<int, 1>(), x1);
+                // (the first turn has what is not finite, too)
+                if (more) each<8>([&](auto e) { x0[e] = fabsf(x0[e]) >= below ? 0.0f : x0[e], x1[e] = fabsf(x1[e]) >= below ? 0.0f : x1[e]; });
+                const float top = column_max(largest(x1, largest(x0)));
+                const Scale scale(top);
+                const float kept = more ? 1.0f : carry;
+                below = scale.down > 0x1p-126f ? 0.125f * scale.down : 0.0f;          // (behind the last power of two nothing is left)
+                const bool some = WHOLE && __any(least(x1, least(x0)) < __builtin_bit_cast(uint32_t, below) << 1);
+                // What is below 2^-18 of the largest would be off by 2^-25 scale.down.  That matters where this, times the keys' magnitudes, is above 2^-19 of
+                // what all is together: where sum |k| (1 - 64 |x| scale.up) is positive, the large values' keys (next to) zero.
+                if (some && !more) {
+                    float most = 0.0f;
+                    Vec<E, 8> sign[2];
+                    each<8>([&](auto e) {
+                        sign[0][(int)e] = (E)(1.0f - fminf(fabsf(x0[e]) * scale.up * 64.0f, 0x1p14f));
+                        sign[1][(int)e] = (E)(1.0f - fminf(fabsf(x1[e]) * scale.up * 64.0f, 0x1p14f));
+                    });
+                    each<P::TILES>([&](auto t) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        f4 sum = zeros();
+                        each<2>([&](auto ks) {
+                            Vec<E, 8> a[P::RAW];
+                            keys(ks, t, a);
+                            const u4 size = __builtin_bit_cast(u4, a[0]) & 0x7fff7fffu;
+                            sum = matrix(__builtin_bit_cast(Vec<E, 8>, size), sign[ks], sum);
+                        });
+                        each<4>([&](auto e) { most = fmaxf(most, sum[(int)e]); });
+                    });
+                    __builtin_amdgcn_sched_barrier(0);
+                    more = __any(top > 0.0f && most > 0.0f);          // (not in a column of zeros, as those behind the last are)
+                } else {
+                    more = some;
+                }
+                if (more) each<8>([&](auto e) { x0[e] = fabsf(x0[e]) < below ? 0.0f : x0[e], x1[e] = fabsf(x1[e]) < below ? 0.0f : x1[e]; });
+                Vec<E, 8> b[2][TERMS];
+                split(x0, b[0], scale.up);
+                split(x1, b[1], scale.up);
+                each<P::TILES>([&](auto t) {
+                    f4 add = zeros();
+                    each<2>([&](auto ks) {
+                        Vec<E, 8> a[P::RAW];
+                        keys(ks, t, a);
+                        product<Terms<typename P::T>::ORDER_ADDED>(add, a, b[ks]);
+                    });
+                    each<4>([&](auto e) { s[t][(int)e] = __builtin_fmaf(add[(int)e], scale.down, s[t][(int)e] * kept); });
                 });
-                each<4>([&](auto e) { s[t][(int)e] = __builtin_fmaf(add[(int)e], scale.down, s[t][(int)e] * carry); });
-            });
+            } while (more);
         } else {
             each<P::TILES>([&](auto t) { s[t] *= carry; });
             each<2>([&](auto ks) {
@@ -413,7 +451,8 @@ constexpr int rows_waves() {
 // Rows of the result.  A workgroup has one segment, the heads of one state (their keys, values and state are in LDS once for all of them: 12 heads of 96
 // over 4 of 72 250 -> 203 us) and a slice of the columns and goes through the chunks one after the other;
 // of each half of the slice, wavefront w has queries 16 w to 16 w + 15 of a chunk, and columns 16 w to 16 w + 15 of the state.
-template <class P, bool STREAM>
+// LAST: a role leaves its last state (of fp16 another kernel: a loop in it keeps loads from their places, rows of the ragged batch's gradient 114 -> 128 us).
+template <class P, bool STREAM, bool LAST>
 __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kernel(const Args a) {
     typedef typename P::T T;
     typedef typename P::E E;
@@ -536,8 +575,8 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
             } while (++u < outs);
             // (a state that only rows in 16 bits are made of takes the terms that these do)
             if (add) {
-                if (P::MADE == P::ADDED || last != nullptr) state.template update<P::ADDED>(kl, vl, weight, h == 0 ? carry : 1.0f);
-                else state.template update<P::MADE>(kl, vl, weight, h == 0 ? carry : 1.0f);
+                if (P::MADE == P::ADDED || last != nullptr) state.template update<P::ADDED, P::SCALED && LAST>(kl, vl, weight, h == 0 ? carry : 1.0f);
+                else state.template update<P::MADE, false>(kl, vl, weight, h == 0 ? carry : 1.0f);
             }
         } while (++h < sums);
         ot.base += (uint64_t)ot.next;
@@ -613,7 +652,7 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_short_ker
 }
 
 // What each segment adds to the state, from a state of zeros.  The chunks' keys and values pass through LDS for the transposed reads alone.
-template <class P>
+template <class P, bool LAST>
 __global__ __launch_bounds__(P::THREADS) void decay_states_kernel(const Args a) {
     typedef typename P::T T;
     typedef typename P::E E;
@@ -658,8 +697,8 @@ __global__ __launch_bounds__(P::THREADS) void decay_states_kernel(const Args a) 
             vt.base += end ? (uint64_t)vt.next - (uint64_t)(sums - 1) * vmore : vmore;
             rows.load(kt, vt, !end ? n : c + 1 < chunks ? in_chunk(c + 1) : 0);
             __syncthreads();
-            if (P::MADE == P::ADDED || r.last != nullptr) state.template update<P::ADDED>(kl, vl, weight, h == 0 ? carry : 1.0f);
-            else state.template update<P::MADE>(kl, vl, weight, h == 0 ? carry : 1.0f);
+            if (P::MADE == P::ADDED || r.last != nullptr) state.template update<P::ADDED, P::SCALED && LAST>(kl, vl, weight, h == 0 ? carry : 1.0f);
+            else state.template update<P::MADE, false>(kl, vl, weight, h == 0 ? carry : 1.0f);
         }
     }
     state.store(a.place(r.sums_out, sp.unit, hk), r.transposed, kwidth, vwidth, a.dv, c0);
@@ -824,6 +863,19 @@ int by_forms(const char *what, int type, const Args &a, int roles, bool shorts, 
     return SA_OK;
 }
 
+bool leaves_states(const Args &a) {
+    for (int r = 0; r < a.roles; ++r)
+        if (a.role[r].last != nullptr) return true;
+    return false;
+}
+
+// f with the flag as a constant, where there are two kernels for it.
+template <bool TWO, class F>
+void by_flag(bool flag, F f) {
+    if (TWO && !flag) f(std::integral_constant<bool, !TWO>());
+    else f(std::true_type());
+}
+
 // The rows of all roles; before them, where there are segments, the sums of the first `states` roles and their scan.
 int launch(const char *what, int type, Args a, const Plan &p, int states, hipStream_t st) {
     if (a.seq.units() == 0) return SA_OK;
@@ -834,7 +886,8 @@ int launch(const char *what, int type, Args a, const Plan &p, int states, hipStr
     }
     if (p.seg > 0) {
         SA_TRY(by_forms(what, type, a, states, false, [&](auto shape, dim3 grid, const Args &some) {
-            decay_states_kernel<decltype(shape)><<<grid, dim3(decltype(shape)::THREADS), 0, st>>>(some);
+            typedef decltype(shape) S;
+            by_flag<S::SCALED>(leaves_states(some), [&](auto last) { decay_states_kernel<S, last><<<grid, dim3(S::THREADS), 0, st>>>(some); });
         }));
         const dim3 grid((unsigned)((a.state / 4 + kScanThreads - 1) / kScanThreads), (unsigned)(a.Hk * a.seq.B), (unsigned)states);
         decay_scan_kernel<<<grid, dim3(kScanThreads), 0, st>>>(a);
@@ -845,8 +898,10 @@ int launch(const char *what, int type, Args a, const Plan &p, int states, hipStr
         typedef decltype(shape) S;
         bool lines = true;
         for (int r = 0; r < some.roles; ++r) lines = lines && some.role[r].out.width * sizeof(typename S::T) % 128 == 0;
-        if (lines) decay_rows_kernel<S, true><<<grid, dim3(S::THREADS), 0, st>>>(some);
-        else decay_rows_kernel<S, false><<<grid, dim3(S::THREADS), 0, st>>>(some);
+        by_flag<S::SCALED>(leaves_states(some), [&](auto last) {
+            if (lines) decay_rows_kernel<S, true, last><<<grid, dim3(S::THREADS), 0, st>>>(some);
+            else decay_rows_kernel<S, false, last><<<grid, dim3(S::THREADS), 0, st>>>(some);
+        });
     });
 }
 

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from decay_forms import check, reference, sequences
+from decay_forms import allowed, check, reference, sequences
 
 pytestmark = pytest.mark.gpu
 TYPES = [torch.float32, torch.float16, torch.bfloat16]
@@ -193,3 +193,51 @@ def test_more_heads_and_short_sequences_than_a_launch_has_threads_for(sa):
             s = dict(q=q[b, :, heads], k=k[b], v=v[b], dout=out[b, :, heads], log_decay=log_decay, state_in=torch.zeros(1, 1, d, d, device="cuda"),
                      offsets=torch.tensor([0, N], dtype=torch.int32))
             check("out", out[b, :, heads], reference(s, 0.3, [N], state=False)["out"], s, 0.3, torch.float16, [N], False)
+
+
+def spread(lengths, H, Hk, d, dv, seed, names):
+    """fp16 rows whose values span the type: every 7th token large, all others down to subnormals, and of each large token every other element of the
+    left operand (names[0]) zero: what those elements meet are small values alone."""
+    s = sequences(lengths, H, Hk, d, dv, torch.float16, seed=seed)
+    g = torch.Generator().manual_seed(seed + 1)
+    left, right = (s[n] for n in names)
+    T = right.shape[0]
+    right *= (2.0 ** -torch.randint(0, 22, (T, 1, right.shape[-1]), generator=g)).half()
+    large = torch.arange(T) % 7 == 3
+    right[large] = (right[large].sign() * (2e4 + 4e4 * torch.rand(right[large].shape, generator=g))).half()
+    left[large, :, ::2] = 0
+    left[~large] *= (2.0 ** -torch.randint(0, 20, (T, 1, 1), generator=g)[~large]).half()
+    s["log_decay"] = torch.tensor([-0.002, -0.9, -3.0, 0.0][:Hk])
+    return {n: t.cuda() for n, t in s.items()}
+
+
+def subnormal(s, left, right, scale, lengths, gradient=False):
+    """What fp16's subnormal numbers add to what a state may be off by.  The matrix cores cut a sum of 32 products and what is there before 24 bits below the largest
+    product's exponent, to which a subnormal operand counts as one of exponent -14: a product of such a left operand and x costs each of the 33 less
+    than 2^-24 2^-14 |x|, and x's second term 2^-11 of that: in all less than 34 2^-38 |x| into the state, which that chunk's sum is added to in fp32."""
+    t = dict(s, **{left: ((s[left] != 0) & (s[left].abs() < 2.0 ** -14)).double(), right: s[right].abs()})
+    zero = torch.zeros_like(s["state_in"])
+    r = reference(dict(t, state_in=zero, dstate_out=zero), scale, lengths, gradients=gradient)
+    return 34 * 2.0 ** -38 * r["dstate_in" if gradient else "state_out"]
+
+
+@pytest.mark.parametrize("H,Hk,d,dv", [(4, 4, 64, 64), (4, 2, 32, 40), (2, 2, 96, 72), (2, 2, 128, 128), (2, 1, 128, 64)])
+@pytest.mark.parametrize("lengths", [[150, 1, 64], [900, 70]], ids=lambda l: "-".join(map(str, l)))
+def test_states_hold_small_values_beside_large_ones(sa, lengths, H, Hk, d, dv):
+    """fp16: an element of a state has fp32's precision of what it is made of, however large the values are whose keys are zero there."""
+    def right(kind, got, want, s, more):
+        slack, half = allowed(kind, s, 0.1, torch.float16, lengths)
+        assert got.isfinite().all()
+        assert bool(((got.double() - want).abs() <= slack + more + (want.abs() + slack) * half + 2.0 ** -133).all())
+
+    s = spread(lengths, H, Hk, d, dv, sum(lengths) + d, ("k", "v"))
+    s["state_in"].zero_()
+    o, last = run(sa, s, 0.1)
+    right("state_out", last, reference(s, 0.1, lengths)["state_out"], s, subnormal(s, "k", "v", 0.1, lengths))
+    s = spread(lengths, H, Hk, d, dv, sum(lengths) + d + 5, ("q", "dout"))
+    s["dstate_out"].zero_()
+    got = sa.sa_decay_attention_backward(s["dout"], s["q"], s["k"], s["v"], s["log_decay"], 0.1, offsets=s["offsets"], dstate_out=s["dstate_out"],
+                                         want_dstate=True)
+    s["state_in"].zero_()
+    want = reference(s, 0.1, lengths, gradients=True)["dstate_in"]
+    right("dstate_in", got[3], want, s, subnormal(s, "q", "dout", 0.1, lengths, True))
