@@ -152,8 +152,9 @@ int sa_linear_attention_01(const uint64_t *q_codes, const uint64_t *k_codes, con
  * they have: bf16 to 2^-17 of each value; fp16 to 2^-22 of it, but no finer than 2^-39 of the largest of the token's products in its 64 tokens or of the state's column.  An infinity or NaN in a
  * token (fp32: 3.39e38 and more, in the state too) may make results of its sequence and head NaN from 63 tokens before it on, and the state; no others.
  * out may not overlap an input.
- * Workspace: states of segments, where sequences and heads are too few to fill the GPU (else the query returns 0; it asks for what any of the types may need;
- * ragged: whether there are offsets).  Its contents do not matter; it belongs to one call from its first launch to its last.
+ * Workspace: states of segments of sequences that are cut: of equal ones where sequences and heads are too few to fill the GPU, of a ragged batch (offsets are
+ * not known to the host) those that are longer than a segment, 256 tokens at least.  The query returns 0 where none can be; it asks for what any of
+ * the types may need; ragged: whether there are offsets.  Its contents do not matter; it belongs to one call from its first launch to its last.
  */
 size_t sa_decay_attention_workspace_bytes(long T, int B, int H, int Hk, int d, int dv, int ragged);
 int sa_decay_attention(const void *q, long q_stride, const void *k, long k_stride, const void *v, long v_stride, int type,

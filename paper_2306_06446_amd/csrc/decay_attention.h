@@ -184,7 +184,8 @@ struct HeadRows {
 // One segment of a sequence: position i of the recurrence is token begin + i (or begin + length - 1 - i, where time is reversed), the segment has
 // those from seg segments on.
 struct Span {
-    int seq, unit, seg;      // (unit: the segment's place in the workspace)
+    int seq, seg;
+    int place;               // the segment's state in the workspace
     int begin, length;       // of the whole sequence
 };
 
@@ -192,11 +193,15 @@ struct Span {
 // multiple of kChunk.  Sequence b's first segment is unit first_unit(b): segments of equal sequences follow each other, in a ragged batch
 // (whose segments are powers of two) there is a place for each full segment of all tokens and one more for each sequence, which is enough: a
 // sequence from a seg + r to c seg + s has at most c - a + 1 segments.
+// The states of segments are at their units; where segments are longer than most sequences (`whole`), only sequences of several segments have any, and the
+// first place is 2 a, which is enough, too: c is a + 1 at least, and the last place a + c below 2 c, the next such sequence's first.
 struct Sequences {
     const int32_t *offsets;  // or null
     int T, B, each;
     int seg, log_seg;
     int per_sequence;        // units of a sequence of an equal batch
+    bool whole;
+    __device__ inline bool cut(int length) const { return !whole || length > seg; }
     __host__ __device__ inline long units() const { return offsets != nullptr ? (long)(T >> log_seg) + B : (long)per_sequence * B; }
     __device__ inline int offset(int b) const {
         const int at = offsets[b];
@@ -206,12 +211,12 @@ struct Sequences {
         Span s;
         s.seq = b, s.seg = 0;
         if (offsets == nullptr) {
-            s.begin = each * b, s.length = each, s.unit = per_sequence * b;
+            s.begin = each * b, s.length = each, s.place = per_sequence * b;
         } else {
             s.begin = __builtin_amdgcn_readfirstlane(offset(b));
             const int end = __builtin_amdgcn_readfirstlane(offset(b + 1));
             s.length = end > s.begin ? end - s.begin : 0;
-            s.unit = (s.begin >> log_seg) + b;
+            s.place = whole ? 2 * (s.begin >> log_seg) : (s.begin >> log_seg) + b;
         }
         return s;
     }
@@ -219,8 +224,8 @@ struct Sequences {
     __device__ inline Span of_unit(uint32_t u) const {
         if (offsets == nullptr) {
             Span s = of_sequence(per_sequence == 1 ? (int)u : (int)(u / (uint32_t)per_sequence));
-            s.seg = (int)u - s.unit;
-            s.unit = (int)u;
+            s.seg = (int)u - s.place;
+            s.place = (int)u;
             return s;
         }
         int b = 0, n = B, at, last;
@@ -239,7 +244,7 @@ struct Sequences {
         const int end = last < 63 ? __builtin_amdgcn_readlane(at, last + 1) : __builtin_amdgcn_readfirstlane(offset(s.seq + 1));
         s.length = end > s.begin ? end - s.begin : 0;
         s.seg = (int)u - ((s.begin >> log_seg) + s.seq);
-        s.unit = (int)u;
+        s.place = whole ? 2 * (s.begin >> log_seg) + s.seg : (int)u;
         return s;
     }
 };

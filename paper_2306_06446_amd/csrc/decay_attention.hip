@@ -42,8 +42,8 @@ struct Role {
     float inside, into, update;          // factors of (q k) v, of q S, of what is added to the state
     const float *first;      // [places][Hk][d][dv] or null: the state before the sequence
     float *last;             // or null: the state behind it
-    const float *starts;     // or null: [units][Hk][d][dv], the state before each segment
-    float *sums_out;         // (states kernel) [units][Hk][d][dv]: what a segment adds to the state
+    const float *starts;     // or null: [places of the workspace][Hk][d][dv], the state before each segment
+    float *sums_out;         // (states kernel) the same: what a segment adds to the state
 };
 
 struct Args {
@@ -470,12 +470,13 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
     const bool transposed = r.transposed, reverse = r.reverse;
     const int c0 = (int)item * P::COLS;
     State<P> state;
-    const bool segments = r.starts != nullptr;       // (asked for first: it takes nothing but the segment's number to find it)
-    if (segments) state.load(a.place(r.starts, (int)unit, hk), transposed, kwidth, vwidth, a.dv, c0);
+    const bool early = r.starts != nullptr && !a.seq.whole;       // (asked for first: it takes nothing but the segment's number to find it)
+    if (early) state.load(a.place(r.starts, (int)unit, hk), transposed, kwidth, vwidth, a.dv, c0);
     else state.clear();
     const Span sp = a.seq.of_unit(unit);
     const int p0 = sp.seg * a.seq.seg, left = sp.length - p0;
     if (sp.seg < 0 || (left <= 0 && (sp.seg > 0 || r.last == nullptr))) return;
+    const bool segments = r.starts != nullptr && a.seq.cut(sp.length);
     const int tokens = left < a.seq.seg ? left : a.seq.seg;
 
     const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -496,9 +497,9 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
     Queries<P> q;
 
     const int place = r.first != nullptr || r.last != nullptr ? state_place(a, sp.seq) : -1;
-    float *const last = r.last != nullptr && place >= 0 ? a.place(r.last, place, hk) : nullptr;
+    float *const last = r.last != nullptr && !segments && place >= 0 ? a.place(r.last, place, hk) : nullptr;
     bool live = segments || (r.first != nullptr && place >= 0);      // a state that is not zero
-    if (live && !segments) state.load(a.place(r.first, place, hk), transposed, kwidth, vwidth, a.dv, c0);
+    if (live && !early) state.load(segments ? a.place(r.starts, sp.place, hk) : a.place(r.first, place, hk), transposed, kwidth, vwidth, a.dv, c0);
 
     // Loads and stores come back in the order in which they left, and the compiler counts those behind the one it waits for, the fewest that may be there
     // on any way to that place.  So every turn of the loop asks for as many rows and queries and stores as many, and what is
@@ -669,7 +670,7 @@ __global__ __launch_bounds__(P::THREADS) void decay_states_kernel(const Args a) 
     const Span sp = a.seq.of_unit(unit);
     const int p0 = sp.seg * a.seq.seg, left = sp.length - p0;
     // the last segment's sum is for the state behind the sequence only
-    if (sp.seg < 0 || left <= 0 || (left <= a.seq.seg && r.last == nullptr)) return;
+    if (sp.seg < 0 || left <= 0 || (left <= a.seq.seg && r.last == nullptr) || !a.seq.cut(sp.length)) return;
     const int tokens = left < a.seq.seg ? left : a.seq.seg, chunks = (tokens + kChunk - 1) / kChunk;
     const float rate = uniform(decay_rate(a.g[hk]));
     State<P> state;
@@ -701,7 +702,7 @@ __global__ __launch_bounds__(P::THREADS) void decay_states_kernel(const Args a) 
             else state.template update<P::MADE, false>(kl, vl, weight, h == 0 ? carry : 1.0f);
         }
     }
-    state.store(a.place(r.sums_out, sp.unit, hk), r.transposed, kwidth, vwidth, a.dv, c0);
+    state.store(a.place(r.sums_out, sp.place, hk), r.transposed, kwidth, vwidth, a.dv, c0);
 }
 
 // From the segments' sums to the states before them, in their place, and to the state behind the sequence.  A thread has 4 elements, 16 segments of them
@@ -713,12 +714,13 @@ __global__ __launch_bounds__(kScanThreads) void decay_scan_kernel(const Args a) 
     const int at = (int)(blockIdx.x * kScanThreads + threadIdx.x) * 4;
     if (at >= a.state) return;
     const Span sp = a.seq.of_sequence(b);
+    if (!a.seq.cut(sp.length)) return;
     const int place = r.first != nullptr || r.last != nullptr ? state_place(a, b) : -1;
     const int segs = (sp.length + a.seq.seg - 1) / a.seq.seg;
     const float rate = uniform(decay_rate(a.g[hk]));
     f4 x = f4{0.0f, 0.0f, 0.0f, 0.0f};
     if (r.first != nullptr && place >= 0) x = *reinterpret_cast<const f4 *>(a.place(r.first, place, hk) + at);
-    float *p = a.place(r.sums_out, sp.unit, hk) + at;
+    float *p = a.place(r.sums_out, sp.place, hk) + at;
     const long next = (long)a.Hk * a.state;
     const float whole = decay_pow(rate, a.seq.seg);
     const int sums = r.last != nullptr ? segs : segs - 1;    // (of the last segment only where the state behind it is asked for)
@@ -759,6 +761,7 @@ struct Plan {
     int seg = 0;             // 0: one pass
     int per_sequence = 1;
     bool shorts = false;     // decay_short_kernel, segments of 64 queries
+    bool whole = false;      // sequences of one segment are rows from their own first state to their own last
 };
 
 // What a call's rows take: workgroups of a segment and key/value head, and how many of them fill the GPU.
@@ -790,10 +793,13 @@ Plan make_plan(long T, int B, int H, int Hk, const Load &l, bool ragged, bool st
         p.shorts = true;
         seg = kChunk;
     } else if ((2 * groups <= l.fill || ragged) && longest > kLeast) {
-        // (of a ragged batch four times as many: the GPU is busy as long as there are segments left, and its longest sequence may be many times the mean)
-        const long parts = std::max(1L, (ragged ? kRagged : 1) * l.fill / groups);
-        seg = (mean + parts - 1) / parts;
+        // (of a ragged batch four times as many: the GPU is busy as long as there are segments left, and its longest sequence may be many times the mean; no
+        // more of them where there are more sequences and states than that)
+        const long most = ragged ? kRagged * l.fill : l.fill;
+        if (groups <= most) seg = (mean + most / groups - 1) / (most / groups);
+        else seg = (long)((double)mean * (double)groups / (double)most);
         if (seg < kLeast) seg = kLeast;
+        if (ragged && seg >= T) seg = 0;
     }
     if (!ragged && !p.shorts && seg >= T / B) seg = 0;
     if (seg > 0) {
@@ -801,6 +807,8 @@ Plan make_plan(long T, int B, int H, int Hk, const Load &l, bool ragged, bool st
             long power = kChunk;
             while (2 * power <= seg) power *= 2;
             seg = power;
+            // Of most sequences one segment: their states stay out of the workspace and their keys and values are read once
+            p.whole = !p.shorts && seg >= mean;
         } else {
             seg = (seg + kChunk - 1) / kChunk * kChunk;
             p.per_sequence = (int)((T / B + seg - 1) / seg);
@@ -812,15 +820,15 @@ Plan make_plan(long T, int B, int H, int Hk, const Load &l, bool ragged, bool st
 
 Sequences sequences(const int32_t *offsets, long T, int B, const Plan &p) {
     // one pass: one segment to a sequence, unit b is sequence b
-    Sequences s{offsets, (int)T, B, offsets == nullptr ? (int)(T / B) : 0, p.seg > 0 ? p.seg : 1 << 30, 30, p.per_sequence};
+    Sequences s{offsets, (int)T, B, offsets == nullptr ? (int)(T / B) : 0, p.seg > 0 ? p.seg : 1 << 30, 30, p.per_sequence, p.whole};
     while (s.log_seg > 0 && 1 << s.log_seg > s.seg) --s.log_seg;
     return s;
 }
 
 size_t plan_bytes(const Plan &p, long T, int B, bool ragged, int Hk, int d, int dv) {
     if (p.seg == 0 || p.shorts) return 0;
-    const long units = ragged ? T / p.seg + B : (long)p.per_sequence * B;
-    return (size_t)units * Hk * d * dv * sizeof(float);
+    const long places = p.whole ? 2 * (T / p.seg) : ragged ? T / p.seg + B : (long)p.per_sequence * B;
+    return (size_t)places * Hk * d * dv * sizeof(float);
 }
 
 template <class F>
@@ -892,7 +900,7 @@ int launch(const char *what, int type, Args a, const Plan &p, int states, hipStr
         const dim3 grid((unsigned)((a.state / 4 + kScanThreads - 1) / kScanThreads), (unsigned)(a.Hk * a.seq.B), (unsigned)states);
         decay_scan_kernel<<<grid, dim3(kScanThreads), 0, st>>>(a);
         SA_TRY(check_launch(what));
-        for (int r = 0; r < a.roles; ++r) a.role[r].first = nullptr, a.role[r].last = nullptr;
+        for (int r = 0; r < a.roles && !p.whole; ++r) a.role[r].first = nullptr, a.role[r].last = nullptr;
     }
     return by_forms(what, type, a, a.roles, false, [&](auto shape, dim3 grid, const Args &some) {
         typedef decltype(shape) S;

@@ -116,6 +116,16 @@ def test_workspaces_hold_what_is_asked_for(lib, T, B, ragged):      # noqa: F811
                                                    back, None) == HIP
 
 
+@pytest.mark.parametrize("T,B,H,Hk,d,dv", [(51200, 512, 32, 32, 128, 128), (51200, 512, 32, 32, 64, 64), (20000, 20000, 2, 2, 64, 64), (3000, 3000, 16, 16, 128, 128),
+                                             (5000, 40, 12, 4, 96, 72)])
+def test_short_ragged_sequences_take_no_places_of_their_own(lib, T, B, H, Hk, d, dv):      # noqa: F811
+    """A sequence of one segment (256 tokens at least) needs no state in the workspace, and there are T / 256 sequences of more at most, with T / 256 ends of
+    full segments: however many sequences there are, 2 T / 256 places."""
+    most = 2 * (T // 256) * 4 * Hk * d * dv
+    assert 0 < lib.sa_decay_attention_workspace_bytes(T, B, H, Hk, d, dv, 1) <= most
+    assert 0 < lib.sa_decay_attention_backward_workspace_bytes(T, B, H, Hk, d, dv, 1) <= 2 * most
+
+
 class Library:
     def __getattr__(self, name):
         return lambda *args: self.calls.append((name, args)) or 0

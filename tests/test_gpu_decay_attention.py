@@ -241,3 +241,59 @@ def test_states_hold_small_values_beside_large_ones(sa, lengths, H, Hk, d, dv):
     s["state_in"].zero_()
     want = reference(s, 0.1, lengths, gradients=True)["dstate_in"]
     right("dstate_in", got[3], want, s, subnormal(s, "q", "dout", 0.1, lengths, True))
+
+
+# most sequences of one segment (their mean is below 256), some of several, empty ones at the ends and between
+MIXED = [[0, 3, 900, 0, 40, 70, 1, 300, 5, 9, 257, 256, 0], [520, 5, 0, 9, 64, 100]]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,Hk,d,dv", [(3, 3, 64, 64), (6, 2, 96, 72), (2, 2, 128, 128)])
+@pytest.mark.parametrize("lengths", MIXED, ids=lambda l: "-".join(map(str, l)))
+@pytest.mark.parametrize("first,last", [(False, False), (True, False), (False, True), (True, True)])
+def test_short_sequences_among_long_ones(sa, lengths, H, Hk, d, dv, dtype, first, last):
+    """Sequences of one segment go from their own state to their own, those of several through the workspace."""
+    s = sequences(lengths, H, Hk, d, dv, dtype, seed=H + d, device="cuda", offset=2, behind=3)
+    if not first:
+        s["state_in"].zero_()
+    ws = torch.full((sa.sa_decay_attention_workspace_bytes(s["q"].shape[0], len(lengths), H, Hk, d, dv, True) // 4,), float("nan"), device="cuda")
+    assert ws.numel() > 0
+    o, left = sa.sa_decay_attention(s["q"], s["k"], s["v"], s["log_decay"], 0.2, offsets=s["offsets"], state_in=s["state_in"] if first else None,
+                                    want_state=last, out=torch.full_like(s["dout"], 7.0), workspace=ws)
+    want = reference(s, 0.2, lengths)
+    check("out", o, want["out"], s, 0.2, dtype, lengths)
+    assert bool((o[:2] == 7.0).all()) and bool((o[-3:] == 7.0).all())
+    if last:
+        check("state_out", left, want["state_out"], s, 0.2, dtype, lengths)
+
+
+def test_short_sequences_among_long_ones_in_place(sa):
+    """A cache's states in place; slots that are none."""
+    lengths, H, d = MIXED[0], 2, 64
+    s = sequences(lengths, H, H, d, d, torch.bfloat16, seed=8, device="cuda")
+    slots = torch.tensor([3, 14, 7, 0, -1, 9, 2, 15, 1, 4, 10, 99, 12], dtype=torch.int32, device="cuda")
+    cache = torch.randn(15, H, d, d, device="cuda")
+    before = cache.clone()
+    s["state_in"] = torch.stack([before[p] if 0 <= p < 15 else torch.zeros_like(before[0]) for p in slots.tolist()])
+    o, _ = sa.sa_decay_attention(s["q"], s["k"], s["v"], s["log_decay"], 0.1, offsets=s["offsets"], state_in=cache, state_out=cache, slots=slots)
+    want = reference(s, 0.1, lengths)
+    check("out", o, want["out"], s, 0.1, torch.bfloat16, lengths)
+    left = torch.stack([cache[p] if 0 <= p < 15 else want["state_out"][b].float() for b, p in enumerate(slots.tolist())])
+    check("state_out", left, want["state_out"], s, 0.1, torch.bfloat16, lengths)
+    others = [p for p in range(15) if p not in slots.tolist()]
+    assert torch.equal(cache[others], before[others])
+
+
+def test_offsets_that_are_none_among_short_sequences(sa):
+    """Offsets that descend or leave the tokens, in a batch whose sequences are short on average: nothing outside is read or written."""
+    T, H, d = 2000, 2, 64
+    s = sequences([T], H, H, d, d, torch.float32, seed=1, device="cuda")
+    bad = torch.randint(-3000, 5000, (8, 21), generator=torch.Generator().manual_seed(3)).to(torch.int32)
+    state = torch.randn(20, H, d, d, device="cuda")
+    need = sa.sa_decay_attention_workspace_bytes(T, 20, H, H, d, d, True) // 4
+    for off in bad:
+        guard, ws = torch.full((T + 200, H, d), 3.0, device="cuda"), torch.full((need + 2048,), 5.0, device="cuda")
+        sa.sa_decay_attention(s["q"], s["k"], s["v"], s["log_decay"], 0.1, offsets=off.cuda(), state_in=state, want_state=True, out=guard[100:T + 100],
+                              workspace=ws[1024:1024 + need])
+        assert bool((guard[:100] == 3.0).all()) and bool((guard[T + 100:] == 3.0).all())
+        assert bool((ws[:1024] == 5.0).all()) and bool((ws[1024 + need:] == 5.0).all())

@@ -183,3 +183,22 @@ def test_the_recurrence_token_by_token(sa, H, Hk, dtype):
             dstate[b] *= fade
     for name, g, want in zip(("dk", "dv", "dstate_in"), got[1:], (dk, dv_rows, dstate)):
         check(name, g, want, s, scale, dtype, lengths)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,Hk,d,dv", [(3, 3, 64, 64), (6, 2, 96, 72), (2, 1, 40, 128)])
+@pytest.mark.parametrize("state", [False, True])
+def test_short_sequences_among_long_ones(sa, H, Hk, d, dv, dtype, state):
+    """Most sequences of one segment (their mean is below 256), which take no state through the workspace."""
+    lengths = [0, 3, 900, 0, 40, 70, 1, 300, 5, 9, 257, 256, 0]
+    s = sequences(lengths, H, Hk, d, dv, dtype, seed=H + d, device="cuda", offset=2, behind=3)
+    ws = torch.full((sa.sa_decay_attention_backward_workspace_bytes(s["q"].shape[0], len(lengths), H, Hk, d, dv, True) // 4,), float("nan"), device="cuda")
+    outs = {n: torch.full_like(s[n[1:]], 7.0) for n in ("dq", "dk", "dv")}
+    got = sa.sa_decay_attention_backward(s["dout"], s["q"], s["k"], s["v"], s["log_decay"], 0.2, offsets=s["offsets"], workspace=ws, **outs,
+                                         state_in=s["state_in"] if state else None, dstate_out=s["dstate_out"] if state else None, want_dstate=state)
+    want = reference(s, 0.2, lengths, state=state, gradients=True)
+    for name, g in zip(("dq", "dk", "dv", "dstate_in"), got):
+        if g is not None:
+            check(name, g, want[name], s, 0.2, dtype, lengths, state)
+        if name != "dstate_in":
+            assert bool((g[:2] == 7.0).all()) and bool((g[-3:] == 7.0).all())
