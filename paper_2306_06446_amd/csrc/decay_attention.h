@@ -112,6 +112,19 @@ __device__ inline void product(f4 &c, const Vec<E, 8> (&a)[NA], const Vec<E, 8> 
     }
 }
 
+// Results of the matrix cores at the end of a way through the code that others join.  What reads them has to come 8 wait states later, and the compiler, which
+// sees to that, does not where it can also come to the place by a longer way: of 32 keys in fp16, the results of one of four wavefronts were read 2 wait
+// states behind their product, and wrong.
+template <int N>
+__device__ inline void settled(f4 (&x)[N]) {
+    each<N>([&](auto i) {
+        f4 y = x[i];
+        if constexpr (i + 1 < N) asm volatile("" : "+v"(y));
+        else asm volatile("s_nop 7" : "+v"(y));
+        x[i] = y;
+    });
+}
+
 // Four tokens of one column: the 16 lanes of a group point at 4 rows (lane / 4 % 4) and 4 blocks of 4 columns (lane % 4), lane l
 // gets column l % 16 of the 4 rows.
 template <class E>

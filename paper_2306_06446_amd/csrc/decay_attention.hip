@@ -306,6 +306,7 @@ struct State {
                     product<Terms<typename P::T>::ORDER_ADDED>(s[t], a, b);
                 });
             });
+            settled(s);
         }
     }
 };
@@ -428,6 +429,7 @@ __device__ inline void add_values(f4 (&o)[4], const Vec<typename P::E, 8> (&q)[P
             o[t] = sum;
         }
     });
+    settled(o);
 }
 
 // The same for a wavefront's own chunk: each wavefront has code of its own, without a branch in it, so that loads and products of its tiles overlap.
@@ -546,11 +548,11 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
             __syncthreads();
             int u = 0;
             do {
-                auto next_q = [&] {
-                    const bool turn = u + 1 == outs;
-                    if (end) qt.base += turn ? (uint64_t)qt.next - (uint64_t)(outs - 1) * kmore : kmore;
-                    q.load(qt, qat, turn && end ? next : n, kwidth);     // (the same again for the next head of the keys)
-                };
+                // (where they are is settled here: a branch between products and what reads them is one too many)
+                const bool turn = u + 1 == outs;
+                if (end) qt.base += turn ? (uint64_t)qt.next - (uint64_t)(outs - 1) * kmore : kmore;
+                const int next_n = turn && end ? next : n;
+                auto next_q = [&] { q.load(qt, qat, next_n, kwidth); };      // (the same again for the next head of the keys)
                 if (u > 0) q.arrived();
                 if (h == 0) each<4>([&](auto t) { o[t] = zeros(); });
                 float decayed = from_first;

@@ -557,6 +557,11 @@ __device__ __forceinline__ void nt_gemm_tile(const GemmArgs &g, const Store &sto
     } else {
         for (int s = 0; s < n_stages; ++s) stage(s, Ask{}, Ask{}, Ask{});
     }
+    // What reads the last products comes 12 wait states later at least.  (The compiler sees to that, but not where it can also come to the place by a longer
+    // way: it left 10 and 11.)
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 7\n\ts_nop 3");
+    __builtin_amdgcn_sched_barrier(0);
 
     // Transposed tile: accumulator register r of lane l holds row l % 32, column 8 (r / 4) + 4 (l / 32) + r % 4.
     // ---- sign codes: a wavefront's columns are one code word of a head or half of one; each half-wavefront has every
