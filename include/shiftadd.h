@@ -149,8 +149,9 @@ int sa_linear_attention_01(const uint64_t *q_codes, const uint64_t *k_codes, con
  * d and dv are multiples of 8, up to 128; H <= 4096, B * Hk <= 65535, T < 2^30, strides below 2^22 elements.  Rows and states begin at multiples of 16 bytes.
  * Sums and states are fp32 in a fixed order (the same call gives the same bits), q, k and v enter them exactly (fp16 below 2^-14, its subnormal numbers:
  * to 2^-38) and out is rounded once.  What rows of 16 bits are made of on the way, the products q k of a token and the state that it meets, enters them in more bits than
- * they have: bf16 to 2^-17 of each value; fp16 to 2^-22 of it, but no finer than 2^-39 of the largest of the token's products in its 64 tokens or of the state's column.  An infinity or NaN in a
- * token (fp32: 3.39e38 and more, in the state too) may make results of its sequence and head NaN from 63 tokens before it on, and the state; no others.
+ * they have: bf16 to 2^-17 of each value; fp16 to 2^-22 of it, but no finer than 2^-39 of the largest of the token's products in its 64 tokens or of the state's column.
+ * An infinity or NaN in a token (fp32: 3.39e38 and more, in the state too) reaches rows from that token on, as the formula has it, and the state, as an
+ * infinity or NaN; rows before it, whose bits stay the same, other heads and other sequences do not see it.
  * out may not overlap an input.
  * Workspace: states of segments of sequences that are cut: of equal ones where sequences and heads are too few to fill the GPU, of a ragged batch (offsets are
  * not known to the host) those that are longer than a segment, 256 tokens at least.  The query returns 0 where none can be; it asks for what any of
@@ -176,7 +177,7 @@ int sa_decay_attention_step(const void *q, long q_stride, const void *k, long k_
  *   dq_t = scale * S_t dout_t,   dk_t = R_t v_t,   dv_t = R_t^T k_t,   dstate_in = exp(log_decay) * R_0 (of an empty sequence dstate_out)
  * dq, dk, dv as q, k and v, of the same type; state_in_or_null as in the forward call (S is computed again), dstate_out_or_null and
  * dstate_in_or_null fp32 [B, Hk, d, dv].  No output may overlap an input or another output.  Sequences, types, sizes and workspace as above; an infinity or
- * NaN in a token may make the gradients of q of its sequence and head NaN from 63 tokens before it on, those of k and v up to 63 tokens behind it.
+ * NaN in a token reaches dq from that token on and dk and dv up to it.
  */
 size_t sa_decay_attention_backward_workspace_bytes(long T, int B, int H, int Hk, int d, int dv, int ragged);
 int sa_decay_attention_backward(const void *dout, long dout_stride, const void *q, long q_stride, const void *k, long k_stride,

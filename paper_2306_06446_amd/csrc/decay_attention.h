@@ -135,6 +135,13 @@ __device__ inline Vec<E, 4> read_transposed(const E *p) {
 template <class E>
 __device__ inline Vec<E, 8> join(const Vec<E, 4> &a, const Vec<E, 4> &b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
+// The thread's number once more, for what is seldom done and not worth registers for what could be made of it ahead.
+__device__ inline int thread_of(int wave) {
+    int lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+    asm volatile("" : "+v"(lane));
+    return 64 * wave + lane;
+}
+
 // What all lanes have the same, in a scalar register.
 // (The builtin's result is signed: as the low half of an address it would set all of the high one.)
 __device__ inline uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
@@ -173,6 +180,14 @@ struct Eight {
         }
     }
 };
+// What is not finite as an operand of the matrix cores (the first term of an fp32 value, too, that is rounded to infinity): one by one, and two at a time,
+// whose products with zero are added to a sum of zeros.
+__device__ inline bool not_finite(bf16_t x) { return (__builtin_bit_cast(uint16_t, x) & 0x7fffu) >= 0x7f80u; }
+__device__ inline bool not_finite(f16_t x) { return (__builtin_bit_cast(uint16_t, x) & 0x7fffu) >= 0x7c00u; }
+__device__ inline float times_zero(const Vec<f16_t, 2> &x, float sum) { return __builtin_amdgcn_fdot2(x, Vec<f16_t, 2>{(f16_t)0.0f, (f16_t)0.0f}, sum, false); }
+__device__ inline float times_zero(const Vec<bf16_t, 2> &x, float sum) {
+    return __builtin_amdgcn_fdot2_f32_bf16(x, Vec<bf16_t, 2>{(bf16_t)0.0f, (bf16_t)0.0f}, sum, false);
+}
 // STREAM: past the caches' reuse order, for results that fill whole lines of 128 bytes (gradient of 64 x 197 tokens, 12 heads of 64, bf16: 58 -> 50 us; rows
 // of 144 bytes, which do not, lost 6 %).
 template <class T, bool STREAM>

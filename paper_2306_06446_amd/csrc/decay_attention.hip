@@ -76,6 +76,16 @@ struct Shape {
     // 16 a + 4 t + b of 64, so that a lane's results are 16 columns side by side while a tile's columns are side by side in LDS.
     // (fp16) The columns' scales are behind the values' rows, 8 to a row: 256 bytes more would be a workgroup less of keys of 96 on a CU.
     static __device__ inline float *down(E (*vl)[kChunk][VP], int at) { return reinterpret_cast<float *>(&vl[0][at >> 3][COLS]) + (at & 7); }
+    // Values that are not finite: a zero takes their place in the products, as zero products of earlier rows with them would be NaN, and what comes behind them
+    // is NaN in memory.  Behind the keys' rows in LDS, 8 to a row: each column's first place in the segment that has one, and whether any has.  (Looking for them
+    // takes 0 to 3 % of a call, 7 of fp16 with keys of 128: 16384 tokens, 16 heads, 144 -> 154 us.)
+    static constexpr int kNone = 0x7fffffff;
+    static __device__ inline int *spoilt(E (*kl)[kChunk][KP], int at) { return reinterpret_cast<int *>(&kl[0][at >> 3][DK]) + (at & 7); }
+    static __device__ inline int *any_spoilt(E (*kl)[kChunk][KP]) { return spoilt(kl, 128); }
+    static __device__ inline void none_spoilt(E (*kl)[kChunk][KP]) {
+        if ((int)threadIdx.x < COLS) *spoilt(kl, (int)threadIdx.x) = kNone;
+        if ((int)threadIdx.x == COLS) *any_spoilt(kl) = 0;
+    }
     static __device__ inline int column(int at) { return (at & ~63) + 16 * ((at & 15) >> 2) + 4 * ((at & 63) >> 4) + (at & 3); }
     static constexpr int KPIECES = kChunk * DK / 8 / THREADS, VPIECES = kChunk * COLS / 8 / THREADS;
     static constexpr int TILES = DK / 16;
@@ -123,25 +133,42 @@ struct Rows {
         each<KN>([&](auto j) { k[j].load(kp, kat[j] - kt.skipped(n)); });
         each<VN>([&](auto j) { v[j].load(vp, vat[j] - vt.skipped(n)); });
     }
-    __device__ inline void stage(E (*kl)[kChunk][P::KP], E (*vl)[kChunk][P::VP]) const {
+    // 8 columns are 4 of each of two tiles
+    __device__ inline static int vplace(int col) { return (col & ~63) + 16 * ((col & 8) >> 2) + 4 * ((col & 63) >> 4); }
+    // (the chunk begins at place c of the segment)
+    __device__ inline static void remove(E (*kl)[kChunk][P::KP], E (*vl)[kChunk][P::VP], int c, int wave) {
+        const int thread = thread_of(wave);
+#pragma unroll 1
+        for (int i = 0; i < 8 * VN; ++i) {
+            const int piece = thread + P::THREADS * (i >> 3), row = piece / (P::COLS / 8), at = vplace(piece % (P::COLS / 8) * 8) + (i & 3) + 4 * (i & 4);
+            if (!not_finite(vl[0][row][at])) continue;
+            each<P::RAW>([&](auto p) { vl[p][row][at] = (E)0.0f; });
+            atomicMin(P::spoilt(kl, at), c + row);
+            *P::any_spoilt(kl) = 1;
+        }
+    }
+    // Whether all values are finite as operands.
+    __device__ inline bool stage(E (*kl)[kChunk][P::KP], E (*vl)[kChunk][P::VP]) const {
         each<KN>([&](auto j_) {
             constexpr int j = j_;
             Vec<E, 8> t[P::RAW];
             k[j].terms(t);
             each<P::RAW>([&](auto p) { *reinterpret_cast<Vec<E, 8> *>(&kl[p][krow(j)][kcol(j)]) = t[p]; });
         });
+        float nothing = 0.0f;        // NaN else
         each<VN>([&](auto j_) {
             constexpr int j = j_;
             Vec<E, 8> t[P::RAW];
             v[j].terms(t);
+            each<4>([&](auto i) { nothing = times_zero(Vec<E, 2>{t[0][2 * i], t[0][2 * i + 1]}, nothing); });
             each<P::RAW>([&](auto p_) {
                 constexpr int p = p_;
-                // 8 columns are 4 of each of two tiles
-                E *to = &vl[p][vrow(j)][(vcol(j) & ~63) + 16 * ((vcol(j) & 8) >> 2) + 4 * ((vcol(j) & 63) >> 4)];
+                E *to = &vl[p][vrow(j)][vplace(vcol(j))];
                 *reinterpret_cast<Vec<E, 4> *>(to) = __builtin_shufflevector(t[p], t[p], 0, 1, 2, 3);
                 *reinterpret_cast<Vec<E, 4> *>(to + 16) = __builtin_shufflevector(t[p], t[p], 4, 5, 6, 7);
             });
         });
+        return nothing == 0.0f;
     }
 };
 
@@ -172,8 +199,8 @@ struct State {
             }
         });
     }
-    __device__ inline void store(float *p, bool transposed, int rows, int cols, int dv, int c0) const {
-        const int lane = (int)threadIdx.x & 63, g = lane >> 4, col = c0 + P::column(16 * ((int)threadIdx.x >> 6) + (lane & 15));
+    __device__ inline void store(float *p, bool transposed, int rows, int cols, int dv, int c0, int thread) const {
+        const int lane = thread & 63, g = lane >> 4, col = c0 + P::column(16 * (thread >> 6) + (lane & 15));
         if (col >= cols) return;
         each<P::TILES>([&](auto t_) {
             constexpr int t = t_;
@@ -188,6 +215,10 @@ struct State {
                 });
             }
         });
+    }
+    __device__ inline void spoil(E (*kl)[kChunk][P::KP], int thread) {
+        if (*P::spoilt(kl, 16 * (thread >> 6) + (thread & 15)) == P::kNone) return;
+        each<P::TILES>([&](auto t) { s[t] = f4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")}; });
     }
     // To LDS as terms, for the product with q: [column][row].
     __device__ inline void stage(E (*sl)[P::COLS][P::KP], E (*vl)[kChunk][P::VP]) const {
@@ -272,7 +303,7 @@ struct State {
                             const u4 size = __builtin_bit_cast(u4, a[0]) & 0x7fff7fffu;
                             sum = matrix(__builtin_bit_cast(Vec<E, 8>, size), sign[ks], sum);
                         });
-                        each<4>([&](auto e) { most = fmaxf(most, sum[(int)e]); });
+                        each<4>([&](auto e) { most = fmaxf(most, sum[(int)e] < __builtin_inff() ? sum[(int)e] : 0.0f); });       // (a row that is not finite has no say)
                     });
                     __builtin_amdgcn_sched_barrier(0);
                     more = __any(top > 0.0f && most > 0.0f);          // (not in a column of zeros, as those behind the last are)
@@ -443,6 +474,17 @@ __device__ inline void add_own_values(f4 (&o)[4], const Vec<typename P::E, 8> (&
     else add_values<P, 3>(o, q, kl, vl, half, inside, from_first, behind, keys_done);
 }
 
+// Results of the chunk at place c of the segment behind values that are not finite.
+template <class P>
+__device__ inline void spoil_rows(f4 (&o)[4], typename P::E (*kl)[kChunk][P::KP], int c, int wave) {
+    typedef int i4 __attribute__((ext_vector_type(4)));
+    const int thread = thread_of(wave), g = (thread & 63) >> 4, half = kHalf * (thread >> 8), query = c + 16 * (thread >> 6 & 3) + (thread & 15);
+    each<4>([&](auto t) {
+        const i4 first = *reinterpret_cast<const i4 *>(P::spoilt(kl, half + 16 * t + 4 * g));
+        each<4>([&](auto e) { o[t][(int)e] = query >= first[(int)e] ? __builtin_nanf("") : o[t][(int)e]; });
+    });
+}
+
 // Wavefronts on a SIMD: as many workgroups as have room for their rows in a CU's LDS, unless registers would go to scratch memory, whose loads wait for
 // the rows that are under way (8 x 16384 tokens, 4 heads of 64, bf16: 65 us with 165 registers, 93 with 168 and 22 in memory).
 template <class P>
@@ -463,6 +505,7 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
     __shared__ __attribute__((aligned(16))) E vl[P::RAW][kChunk][P::VP];
     __shared__ __attribute__((aligned(16))) E sl[P::MADE][P::COLS][P::KP];
     __shared__ __attribute__((aligned(16))) float weight[kChunk], behind[kChunk];      // exp(g (64 - j)) in the latter
+    P::none_spoilt(kl);
     uint32_t unit, item;
     int hk;
     const Role &r = role_of(a, unit, hk, item);
@@ -534,8 +577,8 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
         if (n < kChunk) carry = uniform(decay_pow(rate, n));
         int h = 0;
         do {
-            if (c + h > 0) __syncthreads();
-            rows.stage(kl, vl);
+            __syncthreads();
+            if (__builtin_expect(!rows.stage(kl, vl), 0)) rows.remove(kl, vl, c * kChunk, wave);
             if (h == 0) {
                 if (n < kChunk && c > 0) stage_weights(weight, rate, n, shift, update);
                 if (live) state.stage(sl, vl);
@@ -546,6 +589,7 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
             vt.base += end ? (uint64_t)vt.next - (uint64_t)(sums - 1) * vmore : vmore;
             rows.load(kt, vt, end ? next : n);
             __syncthreads();
+            const int spoilt = *P::any_spoilt(kl);
             int u = 0;
             do {
                 // (where they are is settled here: a branch between products and what reads them is one too many)
@@ -574,6 +618,7 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
                     });
                 }
                 add_own_values<P>(o, q.t, kl, vl, w, half, inside, scale * decayed, behind, next_q);
+                if (uniform((uint32_t)spoilt) != 0) spoil_rows<P>(o, kl, c * kChunk, wave);
                 store(end ? n : 0, (uint64_t)u * vmore, o);
             } while (++u < outs);
             // (a state that only rows in 16 bits are made of takes the terms that these do)
@@ -585,7 +630,11 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_rows_kern
         ot.base += (uint64_t)ot.next;
         live = live || add;
     }
-    if (last != nullptr) state.store(last, transposed, kwidth, vwidth, a.dv, c0);
+    if (last != nullptr) {
+        const int thread = thread_of(wave);
+        if (chunks > 0) state.spoil(kl, thread);
+        state.store(last, transposed, kwidth, vwidth, a.dv, c0, thread);
+    }
 }
 
 // Few short sequences without a state before or behind them (197 tokens, 3 heads of 64, fp32: 21 -> 12 us on the device; with 768 sequences and heads of 197
@@ -598,6 +647,7 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_short_ker
     __shared__ __attribute__((aligned(16))) E kl[P::RAW][kChunk][P::KP];
     __shared__ __attribute__((aligned(16))) E vl[P::RAW][kChunk][P::VP];
     __shared__ __attribute__((aligned(16))) float behind[kChunk];
+    P::none_spoilt(kl);
     uint32_t unit, item;
     int hk;
     const Role &r = role_of(a, unit, hk, item);
@@ -635,8 +685,8 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_short_ker
     q.arrived();
     for (int c = 0; c <= sp.seg; ++c) {
         for (int h = 0; h < sums; ++h) {
-            if (c + h > 0) __syncthreads();
-            rows.stage(kl, vl);
+            __syncthreads();
+            if (__builtin_expect(!rows.stage(kl, vl), 0)) rows.remove(kl, vl, c * kChunk, wave);
             const bool end = h + 1 == sums;
             kt.base += end ? (uint64_t)kt.next - (uint64_t)(sums - 1) * kmore : kmore;
             vt.base += end ? (uint64_t)vt.next - (uint64_t)(sums - 1) * vmore : vmore;
@@ -646,6 +696,7 @@ __global__ __launch_bounds__(P::THREADS, (rows_waves<P>())) void decay_short_ker
             else add_own_values<P>(o, q.t, kl, vl, w, half, inside, from_first, behind, [] {});
         }
     }
+    if (*P::any_spoilt(kl) != 0) spoil_rows<P>(o, kl, sp.seg * kChunk, wave);
     const __amdgpu_buffer_rsrc_t to = ot.rows(mine);
     each<2>([&](auto p) {
         float x[8];
@@ -704,7 +755,7 @@ __global__ __launch_bounds__(P::THREADS) void decay_states_kernel(const Args a) 
             else state.template update<P::MADE, false>(kl, vl, weight, h == 0 ? carry : 1.0f);
         }
     }
-    state.store(a.place(r.sums_out, sp.place, hk), r.transposed, kwidth, vwidth, a.dv, c0);
+    state.store(a.place(r.sums_out, sp.place, hk), r.transposed, kwidth, vwidth, a.dv, c0, (int)threadIdx.x);
 }
 
 // From the segments' sums to the states before them, in their place, and to the state behind the sequence.  A thread has 4 elements, 16 segments of them

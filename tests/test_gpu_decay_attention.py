@@ -297,3 +297,58 @@ def test_offsets_that_are_none_among_short_sequences(sa):
                               workspace=ws[1024:1024 + need])
         assert bool((guard[:100] == 3.0).all()) and bool((guard[T + 100:] == 3.0).all())
         assert bool((ws[:1024] == 5.0).all()) and bool((ws[1024 + need:] == 5.0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lengths", [[130, 90], [1400, 70], [197]], ids=lambda l: "-".join(map(str, l)))
+@pytest.mark.parametrize("state", [False, True])
+@pytest.mark.parametrize("H,Hk,d,dv", [(2, 2, 64, 64), (4, 2, 96, 72), (2, 2, 128, 128), (2, 2, 64, 104), (3, 3, 32, 40)])
+def test_rows_before_what_is_not_finite_stay_as_they_are(sa, lengths, H, Hk, d, dv, dtype, state):
+    """Rows do not see later tokens, whatever is in them: the same bits; from the token on the columns of its values are NaN, all others the same bits."""
+    s = sequences(lengths, H, Hk, d, dv, dtype, seed=4, device="cuda")
+    clean, left = run(sa, s, 0.1, state)
+    N, G = lengths[0], H // Hk
+    for at in sorted({0, 37, N - 20, N - 1}):
+        for name, value in (("q", float("nan")), ("k", float("nan")), ("k", -float("inf")), ("v", float("nan")), ("v", float("inf"))):
+            bad = dict(s, **{name: s[name].clone()})
+            bad[name][at, 1, 5] = value
+            o, last = run(sa, bad, 0.1, state)
+            heads = slice(1, 2) if name == "q" else slice(G, 2 * G)
+            rest = o.clone()
+            if name == "q":
+                assert not o[at, 1].isfinite().any() and torch.equal(o[at + 1:N], clean[at + 1:N])
+                rest[at, heads] = clean[at, heads]
+            elif name == "k":
+                assert not o[at, heads].isfinite().any()
+                rest[at:N, heads] = clean[at:N, heads]
+            else:
+                assert o[at:N, heads, 5].isnan().all()
+                rest[at:N, heads, 5] = clean[at:N, heads, 5]
+            assert torch.equal(rest, clean), (name, at)
+            if state:
+                same = last.clone()
+                if name == "k":
+                    assert not last[0, 1, 5].isfinite().any()
+                    same[0, 1, 5] = left[0, 1, 5]
+                if name == "v":
+                    assert last[0, 1, :, 5].isnan().all()
+                    same[0, 1, :, 5] = left[0, 1, :, 5]
+                assert torch.equal(same, left), (name, at)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,N", [(3, 200), (2, 1500), (300, 100)])
+def test_padding_of_any_bits(sa, B, N, dtype):
+    """A padded batch of one length, whose rows behind each sequence's tokens are whatever was in memory."""
+    H, d = 4, 64
+    s = sequences([N] * B, H, H, d, d, dtype, seed=5, device="cuda")
+    q, k, v = (s[n].view(B, N, H, d) for n in ("q", "k", "v"))
+    clean, _ = sa.sa_decay_attention(q, k, v, s["log_decay"], 0.1)
+    valid = torch.randint(0, N + 1, (B,), generator=torch.Generator().manual_seed(1)).cuda()
+    behind = torch.arange(N, device="cuda")[None, :] >= valid[:, None]
+    junk = torch.randint(-2 ** 31, 2 ** 31 - 1, (B, N, H, d), generator=torch.Generator(device="cuda").manual_seed(2), device="cuda").to(torch.int32)
+    junk = junk.view(dtype)[..., :d]
+    q, k, v = (torch.where(behind[..., None, None], junk.roll(i, 1), t) for i, t in enumerate((q, k, v)))
+    assert not v.isfinite().all()
+    o, _ = sa.sa_decay_attention(q, k, v, s["log_decay"], 0.1)
+    assert torch.equal(o[~behind], clean[~behind])

@@ -202,3 +202,31 @@ def test_short_sequences_among_long_ones(sa, H, Hk, d, dv, dtype, state):
             check(name, g, want[name], s, 0.2, dtype, lengths, state)
         if name != "dstate_in":
             assert bool((g[:2] == 7.0).all()) and bool((g[-3:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N", [197, 1400])
+@pytest.mark.parametrize("H,Hk,d,dv", [(2, 2, 64, 64), (4, 2, 96, 72), (2, 2, 128, 128)])
+def test_gradients_of_what_does_not_see_it_stay_as_they_are(sa, N, H, Hk, d, dv, dtype):
+    """What is not finite in a token reaches dq of later tokens alone, dk and dv of earlier ones alone: all others have the same bits."""
+    s = sequences([N, 30], H, Hk, d, dv, dtype, seed=4, device="cuda")
+    call = lambda s: sa.sa_decay_attention_backward(s["dout"], s["q"], s["k"], s["v"], s["log_decay"], 0.1, offsets=s["offsets"], want_dstate=True)      # noqa: E731
+    clean = call(s)
+    none = slice(0, 0)
+    for at in (0, 70, N - 1):
+        on, up, own = slice(at, N), slice(0, at + 1), slice(at, at + 1)
+        #                 rows of dq, dk and dv that see the token (dq does not depend on q, dk not on k, dv not on v; the token's own dq on its dout)
+        for name, sees in (("dout", (own, up, up)), ("q", (none, up, up)), ("k", (on, none, own)), ("v", (on, own, none))):
+            bad = dict(s, **{name: s[name].clone()})
+            bad[name][at, -1, 3] = float("nan")
+            got = call(bad)
+            for g, c, rows, label in zip(got, clean, sees, ("dq", "dk", "dv")):
+                heads = slice(H - 1, H) if name in ("dout", "q") and label == "dq" else slice((Hk - 1) * (g.shape[1] // Hk), g.shape[1])
+                rest = g.clone()
+                rest[rows, heads] = c[rows, heads]
+                assert torch.equal(rest, c), (name, at, label)
+                assert rows == none or not g[rows, heads].isfinite().all(), (name, at, label)
+            if name in ("k", "v"):
+                assert torch.equal(got[3], clean[3])
+            else:
+                assert torch.equal(got[3][:, :Hk - 1], clean[3][:, :Hk - 1]) and torch.equal(got[3][1:], clean[3][1:]) and got[3][0, -1].isnan().any()
