@@ -14,11 +14,11 @@
 // before them (decay_scan_kernel), the rows from there (decay_rows_kernel).  Keys and values are then read twice.  Few short sequences need
 // no state (decay_short_kernel).
 //
-// What bounds it, with keys of up to 64 in 16 bits: memory.  8 x 16384 tokens, 4 heads of 64, bf16: rows 53 us (268 MB, 5 TB/s), sums of the segments 33
-// (134 MB), their scan 6; 64 x 197 tokens, 12 heads of 64, one pass: 20 us (77 MB, 15 at a copy's rate).  Its gradient at 8 x 16384: rows 135 us,
-// 805 MB through the memory-side cache of which 430 come from memory.  With keys of 128, latency: 16384 tokens, 16 heads of 128, bf16: rows
-// 81 us (268 MB; vector ALU 31 %, LDS 37 %, matrix cores 21 % of the time), as the terms of the state take 70 KB of LDS and 200 registers leave two
-// wavefronts to a SIMD.  The same of fp32, whose operands are three terms: 8 x 16384 tokens, 4 heads of 64: 234 us in all (537 MB, 107 us).
+// What bounds it, with keys of up to 64 in 16 bits: memory.  8 x 16384 tokens, 4 heads of 64, bf16 (medians of launches one after the other): rows 54 us (268 MB,
+// 5 TB/s), sums of the segments 34 (134 MB), their scan 7.6; 64 x 197 tokens, 12 heads of 64, one pass: 21 us (77 MB, 15 at a copy's rate).  Its gradient at 8 x 16384:
+// rows 140 to 172 us, 805 MB through the memory-side cache of which 430 come from memory.  With keys of 128, latency: 16384 tokens, 16 heads of 128, bf16: rows 82 us (268 MB;
+// vector ALU 31 %, LDS 37 %, matrix cores 21 % of the time), as the terms of the state take 70 KB of LDS and 187 registers leave two wavefronts to a SIMD.  The same of
+// fp32, whose operands are three terms: 8 x 16384 tokens, 4 heads of 64: 238 us in all (537 MB, 107 us).
 #include <algorithm>
 #include <initializer_list>
 #include <type_traits>
