@@ -70,3 +70,50 @@ def test_thousands(sa, B, T):
         check("state_out", last[b:b + 1], want["state_out"], one, 0.3, torch.bfloat16, [lengths[b]])
     empty = [b for b in range(B) if not lengths[b]]
     assert torch.equal(last[empty], s["state_in"][empty])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+def test_two_streams_and_a_graph(sa, dtype):
+    """Short sequences among long ones: two calls at once on streams of their own, with a workspace each, and a captured step that is replayed on other values:
+    the bits of calls by themselves."""
+    B, T, H, d = 80, 4000, 2, 64
+    lengths = lengths_of(B, T, 3)
+    sets = [sequences(lengths, H, H, d, d, dtype, seed=i, device="cuda") for i in range(3)]
+
+    def step(s, buffers):
+        o, last, grads, ws = buffers
+        sa.sa_decay_attention(s["q"], s["k"], s["v"], s["log_decay"], 0.1, offsets=s["offsets"], state_in=s["state_in"], out=o, state_out=last, workspace=ws[0])
+        sa.sa_decay_attention_backward(s["dout"], s["q"], s["k"], s["v"], s["log_decay"], 0.1, offsets=s["offsets"], state_in=s["state_in"],
+                                       dstate_out=s["dstate_out"], workspace=ws[1], **grads)
+        return [o, last] + list(grads.values())
+
+    def buffers():
+        s = sets[0]
+        ws = [torch.empty(max(16, n), dtype=torch.uint8, device="cuda") for n in (
+            sa.sa_decay_attention_workspace_bytes(T, B, H, H, d, d, True), sa.sa_decay_attention_backward_workspace_bytes(T, B, H, H, d, d, True))]
+        return (torch.zeros_like(s["dout"]), torch.empty_like(s["state_in"]),
+                dict(dq=torch.zeros_like(s["q"]), dk=torch.zeros_like(s["k"]), dv=torch.zeros_like(s["v"]), dstate_in=torch.empty_like(s["state_in"])), ws)
+
+    alone = [[t.clone() for t in step(s, buffers())] for s in sets]
+    streams, own = [torch.cuda.Stream() for _ in range(2)], [buffers() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for stream, s, b in zip(streams, sets, own):
+            with torch.cuda.stream(stream):
+                got = step(s, b)
+    torch.cuda.synchronize()
+    for want, (o, last, grads, _) in zip(alone, own):
+        assert all(torch.equal(a, b) for a, b in zip(want, [o, last] + list(grads.values())))
+    s, b, graph = {n: t.clone() for n, t in sets[0].items()}, own[0], torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=streams[0]):
+        got = step(s, b)
+    for i in (2, 0, 1, 2):
+        for n, t in s.items():
+            t.copy_(sets[i][n])
+        for t in got:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, alone[i])), i
+        torch.randn(1000, 1000, device="cuda").sum()
